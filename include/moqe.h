@@ -15,7 +15,9 @@
  * Beside the block: the paper's two router models (moqe_route_nlp, moqe_route_cv; Section 3.2), whose choice
  * drives the block through moqe_forward_routed; the router-training label pass and the load-balance
  * statistics of Section 3.3 (moqe_label_pass, moqe_balance_stats); samples of different lengths
- * (moqe_*_ragged); on-demand residency of the experts' weights (moqe_cache_*, Section 4.4).
+ * (moqe_*_ragged); on-demand residency of the experts' weights (moqe_cache_*, Section 4.4).  What a decoder layer of
+ * an expert does around its products: norms with the residual (moqe_residual_norm), rotary positions and a paged key/value
+ * cache in 8 bits (moqe_kv_append), attention over that cache (moqe_kv_attention).
  *
  * Conventions (all entry points).
  *  - Return value: 0 on success, a negative MOQE_E_* code on failure.  Every argument
@@ -28,7 +30,8 @@
  *    cache (moqe_cache_create) owns the device slots it allocates until moqe_cache_destroy.
  *    An activation matrix (rows x features, bf16) and a packed weight matrix must each stay below 4 GiB
  *    (the kernels address them with 32-bit byte offsets; larger ones are refused with MOQE_E_SHAPE).  Descriptor structs
- *    (moqe_qmat, moqe_router, moqe_nlp_router, moqe_cv_router, moqe_block, moqe_aux) and arrays of them are HOST memory,
+ *    (moqe_qmat, moqe_router, moqe_nlp_router, moqe_cv_router, moqe_block, moqe_aux, moqe_norm, moqe_residual_step,
+ *    moqe_kv_cache, moqe_kv_batch, moqe_rope, moqe_attention) and arrays of them are HOST memory,
  *    read during the call only.  Scratch memory is a caller-provided device workspace
  *    whose size comes from the matching *_workspace_bytes query; it must be 256-byte
  *    aligned and may be reused between calls on the same stream.
@@ -405,6 +408,105 @@ int32_t moqe_cache_destroy(moqe_expert_cache* cache);
 int32_t moqe_cache_acquire(moqe_expert_cache* cache, const int32_t* want, int32_t n, void** dev_ptrs,
                            int32_t* copied, void* stream);
 int32_t moqe_cache_stats(const moqe_expert_cache* cache, uint64_t* copies, uint64_t* copied_bytes);
+
+/* ---- a decoder layer around the products ---------------------------------------------- */
+
+/* Norms before and after a block, with the block's gate and residual scale.  For rows i < M of d features, in fp32:
+ *   u = y_i, or post(y_i) when post.kind is not MOQE_NORM_NONE
+ *   t = residual_i + scale * gate (.) u        (no gate: ones;  y NULL: t = residual_i)
+ *   residual_out_i = t, rounded to the residual's type;  out_i = bf16(pre(t))  (pre of the unrounded t)
+ * MOQE_NORM_RMS  : x / sqrt(mean(x^2) + eps) * gain;   MOQE_NORM_LAYER: (x - mean) / sqrt(biased variance + eps) * gain + offset.
+ *   gain, offset : device float [d]; NULL: ones, zeros (offset only with MOQE_NORM_LAYER)
+ *   y            : MOQE_TYPE_F32 or MOQE_TYPE_BF16 rows (what moqe_forward wrote), row i at element i * y_stride
+ *   residual     : rows of residual_type; residual_out may be NULL (not kept) or the same memory as residual (same stride then)
+ *   gate         : device float [d], or with gate_rows > 0 [ceil(M / gate_rows), d]: row i takes gate row i / gate_rows
+ *   out          : bf16 rows, or NULL (then pre is not evaluated)
+ * d <= 32768.  Strides are in elements and at least d.  Sizes that are multiples of 8 on 16-byte aligned rows take wide loads, any others
+ * work too.  Sums in a fixed order (deterministic).  One launch; M == 0 is a no-op. */
+#define MOQE_TYPE_F32    0
+#define MOQE_TYPE_BF16   1
+#define MOQE_NORM_NONE   0
+#define MOQE_NORM_RMS    1
+#define MOQE_NORM_LAYER  2
+typedef struct moqe_norm { const float *gain, *offset; int32_t kind; float eps; } moqe_norm;
+typedef struct moqe_residual_step {
+  const void* y; const void* residual; void* residual_out; void* out; const float* gate;   /* device */
+  int64_t y_stride, residual_stride, residual_out_stride, out_stride;
+  moqe_norm post, pre;
+  int32_t M, d, y_type, residual_type, gate_rows;
+  float scale;
+} moqe_residual_step;
+int32_t moqe_residual_norm(const moqe_residual_step* step, void* stream);
+
+/* A paged key/value cache in 8 bits.  A block holds block_tokens (32, 64 or 128) consecutive tokens of one sequence, for every key head:
+ * e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; largest 448, no infinities) of the keys and of the values, and one power-of-two scale for
+ * the keys and one for the values of each block and head; an element is scale * code.  With a power of two a growing scale moves
+ * codes exactly (but for those that become subnormal), and scale * code is exact in bf16.
+ *   k, v             : device, 16-byte aligned, moqe_kv_codes_bytes(cache) bytes each; k_scale, v_scale: device float [n_blocks, n_heads]
+ * Nothing of it has to be cleared before its first use.
+ * Codes of one block and head, in the order in which matrix cores take them (16 bytes for each of 64 lanes):
+ *   keys   [block_tokens / 16][head_dim / 64][lane 16 kq + r][16]  byte 8 st + i: token r, dim 32 st + 8 kq + i
+ *   values [block_tokens / 32][head_dim / 32][lane 16 kq + r][16]  byte 8 dt + i: dim 16 dt + r, token 4 kq + i (i < 4) or 12 + 4 kq + i
+ * head_dim 64, 128 or 256. */
+typedef struct moqe_kv_cache {
+  uint8_t *k, *v; float *k_scale, *v_scale;
+  int32_t n_blocks, block_tokens, n_heads, head_dim;
+} moqe_kv_cache;
+size_t moqe_kv_codes_bytes(const moqe_kv_cache* cache);
+
+/* The sequences of a call.  Sequence s brings T new rows (rows s*T ..), or with cu_rows the rows cu_rows[s] .. cu_rows[s+1) of M in all, at most T
+ * of them.  They are its last tokens: kv_len[s] counts its tokens with them, so row i of n has position kv_len[s] - n + i.
+ *   block_table : device int32 [S, table_width]: block of tokens j * block_tokens ..  An entry outside [0, n_blocks) stands for an absent block
+ *                 (given back, or not needed by this call): nothing is written there, and its tokens are not seen.
+ *   kv_len      : device int32 [S]; values are taken into [0, table_width * block_tokens]
+ *   cu_rows     : device int32 [S+1] or NULL (then M = S*T); values are taken into [0, M], and rows past the first T of a sequence are not computed */
+typedef struct moqe_kv_batch {
+  const int32_t *block_table, *kv_len, *cu_rows;
+  int32_t S, T, M, table_width;
+} moqe_kv_batch;
+
+/* Rotary positions.  Of every query and key head the first rot_dim dims (a multiple of 16, 0: none) are turned in pairs (a, b) by the angle
+ * p * inv_freq[j] of the row's position p:  a' = mscale (a cos - b sin), b' = mscale (b cos + a sin);  pair j < rot_dim / 2 is dims
+ * (j, j + rot_dim / 2), or with interleaved (2j, 2j + 1).  inv_freq: device double [rot_dim / 2] (angles are reduced in 64 bits, so far positions keep
+ * their accuracy; how positions are scaled for long contexts is in this table and in mscale).
+ * q_gain, k_gain: device float [head_dim] or NULL: an RMS norm with eps of every query / key head before it is turned. */
+typedef struct moqe_rope {
+  const double* inv_freq; const float *q_gain, *k_gain;
+  float eps, mscale;
+  int32_t rot_dim, interleaved;
+} moqe_rope;
+
+/* Positions and cache of a layer's fused projection.  qkv: rows of n_heads query heads, cache->n_heads key heads and cache->n_heads value heads of head_dim,
+ * MOQE_TYPE_F32 or MOQE_TYPE_BF16, 16-byte aligned, row m at element m * qkv_stride (a multiple of 8).  Queries are turned and written as bf16 rows to
+ * q_out (row m at m * q_stride, 16-byte aligned, a multiple of 8).  Keys are turned, keys and values quantized to nearest (ties to even) from fp32:
+ *   need = the smallest power of two with max |x| <= 448 need over the call's finite values for this block and head (2^-120 .. 2^120);
+ *   if the block held earlier tokens of the sequence, scale = max(need, old scale), and where that grows their codes become e4m3(code * old / scale);
+ *   else scale = need.  Codes of tokens past kv_len keep what they hold.  Infinities become the largest code, NaN stays.
+ * Rows at positions below 0 are not stored.  No two sequences of a call may write the same block.  n_heads a multiple of cache->n_heads.
+ * One launch. */
+int32_t moqe_kv_append(const void* qkv, int32_t qkv_type, int64_t qkv_stride, int32_t n_heads, const moqe_rope* rope,
+                       const moqe_kv_batch* batch, const moqe_kv_cache* cache, void* q_out, int64_t q_stride, void* stream);
+
+/* Attention of a call's rows over the cache (after moqe_kv_append: over themselves too).  Query head h reads key head h / (n_heads / cache->n_heads):
+ *   a = scale * q . k_t;   cap > 0: a = cap * tanh(a / cap);   slopes: a -= slopes[h] * |p - t|
+ *   out = sum_t softmax(a)_t v_t over the tokens t that the row at position p sees:
+ *         t < kv_len, its block present, and (t < prefix, or t <= p and (window <= 0 or p - t < window))
+ * A row that sees nothing gives zeros; what lies in places that a row does not see has no influence on it, NaN included.
+ *   q, out : bf16 rows of n_heads * head_dim, 16-byte aligned, row strides multiples of 8 elements
+ *   slopes : device float [n_heads] or NULL (linear biases by distance);  prefix: device int32 [S] or NULL (tokens that every row of the sequence sees)
+ * Arithmetic: keys and values are exact in bf16; products on bf16 matrix cores with fp32 accumulation; scores, softmax and sums in fp32; the weights
+ * exp(a - max) are rounded to bf16 before their product with the values (as are q and out: 2^-8 of a value at most, errors that average out over the tokens).
+ * Sums run in an order that depends on sizes only (deterministic).  Few rows: the tokens are divided over work-groups by their number on the
+ * device, and a second launch joins the parts; workspace as the query says, 256-byte aligned. */
+typedef struct moqe_attention {
+  const float* slopes; const int32_t* prefix;
+  float scale, cap;
+  int32_t n_heads, window;
+} moqe_attention;
+size_t  moqe_kv_attention_workspace_bytes(const moqe_attention* attn, const moqe_kv_batch* batch, const moqe_kv_cache* cache);
+int32_t moqe_kv_attention(const void* q, int64_t q_stride, const moqe_attention* attn, const moqe_kv_batch* batch,
+                          const moqe_kv_cache* cache, void* out, int64_t out_stride,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- timing ------------------------------------------------------------------------- */
 

@@ -77,6 +77,37 @@ class _Aux(C.Structure):
                 ("offsets", C.c_void_p), ("perm", C.c_void_p), ("inv_perm", C.c_void_p), ("h", C.c_void_p)]
 
 
+class _Norm(C.Structure):
+    _fields_ = [("gain", C.c_void_p), ("offset", C.c_void_p), ("kind", C.c_int32), ("eps", C.c_float)]
+
+
+class _ResidualStep(C.Structure):
+    _fields_ = [("y", C.c_void_p), ("residual", C.c_void_p), ("residual_out", C.c_void_p), ("out", C.c_void_p), ("gate", C.c_void_p),
+                ("y_stride", C.c_int64), ("residual_stride", C.c_int64), ("residual_out_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("post", _Norm), ("pre", _Norm), ("M", C.c_int32), ("d", C.c_int32), ("y_type", C.c_int32),
+                ("residual_type", C.c_int32), ("gate_rows", C.c_int32), ("scale", C.c_float)]
+
+
+class _KvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_blocks", C.c_int32),
+                ("block_tokens", C.c_int32), ("n_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class _KvBatch(C.Structure):
+    _fields_ = [("block_table", C.c_void_p), ("kv_len", C.c_void_p), ("cu_rows", C.c_void_p), ("S", C.c_int32), ("T", C.c_int32),
+                ("M", C.c_int32), ("table_width", C.c_int32)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("eps", C.c_float), ("mscale", C.c_float),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("slopes", C.c_void_p), ("prefix", C.c_void_p), ("scale", C.c_float), ("cap", C.c_float), ("n_heads", C.c_int32),
+                ("window", C.c_int32)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2508_09204_amd.build` "
@@ -117,6 +148,12 @@ def _load() -> C.CDLL:
         "moqe_cache_destroy": (i32, [vp]),
         "moqe_cache_acquire": (i32, [vp, C.POINTER(i32), i32, C.POINTER(vp), C.POINTER(i32), vp]),
         "moqe_cache_stats": (i32, [vp, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]),
+        "moqe_residual_norm": (i32, [C.POINTER(_ResidualStep), vp]),
+        "moqe_kv_codes_bytes": (sz, [C.POINTER(_KvCache)]),
+        "moqe_kv_append": (i32, [vp, i32, C.c_int64, i32, C.POINTER(_Rope), C.POINTER(_KvBatch), C.POINTER(_KvCache), vp, C.c_int64, vp]),
+        "moqe_kv_attention_workspace_bytes": (sz, [C.POINTER(_Attention), C.POINTER(_KvBatch), C.POINTER(_KvCache)]),
+        "moqe_kv_attention": (i32, [vp, C.c_int64, C.POINTER(_Attention), C.POINTER(_KvBatch), C.POINTER(_KvCache), vp, C.c_int64,
+                                    vp, sz, vp]),
         "moqe_profile_enable": (i32, [i32]),
         "moqe_profile_read": (i32, [i32, C.POINTER(i32), C.POINTER(C.c_double)]),
     }
@@ -137,7 +174,8 @@ EXPORTED = ["moqe_version", "moqe_last_error_string", "moqe_set_dry_run", "moqe_
             "moqe_expand_rows", "moqe_workspace_bytes_ragged", "moqe_forward_ragged", "moqe_quantize_rtn", "moqe_packed_bytes", "moqe_pack_qmat",
             "moqe_unpack_qmat", "moqe_grouped_qgemm_workspace_bytes", "moqe_grouped_qgemm",
             "moqe_workspace_bytes", "moqe_forward", "moqe_forward_static", "moqe_workspace_bytes_routed", "moqe_forward_routed", "moqe_label_pass_workspace_bytes", "moqe_label_pass", "moqe_cache_create", "moqe_cache_destroy", "moqe_cache_acquire",
-            "moqe_cache_stats", "moqe_profile_enable", "moqe_profile_read"]
+            "moqe_cache_stats", "moqe_residual_norm", "moqe_kv_codes_bytes", "moqe_kv_append", "moqe_kv_attention_workspace_bytes",
+            "moqe_kv_attention", "moqe_profile_enable", "moqe_profile_read"]
 
 
 def _check(rc: int) -> None:
@@ -532,3 +570,219 @@ class ForwardCall:
         rc = lib.moqe_forward(*self._args, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
+
+
+# --------------------------------------------------------------------------------------
+# A decoder layer around the products
+# --------------------------------------------------------------------------------------
+TYPE_F32, TYPE_BF16 = 0, 1
+NORM_KINDS = {"none": 0, "rms": 1, "layer": 2}
+
+
+def _type_of(t: torch.Tensor, what: str) -> int:
+    if t.dtype == torch.float32:
+        return TYPE_F32
+    if t.dtype == torch.bfloat16:
+        return TYPE_BF16
+    raise TypeError(f"{what} must be float32 or bfloat16, not {t.dtype}")
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str, dtype=torch.float32) -> Optional[int]:
+    """Address of a contiguous tensor of n values that the library reads as `dtype`."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be {n} contiguous values of {dtype}")
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, M: int, width: int, what: str, dtype=None):
+    """Address and row stride of M rows of `width` values; trailing dimensions of a row have to be dense."""
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+    if t.dim() < 2 or t.shape[0] != M or t[0:1].numel() != width:
+        raise ValueError(f"{what} must have {M} rows of {width} values, got {tuple(t.shape)}")
+    n = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size > 1 and stride != n:
+            raise ValueError(f"the values of a row of {what} must be dense")
+        n *= size
+    return t.data_ptr(), t.stride(0) if M > 1 else max(t.stride(0), width)
+
+
+@dataclass
+class Norm:
+    """kind "rms" or "layer"; gain and offset fp32 [d] or None."""
+    kind: str
+    eps: float
+    gain: Optional[torch.Tensor] = None
+    offset: Optional[torch.Tensor] = None
+
+    def c(self, d: int) -> _Norm:
+        return _Norm(_vector(self.gain, d, "gain"), _vector(self.offset, d, "offset"), NORM_KINDS[self.kind], self.eps)
+
+
+class ResidualNormCall:
+    """moqe_residual_norm with its arguments marshalled once; calling it only enqueues the work.
+    y [M, d] fp32 or bf16 or None, residual [M, d] fp32 or bf16, out bf16 [M, d] or None, residual_out like residual (may be it) or None."""
+
+    def __init__(self, y: Optional[torch.Tensor], residual: torch.Tensor, out: Optional[torch.Tensor],
+                 residual_out: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
+                 scale: float = 1.0, post: Optional[Norm] = None, pre: Optional[Norm] = None):
+        M, d = residual.shape
+        s = _ResidualStep()
+        s.M, s.d, s.gate_rows, s.scale = M, d, gate_rows, scale
+        s.residual_type = _type_of(residual, "residual")
+        s.residual, s.residual_stride = _rows(residual, M, d, "residual")
+        if y is not None:
+            s.y_type = _type_of(y, "y")
+            s.y, s.y_stride = _rows(y, M, d, "y")
+        if residual_out is not None:
+            s.residual_out, s.residual_out_stride = _rows(residual_out, M, d, "residual_out", residual.dtype)
+        if out is not None:
+            s.out, s.out_stride = _rows(out, M, d, "out", torch.bfloat16)
+        s.gate = _vector(gate, d * (-(-M // gate_rows) if gate_rows > 0 else 1), "gate")
+        s.post = post.c(d) if post is not None else _Norm()
+        s.pre = pre.c(d) if pre is not None else _Norm()
+        self._keep = (y, residual, out, residual_out, gate, post, pre)
+        self._step = s
+        self._arg = C.byref(s)
+
+    def __call__(self, stream: Optional[int] = None) -> None:
+        rc = lib.moqe_residual_norm(self._arg, _stream() if stream is None else stream)
+        if rc != 0:
+            _check(rc)
+
+
+def moqe_residual_norm(y: Optional[torch.Tensor], residual: torch.Tensor, out: Optional[torch.Tensor],
+                       residual_out: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
+                       scale: float = 1.0, post: Optional[Norm] = None, pre: Optional[Norm] = None) -> None:
+    ResidualNormCall(y, residual, out, residual_out, gate, gate_rows, scale, post, pre)()
+
+
+@dataclass
+class KvCache:
+    """The paged cache in 8 bits: k, v uint8 [n_blocks, n_heads, block_tokens * head_dim], scales fp32 [n_blocks, n_heads]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    block_tokens: int
+    head_dim: int
+
+    @classmethod
+    def empty(cls, n_blocks: int, n_heads: int, block_tokens: int, head_dim: int, device) -> "KvCache":
+        codes = [torch.empty((n_blocks, n_heads, block_tokens * head_dim), dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.empty((n_blocks, n_heads), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(*codes, *scales, block_tokens, head_dim)
+
+    def c(self) -> _KvCache:
+        n_blocks, n_heads = self.k_scale.shape
+        c = _KvCache(None, None, None, None, n_blocks, self.block_tokens, n_heads, self.head_dim)
+        codes = n_blocks * n_heads * self.block_tokens * self.head_dim
+        c.k, c.v = _vector(self.k, codes, "k", torch.uint8), _vector(self.v, codes, "v", torch.uint8)
+        c.k_scale, c.v_scale = (_vector(t, n_blocks * n_heads, "scales") for t in (self.k_scale, self.v_scale))
+        return c
+
+
+def moqe_kv_codes_bytes(cache: KvCache) -> int:
+    c = cache.c()
+    return lib.moqe_kv_codes_bytes(C.byref(c))
+
+
+@dataclass
+class KvBatch:
+    """The sequences of a call: block_table int32 [S, width], kv_len int32 [S], T rows each or cu_rows int32 [S + 1] with at most T each."""
+    block_table: torch.Tensor
+    kv_len: torch.Tensor
+    S: int
+    T: int
+    M: int
+    cu_rows: Optional[torch.Tensor] = None
+
+    def c(self) -> _KvBatch:
+        width = self.block_table.shape[1]
+        return _KvBatch(_vector(self.block_table, self.S * width, "block_table", torch.int32), _vector(self.kv_len, self.S, "kv_len", torch.int32),
+                        _vector(self.cu_rows, self.S + 1, "cu_rows", torch.int32), self.S, self.T, self.M, width)
+
+
+@dataclass
+class Rope:
+    """Rotary positions: inv_freq float64 [rot_dim / 2] on the device (decoder.rope_frequencies makes it), head norms' gains fp32 [head_dim]."""
+    inv_freq: Optional[torch.Tensor]
+    rot_dim: int
+    interleaved: bool = False
+    mscale: float = 1.0
+    q_gain: Optional[torch.Tensor] = None
+    k_gain: Optional[torch.Tensor] = None
+    eps: float = 1e-6
+
+    def c(self, head_dim: int) -> _Rope:
+        return _Rope(_vector(self.inv_freq, self.rot_dim // 2, "inv_freq", torch.float64), _vector(self.q_gain, head_dim, "q_gain"),
+                     _vector(self.k_gain, head_dim, "k_gain"), self.eps, self.mscale, self.rot_dim, int(self.interleaved))
+
+
+@dataclass
+class Attention:
+    """Heads, score scale and what a row sees: cap 0 and window 0 are none; slopes fp32 [n_heads], prefix int32 [S]."""
+    n_heads: int
+    scale: float
+    cap: float = 0.0
+    window: int = 0
+    slopes: Optional[torch.Tensor] = None
+    prefix: Optional[torch.Tensor] = None
+
+    def c(self, S: int) -> _Attention:
+        return _Attention(_vector(self.slopes, self.n_heads, "slopes"), _vector(self.prefix, S, "prefix", torch.int32), self.scale, self.cap,
+                          self.n_heads, self.window)
+
+
+class KvAppendCall:
+    """moqe_kv_append with its arguments marshalled once.  qkv [M, (n_heads + 2 kv heads) * head_dim] fp32 or bf16, q_out bf16 [M, n_heads * head_dim]."""
+
+    def __init__(self, qkv: torch.Tensor, n_heads: int, rope: Rope, batch: KvBatch, cache: KvCache, q_out: torch.Tensor):
+        self._c = (rope.c(cache.head_dim), batch.c(), cache.c())
+        self._keep = (qkv, rope, batch, cache, q_out)
+        qp, qs = _rows(qkv, batch.M, (n_heads + 2 * cache.k_scale.shape[1]) * cache.head_dim, "qkv")
+        op, os_ = _rows(q_out, batch.M, n_heads * cache.head_dim, "q_out", torch.bfloat16)
+        self._args = (qp, _type_of(qkv, "qkv"), qs, n_heads, *(C.byref(x) for x in self._c), op, os_)
+
+    def __call__(self, stream: Optional[int] = None) -> None:
+        rc = lib.moqe_kv_append(*self._args, _stream() if stream is None else stream)
+        if rc != 0:
+            _check(rc)
+
+
+def moqe_kv_append(qkv: torch.Tensor, n_heads: int, rope: Rope, batch: KvBatch, cache: KvCache, q_out: torch.Tensor) -> None:
+    KvAppendCall(qkv, n_heads, rope, batch, cache, q_out)()
+
+
+def moqe_kv_attention_workspace_bytes(attn: Attention, batch: KvBatch, cache: KvCache) -> int:
+    a, b, c = attn.c(batch.S), batch.c(), cache.c()
+    return lib.moqe_kv_attention_workspace_bytes(C.byref(a), C.byref(b), C.byref(c))
+
+
+class KvAttentionCall:
+    """moqe_kv_attention with its arguments marshalled once and a workspace of its own.  q, out bf16 [M, n_heads * head_dim]."""
+
+    def __init__(self, q: torch.Tensor, attn: Attention, batch: KvBatch, cache: KvCache, out: torch.Tensor,
+                 workspace: Optional[torch.Tensor] = None):
+        self._c = (attn.c(batch.S), batch.c(), cache.c())
+        refs = tuple(C.byref(x) for x in self._c)
+        if workspace is None:
+            workspace = _workspace(lib.moqe_kv_attention_workspace_bytes(*refs), q.device)
+        self.workspace = workspace
+        self._keep = (q, attn, batch, cache, out)
+        qp, qs = _rows(q, batch.M, attn.n_heads * cache.head_dim, "q", torch.bfloat16)
+        op, os_ = _rows(out, batch.M, attn.n_heads * cache.head_dim, "out", torch.bfloat16)
+        self._args = (qp, qs, *refs, op, os_, _ptr(workspace), workspace.numel())
+
+    def __call__(self, stream: Optional[int] = None) -> None:
+        rc = lib.moqe_kv_attention(*self._args, _stream() if stream is None else stream)
+        if rc != 0:
+            _check(rc)
+
+
+def moqe_kv_attention(q: torch.Tensor, attn: Attention, batch: KvBatch, cache: KvCache, out: torch.Tensor,
+                      workspace: Optional[torch.Tensor] = None) -> None:
+    KvAttentionCall(q, attn, batch, cache, out, workspace)()

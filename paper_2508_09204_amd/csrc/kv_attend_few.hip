@@ -1,0 +1,387 @@
+// Attention over the 8-bit cache for few rows (decode steps, short continuations): bound by reading the cache once.
+#include "kv_device.h"
+
+namespace moqe {
+
+struct FewArgs {
+  const uint16_t* q; uint16_t* out;
+  long long q_stride, out_stride;
+  KvBatch b; KvCache c; KvScore sc;
+  int group, cols;              // query heads to a key head; columns (rows x group) of a sequence and key head at most
+  int target, min_steps;        // chunks wanted in all, steps of 32 tokens that a chunk has at least
+  float2* part_ml; float* part_o;     // [chunk][key head][column] maximum and sum, [..][head_dim] unnormalised rows; NULL: one chunk a sequence
+};
+
+// How the sequences' steps are cut into chunks: all chunks but a sequence's last have C steps.  Every wave works it out by itself.
+struct FewPlan {
+  int s, chunk, first, chunks, steps;      // sequence, chunk in it, number of its first chunk, its chunks, steps of a chunk
+};
+__device__ __forceinline__ KvSteps few_steps(const FewArgs& a, int s, KvSeq* q) {
+  *q = kv_seq(a.b, s, a.c.bt_log2);
+  return kv_steps(q->len, q->n > 0 ? q->len : 0, q->first(), a.sc.window, a.sc.prefix ? a.sc.prefix[s] : 0);
+}
+// The sequence that chunk number `w` falls into (by_chunk), or the chunks of sequence `w`.  False: there is no such chunk.
+__device__ __forceinline__ bool few_plan(const FewArgs& a, int w, bool by_chunk, FewPlan* p) {
+  const int lane = threadIdx.x & 63, S = a.b.S;
+  int total = 0;
+  for (int base = 0; base < S; base += 64) {
+    KvSeq q;
+    total += base + lane < S ? few_steps(a, base + lane, &q).count : 0;
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
+  p->steps = max(a.min_steps, (total + a.target - 1) / a.target);
+  int before = 0;
+  for (int base = 0; base < S; base += 64) {
+    KvSeq q;
+    const int s = base + lane;
+    const int n = s < S ? max(1, (few_steps(a, s, &q).count + p->steps - 1) / p->steps) : 0;
+    int upto = n;                                   // inclusive sum over the lanes
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    const bool here = by_chunk ? w < before + upto : s == w;
+    const unsigned long long hit = __ballot(here);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      p->s = base + l;
+      p->chunks = __shfl(n, l);
+      p->first = before + __shfl(upto, l) - p->chunks;
+      p->chunk = w - p->first;
+      return true;
+    }
+    before += __shfl(upto, 63);
+  }
+  return false;
+}
+
+// One work-group takes a chunk of a sequence's tokens for one key head; its four waves take every fourth step of 32 tokens.  A wave reads its step's codes straight
+// into matrix-core operands (16 bytes a lane, next step's loads ahead of this one's products), keeps its own running maximum and sum for the
+// NC * 16 columns (row i, query head g: column i * group + g), and the waves' results are joined in LDS.
+template <int DH, int NC>
+__global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
+  constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64, VL = DH / 32;
+  constexpr int PAD = DH + 4;
+  __shared__ float obuf[4][16][PAD];
+  __shared__ float2 ml[4][NC * 16];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, kq = lane >> 4;
+  const int h = blockIdx.x % a.c.heads, w = blockIdx.x / a.c.heads;
+  FewPlan pl;
+  if (a.part_o) {
+    if (!few_plan(a, w, true, &pl)) return;
+  } else {
+    pl = FewPlan{w, 0, w, 1, 1 << 30};
+  }
+  KvSeq q;
+  const KvSteps ks = few_steps(a, pl.s, &q);
+  const int rows = min(q.n, a.b.T), first_pos = q.first();
+  const int prefix = a.sc.prefix ? min(a.sc.prefix[pl.s], q.len) : 0;
+  const int j_end = min(ks.count, pl.chunk < 1 ? pl.steps : pl.steps * (pl.chunk + 1));
+  const float scale2 = a.sc.scale * KV_LOG2E;
+
+  kv_bf16x8 qf[NC][KS];
+  int pos[NC];
+  float slope[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int col = c * 16 + r, i = col / a.group, g = col - i * a.group;
+    const bool in = i < rows;
+    pos[c] = first_pos + i;
+    slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
+    const uint16_t* src = a.q + (q.row0 + i) * a.q_stride + static_cast<long long>(h * a.group + g) * DH + kq * 8;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (in) v = *reinterpret_cast<const uint4*>(src + k * 32);
+      qf[c][k] = __builtin_bit_cast(kv_bf16x8, v);
+    }
+  }
+
+  kv_f32x4 o[NC][DT];
+  float m[NC], l[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m[c] = -3e38f;
+    l[c] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[c][d] = kv_f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const long long block_bytes = static_cast<long long>(DH) << a.c.bt_log2;
+  const int* table = a.b.table + static_cast<long long>(pl.s) * a.b.width;
+  for (int j0 = pl.chunk * pl.steps + wave; j0 < j_end; j0 += 256) {        // 64 steps of this wave at a time: lane i looks up step j0 + 4 i
+    int id = -1;
+    float k_scale = 0.f, v_scale = 0.f;
+    const int mine = j0 + 4 * lane;
+    if (mine < j_end) {
+      id = table[ks.step(mine) * 32 >> a.c.bt_log2];
+      if (id < 0 || id >= a.c.n_blocks) id = -1;
+      if (id >= 0) {
+        k_scale = a.c.k_scale[static_cast<long long>(id) * a.c.heads + h];
+        v_scale = a.c.v_scale[static_cast<long long>(id) * a.c.heads + h];
+      }
+    }
+    const int n = min(64, (j_end - j0 + 3) / 4);
+    uint4 kn[2 * KL], vn[VL];
+    auto load = [&](int i) {
+      const int bid = __builtin_amdgcn_readlane(id, i);
+      if (bid >= 0) {
+        const int tok = ks.step(j0 + 4 * i) * 32 & ((1 << a.c.bt_log2) - 1);
+        const long long at = (static_cast<long long>(bid) * a.c.heads + h) * block_bytes + tok * DH + lane * 16;
+#pragma unroll
+        for (int x = 0; x < 2 * KL; ++x) kn[x] = *reinterpret_cast<const uint4*>(a.c.k + at + x * 1024);
+#pragma unroll
+        for (int x = 0; x < VL; ++x) vn[x] = *reinterpret_cast<const uint4*>(a.c.v + at + x * 1024);
+      }
+    };
+    load(0);
+    for (int i = 0; i < n; ++i) {
+      uint4 kc[2 * KL], vc[VL];
+#pragma unroll
+      for (int x = 0; x < 2 * KL; ++x) kc[x] = kn[x];
+#pragma unroll
+      for (int x = 0; x < VL; ++x) vc[x] = vn[x];
+      if (i + 1 < n) load(i + 1);
+      if (__builtin_amdgcn_readlane(id, i) < 0) continue;                     // an absent block: nothing is seen
+      const float sk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), i));
+      const float sv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), i));
+      const int t0 = ks.step(j0 + 4 * i) * 32;
+      const bool full = t0 + 31 < prefix || (t0 + 31 <= first_pos && (a.sc.window <= 0 || first_pos + rows - 1 - t0 < a.sc.window));
+
+      kv_f32x4 s[2][NC];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) s[t][c] = kv_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const uint4 u = kc[t * KL + k / 2];
+          const kv_bf16x8 kf = (k & 1) ? kv_operand(u.z, u.w, sk) : kv_operand(u.x, u.y, sk);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) s[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][k], s[t][c], 0, 0, 0);
+        }
+      }
+      // codes that are NaN must not reach rows that do not see them: 0 * NaN would
+      bool nan = false;
+      if (!full) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int x = 0; x < VL; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) any |= ((&vc[x].x)[y] & 0x7f7f7f7fu) + 0x01010101u;
+        nan = __ballot((any & 0x80808080u) != 0) != 0;
+      }
+      kv_bf16x8 pf[NC];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            float v = s[t][c][x];
+            const int tok = t0 + 16 * t + 4 * kq + x;
+            if (a.sc.cap > 0.f) v = kv_capped(v * a.sc.scale, a.sc.cap) * KV_LOG2E;
+            else v *= scale2;
+            if (a.sc.slopes) v -= slope[c] * fabsf(float(pos[c] - tok));
+            if (!full && !kv_sees(tok, pos[c], q.len, prefix, a.sc.window)) v = -INFINITY;
+            s[t][c][x] = v;
+            top = fmaxf(top, v);
+          }
+        if (__any(top > m[c] + 8.f)) {       // the running maximum follows only where weights would pass 2^8: the sums are rescaled seldom
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float mn = fmaxf(m[c], top), f = exp2f(m[c] - mn);
+          m[c] = mn;
+          l[c] *= f;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[c][d] *= f;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float e = __builtin_amdgcn_exp2f(s[t][c][x] - m[c]);
+            l[c] += e;
+            pf[c][4 * t + x] = static_cast<__bf16>(e);
+          }
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const uint4 u = vc[d / 2];
+        uint32_t lo = (d & 1) ? u.z : u.x, hi = (d & 1) ? u.w : u.y;
+        if (nan) {
+          // bytes of NaN: taken out of the product, counted over what a row sees
+          auto bad = [](uint32_t x) { return (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7; };
+          const uint32_t bl = bad(lo), bh = bad(hi);
+          const kv_bf16x8 ones = kv_operand(bl * 0x38u, bh * 0x38u, 1.f);
+          lo &= ~(bl * 0xffu);
+          hi &= ~(bh * 0xffu);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            kv_bf16x8 seen;
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              seen[x] = static_cast<__bf16>(kv_sees(t0 + x / 4 * 16 + 4 * kq + x % 4, pos[c], q.len, prefix, a.sc.window) ? 1.f : 0.f);
+            const kv_f32x4 cnt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, seen, kv_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[c][d][x] = cnt[x] > 0.f ? NAN : o[c][d][x];
+          }
+        }
+        const kv_bf16x8 vf = kv_operand(lo, hi, sv);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[c], o[c][d], 0, 0, 0);
+      }
+    }
+  }
+
+  // the waves' results: common maximum, then sums in the waves' order
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    l[c] += __shfl_xor(l[c], 16);
+    l[c] += __shfl_xor(l[c], 32);
+    if (kq == 0) ml[wave][c * 16 + r] = make_float2(m[c], l[c]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const float mt = fmaxf(fmaxf(ml[0][c * 16 + r].x, ml[1][c * 16 + r].x), fmaxf(ml[2][c * 16 + r].x, ml[3][c * 16 + r].x));
+    const float f = exp2f(m[c] - mt);
+    if (c > 0) __syncthreads();              // the columns before have been read
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<kv_f32x4*>(&obuf[wave][r][d * 16 + kq * 4]) = o[c][d] * f;
+    __syncthreads();
+    constexpr int V = DH / 16;               // values a thread gathers
+    const int oc = tid / 16, col = c * 16 + oc, d0 = tid % 16 * V, i = col / a.group, g = col - i * a.group;
+    if (i < rows) {
+      float2 x[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) x[v] = ml[v][col];
+      const float mm = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
+      float lt = 0.f;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) lt += x[v].y * exp2f(x[v].x - mm);
+      float y[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[e] = ((obuf[0][oc][d0 + e] + obuf[1][oc][d0 + e]) + obuf[2][oc][d0 + e]) + obuf[3][oc][d0 + e];
+      if (pl.chunks == 1) {
+        const float inv = lt == 0.f ? 0.f : 1.f / lt;
+        uint16_t* dst = a.out + (q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + d0;
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          const __bf16 u0 = static_cast<__bf16>(y[e] * inv), u1 = static_cast<__bf16>(y[e + 1] * inv);
+          *reinterpret_cast<uint32_t*>(dst + e) = uint32_t(__builtin_bit_cast(uint16_t, u0)) | uint32_t(__builtin_bit_cast(uint16_t, u1)) << 16;
+        }
+      } else {
+        const long long at = (static_cast<long long>(w) * a.c.heads + h) * a.cols + col;
+        if (d0 == 0) a.part_ml[at] = make_float2(mm, lt);
+#pragma unroll
+        for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(a.part_o + at * DH + d0 + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+      }
+    }
+  }
+}
+
+// Joins the chunks of a sequence: one wave for each column of a sequence and key head.
+template <int DH>
+__global__ __launch_bounds__(256) void k_kv_attend_join(FewArgs a, int col_tiles) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int h = blockIdx.x % a.c.heads, s = blockIdx.x / a.c.heads / col_tiles, col = blockIdx.x / a.c.heads % col_tiles * 4 + wave;
+  FewPlan pl;
+  if (!few_plan(a, s, false, &pl) || pl.chunks == 1) return;
+  const KvSeq q = kv_seq(a.b, s, a.c.bt_log2);
+  const int i = col / a.group, g = col - i * a.group;
+  if (i >= min(q.n, a.b.T)) return;
+  const long long step = static_cast<long long>(a.c.heads) * a.cols, at = pl.first * step + static_cast<long long>(h) * a.cols + col;
+  float m = -3e38f;
+  for (int c = lane; c < pl.chunks; c += 64) m = fmaxf(m, a.part_ml[at + c * step].x);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  float l = 0.f, o[DH / 64] = {};
+  for (int c0 = 0; c0 < pl.chunks; c0 += 64) {
+    float f = 0.f, lc = 0.f;
+    if (c0 + lane < pl.chunks) {
+      const float2 x = a.part_ml[at + (c0 + lane) * step];
+      f = exp2f(x.x - m);
+      lc = x.y * f;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) lc += __shfl_xor(lc, d);
+    l += lc;
+    const int n = min(64, pl.chunks - c0);
+#pragma unroll 4
+    for (int c = 0; c < n; ++c) {
+      const float fc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), c));
+      const float* p = a.part_o + (at + (c0 + c) * step) * DH + lane * (DH / 64);
+#pragma unroll
+      for (int e = 0; e < DH / 64; ++e) o[e] += fc * p[e];
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* dst = a.out + (q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + lane * (DH / 64);
+#pragma unroll
+  for (int e = 0; e < DH / 64; ++e) dst[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(o[e] * inv));
+}
+
+namespace {
+constexpr int FEW_TARGET_WGS = 1024, FEW_MIN_STEPS = 8;
+long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c) {          // chunks at most; 0: one a sequence
+  const long long most = static_cast<long long>(b.table_width) * c.block_tokens / 32;
+  if (most <= FEW_MIN_STEPS) return 0;
+  const int target = FEW_TARGET_WGS / c.n_heads > 0 ? FEW_TARGET_WGS / c.n_heads : 1;
+  return target + static_cast<long long>(b.S);
+}
+}  // namespace
+
+size_t kv_attend_few_ws_bytes(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c) {
+  const size_t rows = size_t(few_chunks(b, c)) * c.n_heads * (size_t(b.T) * (at.n_heads / c.n_heads));
+  return align256(rows * 8) + align256(rows * c.head_dim * 4);
+}
+
+int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c,
+                             void* out, long long out_stride, void* ws, hipStream_t st) {
+  FewArgs a{};
+  a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
+  a.b = kv_batch_args(b);
+  a.c = kv_cache_args(c);
+  a.sc = KvScore{at.slopes, at.prefix, at.scale, at.cap, at.window};
+  a.group = at.n_heads / c.n_heads;
+  a.cols = b.T * a.group;
+  a.target = FEW_TARGET_WGS / c.n_heads > 0 ? FEW_TARGET_WGS / c.n_heads : 1;
+  a.min_steps = FEW_MIN_STEPS;
+  const long long chunks = few_chunks(b, c);
+  if (chunks) {
+    const size_t rows = size_t(chunks) * c.n_heads * a.cols;
+    a.part_ml = static_cast<float2*>(ws);
+    a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(rows * 8));
+  }
+  const long long wgs = (chunks ? chunks : b.S) * c.n_heads;
+  if (wgs >= (1ll << 31)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld work-groups", wgs);
+  ProfileScope ps(MOQE_PK_OTHER, st);
+  const dim3 grid(static_cast<unsigned>(wgs)), block(256);
+  const int nc = a.cols <= 16 ? 1 : a.cols <= 32 ? 2 : 4;
+  if (c.head_dim == 64) {
+    if (nc == 1) hipLaunchKernelGGL((k_kv_attend_few<64, 1>), grid, block, 0, st, a);
+    else if (nc == 2) hipLaunchKernelGGL((k_kv_attend_few<64, 2>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv_attend_few<64, 4>), grid, block, 0, st, a);
+  } else if (c.head_dim == 128) {
+    if (nc == 1) hipLaunchKernelGGL((k_kv_attend_few<128, 1>), grid, block, 0, st, a);
+    else if (nc == 2) hipLaunchKernelGGL((k_kv_attend_few<128, 2>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv_attend_few<128, 4>), grid, block, 0, st, a);
+  } else {
+    if (nc == 1) hipLaunchKernelGGL((k_kv_attend_few<256, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv_attend_few<256, 2>), grid, block, 0, st, a);
+  }
+  if (chunks) {
+    const int tiles = (a.cols + 3) / 4;
+    const dim3 jgrid(static_cast<unsigned>(static_cast<long long>(b.S) * c.n_heads * tiles));
+    if (c.head_dim == 64) hipLaunchKernelGGL((k_kv_attend_join<64>), jgrid, block, 0, st, a, tiles);
+    else if (c.head_dim == 128) hipLaunchKernelGGL((k_kv_attend_join<128>), jgrid, block, 0, st, a, tiles);
+    else hipLaunchKernelGGL((k_kv_attend_join<256>), jgrid, block, 0, st, a, tiles);
+  }
+  return check_launch("kv_attention");
+}
+
+}  // namespace moqe

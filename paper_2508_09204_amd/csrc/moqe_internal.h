@@ -198,7 +198,7 @@ int32_t check_launch(const char* what);
 // Kernels that need more than 64 KiB of dynamic LDS must ask for it once per kernel: `slot` is a
 // process-wide id of the kernel (LdsKernel); the request is made by the first caller only, under a
 // lock, and every caller gets its outcome.
-enum LdsKernel : int { LDSK_STREAM0 = 0, LDSK_ROUTER_TAIL = 12, LDSK_CV_IMAGE = 14, LDSK_ROUTE_ONE = 15, LDSK_COUNT = 16 };
+enum LdsKernel : int { LDSK_STREAM0 = 0, LDSK_ROUTER_TAIL = 12, LDSK_CV_IMAGE = 14, LDSK_ROUTE_ONE = 15, LDSK_ATTEND_ROWS = 16, LDSK_COUNT = 17 };
 int32_t ensure_dynamic_lds(int slot, const void* kernel, int bytes, const char* what);
 
 int32_t launch_route(const void* x, int S, int T, const moqe_router& r, int32_t* idx, float* logits,
@@ -243,5 +243,15 @@ int32_t launch_qgemm_few(const GemmArgs& ga, bool gateup, hipStream_t st);      
 int32_t launch_qgemm_tile(const GemmArgs& ga, bool gateup, bool equal, hipStream_t st);   // equal: S / K samples in every bucket
 int32_t launch_act_quant(const void* x_bf16, int kdim, int T, const int32_t* offsets, const int32_t* perm,
                          int expert, int max_rows, int8_t* out, float* scales, hipStream_t st);
+
+// Around the products of a decoder layer (residual_norm.hip, kv_append.hip, kv_attend_few.hip, kv_attend_rows.hip): arguments already checked.
+int32_t launch_residual_norm(const moqe_residual_step& s, hipStream_t st);
+int32_t launch_kv_append(const void* qkv, bool bf16, long long qkv_stride, int heads, const moqe_rope& r, const moqe_kv_batch& b,
+                         const moqe_kv_cache& c, void* q_out, long long q_stride, hipStream_t st);
+int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c,
+                             void* out, long long out_stride, void* ws, hipStream_t st);
+size_t  kv_attend_few_ws_bytes(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c);
+int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c,
+                              void* out, long long out_stride, hipStream_t st);
 
 }  // namespace moqe
