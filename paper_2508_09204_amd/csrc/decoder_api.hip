@@ -129,7 +129,7 @@ int32_t moqe_kv_append(const void* qkv, int32_t qkv_type, int64_t qkv_stride, in
 size_t moqe_kv_attention_workspace_bytes(const moqe_attention* at, const moqe_kv_batch* b, const moqe_kv_cache* c) {
   if (check_attention(at, b, c, "moqe_kv_attention_workspace_bytes")) return 0;
   if (b->S == 0 || b->M == 0) return 0;
-  return kv_few_rows(b->T, at->n_heads / c->n_heads, c->head_dim) ? kv_attend_few_ws_bytes(*at, *b, *c) : 0;
+  return kv_few_rows(b->T, at->n_heads / c->n_heads, c->head_dim) ? kv_attend_few_ws_bytes(*at, *b, *c) : kv_attend_rows_ws_bytes(*at, *b, *c);
 }
 
 int32_t moqe_kv_attention(const void* q, int64_t q_stride, const moqe_attention* at, const moqe_kv_batch* b, const moqe_kv_cache* c, void* out,
@@ -148,7 +148,7 @@ int32_t moqe_kv_attention(const void* q, int64_t q_stride, const moqe_attention*
   if (dry_run()) return MOQE_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (kv_few_rows(b->T, at->n_heads / c->n_heads, c->head_dim)) return launch_kv_attend_few(q, q_stride, *at, *b, *c, out, out_stride, workspace, st);
-  return launch_kv_attend_rows(q, q_stride, *at, *b, *c, out, out_stride, st);
+  return launch_kv_attend_rows(q, q_stride, *at, *b, *c, out, out_stride, workspace, st);
 }
 
 }  // extern "C"

@@ -58,8 +58,8 @@ inline bool nlp_whole_rows(long long rows, long long d, long long dm, long long 
   return rows > 4096 || dm == 128 || d_ff <= (dm == 256 ? 20480 : 7680);
 }
 
-// Attention over the cache: the kernel for few rows (tokens divided over work-groups, up to 64 columns of rows x query heads of a key head in registers; 32 where
+// Attention over the cache: the kernel for few rows (tokens divided over work-groups, up to 64 columns of rows x query heads of a key head in registers; 16 where
 // the head is 256 wide), or the one for many?
-inline bool kv_few_rows(long long T, int group, int head_dim) { return T * group <= (head_dim == 256 ? 32 : 64); }
+inline bool kv_few_rows(long long T, int group, int head_dim) { return T * group <= (head_dim == 256 ? 16 : 64); }
 
 }  // namespace moqe

@@ -99,11 +99,6 @@ __device__ __forceinline__ uint32_t rescaled4(uint32_t w, float by) {
                       __builtin_amdgcn_cvt_f32_fp8(w, 3)};
   return codes4(x, by);
 }
-__device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
-  const __bf16 l = static_cast<__bf16>(lo), h = static_cast<__bf16>(hi);
-  return uint32_t(__builtin_bit_cast(uint16_t, l)) | uint32_t(__builtin_bit_cast(uint16_t, h)) << 16;
-}
-
 // Keys (VALUES false) or values of one block and head: the new tokens lo .. hi of block `blk` of the sequence, which lies in cache block `id`.
 template <int DH, bool BF16, bool VALUES>
 __device__ __forceinline__ void append_block(const AppendArgs& a, const KvSeq& q, int head, int blk, int id, int lo, int hi, uint8_t* lds, uint32_t* wave_max) {
@@ -283,7 +278,7 @@ __global__ __launch_bounds__(1024) void k_kv_append(AppendArgs a) {
       if (turned) turn(a.inter, cs, sn, x);
       uint32_t o[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = pair_bf16(x[2 * j], x[2 * j + 1]);
+      for (int j = 0; j < 8; ++j) o[j] = kv_pair(x[2 * j], x[2 * j + 1]);
       *reinterpret_cast<uint4*>(a.q + to + h * DH + da) = make_uint4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<uint4*>(a.q + to + h * DH + db) = make_uint4(o[4], o[5], o[6], o[7]);
     }

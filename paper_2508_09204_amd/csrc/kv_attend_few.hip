@@ -9,7 +9,7 @@ struct FewArgs {
   KvBatch b; KvCache c; KvScore sc;
   int group, cols;              // query heads to a key head; columns (rows x group) of a sequence and key head at most
   int target, min_steps;        // chunks wanted in all, steps of 32 tokens that a chunk has at least
-  float2* part_ml; float* part_o;     // [chunk][key head][column] maximum and sum, [..][head_dim] unnormalised rows; NULL: one chunk a sequence
+  KvParts parts;                // [chunk][key head][column]; NULL: one chunk a sequence
 };
 
 // How the sequences' steps are cut into chunks: all chunks but a sequence's last have C steps.  Every wave works it out by itself.
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, kq = lane >> 4;
   const int h = blockIdx.x % a.c.heads, w = blockIdx.x / a.c.heads;
   FewPlan pl;
-  if (a.part_o) {
+  if (a.parts.o) {
     if (!few_plan(a, w, true, &pl)) return;
   } else {
     pl = FewPlan{w, 0, w, 1, 1 << 30};
@@ -77,11 +77,13 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
   KvSeq q;
   const KvSteps ks = few_steps(a, pl.s, &q);
   const int rows = min(q.n, a.b.T), first_pos = q.first();
-  const int prefix = a.sc.prefix ? min(a.sc.prefix[pl.s], q.len) : 0;
+  if (rows == 0) return;
+  const int pre = a.sc.prefix ? min(a.sc.prefix[pl.s], q.len) : 0, window = a.sc.window, last_pos = first_pos + rows - 1;
   const int j_end = min(ks.count, pl.chunk < 1 ? pl.steps : pl.steps * (pl.chunk + 1));
   const float scale2 = a.sc.scale * KV_LOG2E;
 
   kv_bf16x8 qf[NC][KS];
+  KvSight sight[NC];
   int pos[NC];
   float slope[NC];
 #pragma unroll
@@ -89,6 +91,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
     const int col = c * 16 + r, i = col / a.group, g = col - i * a.group;
     const bool in = i < rows;
     pos[c] = first_pos + i;
+    sight[c] = kv_sight(pos[c], q.len, window);
     slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
     const uint16_t* src = a.q + (q.row0 + i) * a.q_stride + static_cast<long long>(h * a.group + g) * DH + kq * 8;
 #pragma unroll
@@ -109,6 +112,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
     for (int d = 0; d < DT; ++d) o[c][d] = kv_f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  bool nan = false;
   const long long block_bytes = static_cast<long long>(DH) << a.c.bt_log2;
   const int* table = a.b.table + static_cast<long long>(pl.s) * a.b.width;
   for (int j0 = pl.chunk * pl.steps + wave; j0 < j_end; j0 += 256) {        // 64 steps of this wave at a time: lane i looks up step j0 + 4 i
@@ -148,7 +152,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
       const float sk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), i));
       const float sv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), i));
       const int t0 = ks.step(j0 + 4 * i) * 32;
-      const bool full = t0 + 31 < prefix || (t0 + 31 <= first_pos && (a.sc.window <= 0 || first_pos + rows - 1 - t0 < a.sc.window));
+      const bool full = kv_all_see(t0, first_pos, last_pos, pre, window);
 
       kv_f32x4 s[2][NC];
 #pragma unroll
@@ -163,15 +167,12 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
           for (int c = 0; c < NC; ++c) s[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][k], s[t][c], 0, 0, 0);
         }
       }
-      // codes that are NaN must not reach rows that do not see them: 0 * NaN would
-      bool nan = false;
-      if (!full) {
-        uint32_t any = 0;
+      if (!full) {                       // values that are NaN must not reach rows that do not see them: 0 * NaN would
 #pragma unroll
-        for (int x = 0; x < VL; ++x)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) any |= ((&vc[x].x)[y] & 0x7f7f7f7fu) + 0x01010101u;
-        nan = __ballot((any & 0x80808080u) != 0) != 0;
+        for (int x = 0; x < VL; ++x) {
+          nan |= __ballot(kv_nan_bytes(vc[x]) != 0) != 0;
+          vc[x] = kv_without_nan(vc[x]);
+        }
       }
       kv_bf16x8 pf[NC];
 #pragma unroll
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
             if (a.sc.cap > 0.f) v = kv_capped(v * a.sc.scale, a.sc.cap) * KV_LOG2E;
             else v *= scale2;
             if (a.sc.slopes) v -= slope[c] * fabsf(float(pos[c] - tok));
-            if (!full && !kv_sees(tok, pos[c], q.len, prefix, a.sc.window)) v = -INFINITY;
+            if (!full && !sight[c].sees(tok, pre)) v = -INFINITY;
             s[t][c][x] = v;
             top = fmaxf(top, v);
           }
@@ -211,26 +212,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const uint4 u = vc[d / 2];
-        uint32_t lo = (d & 1) ? u.z : u.x, hi = (d & 1) ? u.w : u.y;
-        if (nan) {
-          // bytes of NaN: taken out of the product, counted over what a row sees
-          auto bad = [](uint32_t x) { return (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7; };
-          const uint32_t bl = bad(lo), bh = bad(hi);
-          const kv_bf16x8 ones = kv_operand(bl * 0x38u, bh * 0x38u, 1.f);
-          lo &= ~(bl * 0xffu);
-          hi &= ~(bh * 0xffu);
-#pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            kv_bf16x8 seen;
-#pragma unroll
-            for (int x = 0; x < 8; ++x)
-              seen[x] = static_cast<__bf16>(kv_sees(t0 + x / 4 * 16 + 4 * kq + x % 4, pos[c], q.len, prefix, a.sc.window) ? 1.f : 0.f);
-            const kv_f32x4 cnt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, seen, kv_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) o[c][d][x] = cnt[x] > 0.f ? NAN : o[c][d][x];
-          }
-        }
-        const kv_bf16x8 vf = kv_operand(lo, hi, sv);
+        const kv_bf16x8 vf = (d & 1) ? kv_operand(u.z, u.w, sv) : kv_operand(u.x, u.y, sv);
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[c], o[c][d], 0, 0, 0);
       }
@@ -270,51 +252,88 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
         uint16_t* dst = a.out + (q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + d0;
 #pragma unroll
-        for (int e = 0; e < V; e += 2) {
-          const __bf16 u0 = static_cast<__bf16>(y[e] * inv), u1 = static_cast<__bf16>(y[e + 1] * inv);
-          *reinterpret_cast<uint32_t*>(dst + e) = uint32_t(__builtin_bit_cast(uint16_t, u0)) | uint32_t(__builtin_bit_cast(uint16_t, u1)) << 16;
-        }
+        for (int e = 0; e < V; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = kv_pair(y[e] * inv, y[e + 1] * inv);
       } else {
         const long long at = (static_cast<long long>(w) * a.c.heads + h) * a.cols + col;
-        if (d0 == 0) a.part_ml[at] = make_float2(mm, lt);
+        if (d0 == 0) a.parts.ml[at] = make_float2(mm, lt);
 #pragma unroll
-        for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(a.part_o + at * DH + d0 + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+        for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(a.parts.o + at * DH + d0 + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+      }
+    }
+  }
+
+  // NaN among values that some rows do not see was left out of the products: the dims of those who see it become NaN
+  if (__syncthreads_or(nan) == 0 || !nan) return;
+  for (int j = pl.chunk * pl.steps + wave; j < j_end; j += 4) {
+    const int t0 = ks.step(j) * 32, id = table[t0 >> a.c.bt_log2];
+    if (id < 0 || id >= a.c.n_blocks || kv_all_see(t0, first_pos, last_pos, pre, window)) continue;
+    const uint8_t* v = a.c.v + (static_cast<long long>(id) * a.c.heads + h) * block_bytes + (t0 & ((1 << a.c.bt_log2) - 1)) * DH + lane * 16;
+#pragma unroll 1
+    for (int d = 0; d < DT; ++d) {
+      const uint2 w2 = *reinterpret_cast<const uint2*>(v + d / 2 * 1024 + d % 2 * 8);
+      const kv_bf16x8 bad = kv_operand(kv_nan_bytes(w2.x) * 0x38u, kv_nan_bytes(w2.y) * 0x38u, 1.f);    // 1 where the code is NaN
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        kv_bf16x8 sees;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) sees[y] = static_cast<__bf16>(sight[c].sees(t0 + y / 4 * 16 + 4 * kq + y % 4, pre) ? 1.f : 0.f);
+        const kv_f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, sees, kv_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        const int col = c * 16 + r, i = col / a.group, g = col - i * a.group;
+        if (i >= rows) continue;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if (n[y] > 0.f) {
+            const int dim = d * 16 + kq * 4 + y;
+            if (pl.chunks == 1) a.out[(q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + dim] = 0x7fc0;
+            else a.parts.o[((static_cast<long long>(w) * a.c.heads + h) * a.cols + col) * DH + dim] = NAN;
+          }
       }
     }
   }
 }
 
-// Joins the chunks of a sequence: one wave for each column of a sequence and key head.
+// Joins parts: one wave for each column of a sequence and key head.  splits 0: the chunks of few_plan; else so many parts of every column.
+struct JoinArgs {
+  FewArgs few;
+  int col_tiles, splits;
+};
 template <int DH>
-__global__ __launch_bounds__(256) void k_kv_attend_join(FewArgs a, int col_tiles) {
+__global__ __launch_bounds__(256) void k_kv_attend_join(JoinArgs ja) {
+  const FewArgs& a = ja.few;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int h = blockIdx.x % a.c.heads, s = blockIdx.x / a.c.heads / col_tiles, col = blockIdx.x / a.c.heads % col_tiles * 4 + wave;
-  FewPlan pl;
-  if (!few_plan(a, s, false, &pl) || pl.chunks == 1) return;
+  const int h = blockIdx.x % a.c.heads, s = blockIdx.x / a.c.heads / ja.col_tiles, col = blockIdx.x / a.c.heads % ja.col_tiles * 4 + wave;
+  int chunks = ja.splits;
+  long long step = static_cast<long long>(a.b.S) * a.c.heads * a.cols, at = (static_cast<long long>(s) * a.c.heads + h) * a.cols + col;
+  if (ja.splits == 0) {
+    FewPlan pl;
+    if (!few_plan(a, s, false, &pl) || pl.chunks == 1) return;
+    chunks = pl.chunks;
+    step = static_cast<long long>(a.c.heads) * a.cols;
+    at = pl.first * step + static_cast<long long>(h) * a.cols + col;
+  }
   const KvSeq q = kv_seq(a.b, s, a.c.bt_log2);
   const int i = col / a.group, g = col - i * a.group;
   if (i >= min(q.n, a.b.T)) return;
-  const long long step = static_cast<long long>(a.c.heads) * a.cols, at = pl.first * step + static_cast<long long>(h) * a.cols + col;
   float m = -3e38f;
-  for (int c = lane; c < pl.chunks; c += 64) m = fmaxf(m, a.part_ml[at + c * step].x);
+  for (int c = lane; c < chunks; c += 64) m = fmaxf(m, a.parts.ml[at + c * step].x);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
   float l = 0.f, o[DH / 64] = {};
-  for (int c0 = 0; c0 < pl.chunks; c0 += 64) {
+  for (int c0 = 0; c0 < chunks; c0 += 64) {
     float f = 0.f, lc = 0.f;
-    if (c0 + lane < pl.chunks) {
-      const float2 x = a.part_ml[at + (c0 + lane) * step];
+    if (c0 + lane < chunks) {
+      const float2 x = a.parts.ml[at + (c0 + lane) * step];
       f = exp2f(x.x - m);
       lc = x.y * f;
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) lc += __shfl_xor(lc, d);
     l += lc;
-    const int n = min(64, pl.chunks - c0);
+    const int n = min(64, chunks - c0);
 #pragma unroll 4
     for (int c = 0; c < n; ++c) {
       const float fc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), c));
-      const float* p = a.part_o + (at + (c0 + c) * step) * DH + lane * (DH / 64);
+      const float* p = a.parts.o + (at + (c0 + c) * step) * DH + lane * (DH / 64);
 #pragma unroll
       for (int e = 0; e < DH / 64; ++e) o[e] += fc * p[e];
     }
@@ -333,7 +352,21 @@ long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c) {          
   const int target = FEW_TARGET_WGS / c.n_heads > 0 ? FEW_TARGET_WGS / c.n_heads : 1;
   return target + static_cast<long long>(b.S);
 }
+void launch_join(const FewArgs& a, int dh, int splits, hipStream_t st) {
+  JoinArgs ja{a, (a.cols + 3) / 4, splits};
+  const dim3 grid(static_cast<unsigned>(static_cast<long long>(a.b.S) * a.c.heads * ja.col_tiles)), block(256);
+  if (dh == 64) hipLaunchKernelGGL((k_kv_attend_join<64>), grid, block, 0, st, ja);
+  else if (dh == 128) hipLaunchKernelGGL((k_kv_attend_join<128>), grid, block, 0, st, ja);
+  else hipLaunchKernelGGL((k_kv_attend_join<256>), grid, block, 0, st, ja);
+}
 }  // namespace
+
+void launch_kv_join(const KvParts& parts, const KvBatch& b, const KvCache& c, int dh, int group, int cols, int splits, uint16_t* out, long long out_stride,
+                    hipStream_t st) {
+  FewArgs a{};
+  a.out = out; a.out_stride = out_stride; a.b = b; a.c = c; a.group = group; a.cols = cols; a.parts = parts;
+  launch_join(a, dh, splits, st);
+}
 
 size_t kv_attend_few_ws_bytes(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c) {
   const size_t rows = size_t(few_chunks(b, c)) * c.n_heads * (size_t(b.T) * (at.n_heads / c.n_heads));
@@ -352,11 +385,7 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   a.target = FEW_TARGET_WGS / c.n_heads > 0 ? FEW_TARGET_WGS / c.n_heads : 1;
   a.min_steps = FEW_MIN_STEPS;
   const long long chunks = few_chunks(b, c);
-  if (chunks) {
-    const size_t rows = size_t(chunks) * c.n_heads * a.cols;
-    a.part_ml = static_cast<float2*>(ws);
-    a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(rows * 8));
-  }
+  if (chunks) a.parts = kv_parts(ws, size_t(chunks) * c.n_heads * a.cols);
   const long long wgs = (chunks ? chunks : b.S) * c.n_heads;
   if (wgs >= (1ll << 31)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld work-groups", wgs);
   ProfileScope ps(MOQE_PK_OTHER, st);
@@ -371,16 +400,9 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
     else if (nc == 2) hipLaunchKernelGGL((k_kv_attend_few<128, 2>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((k_kv_attend_few<128, 4>), grid, block, 0, st, a);
   } else {
-    if (nc == 1) hipLaunchKernelGGL((k_kv_attend_few<256, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_kv_attend_few<256, 2>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((k_kv_attend_few<256, 1>), grid, block, 0, st, a);
   }
-  if (chunks) {
-    const int tiles = (a.cols + 3) / 4;
-    const dim3 jgrid(static_cast<unsigned>(static_cast<long long>(b.S) * c.n_heads * tiles));
-    if (c.head_dim == 64) hipLaunchKernelGGL((k_kv_attend_join<64>), jgrid, block, 0, st, a, tiles);
-    else if (c.head_dim == 128) hipLaunchKernelGGL((k_kv_attend_join<128>), jgrid, block, 0, st, a, tiles);
-    else hipLaunchKernelGGL((k_kv_attend_join<256>), jgrid, block, 0, st, a, tiles);
-  }
+  if (chunks) launch_join(a, c.head_dim, 0, st);
   return check_launch("kv_attention");
 }
 

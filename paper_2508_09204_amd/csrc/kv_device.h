@@ -56,6 +56,11 @@ __device__ __forceinline__ kv_bf16x8 kv_operand(uint32_t lo, uint32_t hi, float 
   return u.v;
 }
 
+__device__ __forceinline__ uint32_t kv_pair(float lo, float hi) {          // two bf16, to nearest even
+  const __bf16 l = static_cast<__bf16>(lo), h = static_cast<__bf16>(hi);
+  return uint32_t(__builtin_bit_cast(uint16_t, l)) | uint32_t(__builtin_bit_cast(uint16_t, h)) << 16;
+}
+
 // What turns q . k into the score's base-2 exponent, and who sees what.
 struct KvScore {
   const float* slopes; const int32_t* prefix;
@@ -69,8 +74,40 @@ __device__ __forceinline__ float kv_capped(float a, float cap) {
   return cap - 2.f * cap / (1.f + exp2f(a * (2.f * KV_LOG2E) / cap));
 }
 
-__device__ __forceinline__ bool kv_sees(int t, int p, int len, int prefix, int window) {
-  return t < len && (t < prefix || (t <= p && (window <= 0 || p - t < window)));
+// What a row at position p sees: tokens below `pre` and `span` tokens from `lo` on.
+struct KvSight {
+  int lo;
+  uint32_t span;
+  __device__ __forceinline__ bool sees(int t, int pre) const { return uint32_t(t - lo) < span || t < pre; }
+};
+__device__ __forceinline__ KvSight kv_sight(int p, int len, int window) {
+  const int hi = min(len, p + 1), lo = window > 0 ? max(p - window + 1, 0) : 0;
+  return KvSight{lo, uint32_t(max(hi - lo, 0))};
 }
+// Whether rows at positions p0 .. p1 all see, or may see any of, the 32 tokens from t0 on.
+__device__ __forceinline__ bool kv_all_see(int t0, int p0, int p1, int pre, int window) {
+  return t0 + 31 < pre || (t0 + 31 <= p0 && (window <= 0 || p1 - t0 < window));
+}
+__device__ __forceinline__ bool kv_some_see(int t0, int p0, int p1, int pre, int window) {
+  return t0 < pre || (t0 <= p1 && (window <= 0 || p0 - (t0 + 31) < window));
+}
+
+// Bytes of NaN among four codes, as 1 in their lowest bits.
+__device__ __forceinline__ uint32_t kv_nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7; }
+__device__ __forceinline__ uint32_t kv_nan_bytes(uint4 w) { return kv_nan_bytes(w.x) | kv_nan_bytes(w.y) | kv_nan_bytes(w.z) | kv_nan_bytes(w.w); }
+__device__ __forceinline__ uint4 kv_without_nan(uint4 w) {
+  return make_uint4(w.x & ~(kv_nan_bytes(w.x) * 0xffu), w.y & ~(kv_nan_bytes(w.y) * 0xffu), w.z & ~(kv_nan_bytes(w.z) * 0xffu),
+                    w.w & ~(kv_nan_bytes(w.w) * 0xffu));
+}
+
+// Joins parts of rows: kv_attend_few.hip.
+struct KvParts {
+  float2* ml; float* o;         // [part][..][column] maximum and sum, [..][head_dim] rows that are not divided by the sum; NULL: there is one part
+};
+inline KvParts kv_parts(void* ws, size_t rows) {
+  return KvParts{static_cast<float2*>(ws), reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(rows * 8))};
+}
+void launch_kv_join(const KvParts& parts, const KvBatch& b, const KvCache& c, int dh, int group, int cols, int splits, uint16_t* out, long long out_stride,
+                    hipStream_t st);
 
 }  // namespace moqe
