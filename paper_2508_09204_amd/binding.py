@@ -191,6 +191,8 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream() -> Optional[int]:
+    if torch.cuda.is_initialized():
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())      # 0.1 us, torch.cuda.current_stream() 3 us
     return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
 
 

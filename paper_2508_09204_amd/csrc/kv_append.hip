@@ -23,16 +23,18 @@ __device__ __forceinline__ void slot_dims(const AppendArgs& a, int slot, int* da
   *db = halves ? slot * 8 + a.rot / 2 : slot * 16 + 8;
 }
 
-// cos and sin of the slot's eight angles at position p: reduced to a fraction of a turn in 64 bits, where 32 would lose 2^-24 of p * inv_freq.
+// cos and sin of the slot's eight angles at position p.  They are reduced to a fraction of a turn in 64 bits, where 32 would lose 2^-24 of p * inv_freq; what the
+// fraction loses when it is rounded to 32 comes back to first order: without that, keys that lie between two codes took the wrong one more than twice as often.
 __device__ __forceinline__ void slot_angles(const AppendArgs& a, int slot, int p, float* cs, float* sn) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     double turns = double(p) * (a.inv_freq[slot * 8 + i] * 0.15915494309189535);
     turns -= rint(turns);
+    const float hi = float(turns), lo = float(turns - double(hi)) * 6.2831853f;
     float s, c;
-    sincospif(2.f * float(turns), &s, &c);
-    cs[i] = a.mscale * c;
-    sn[i] = a.mscale * s;
+    sincospif(2.f * hi, &s, &c);
+    cs[i] = a.mscale * fmaf(-lo, s, c);
+    sn[i] = a.mscale * fmaf(lo, c, s);
   }
 }
 

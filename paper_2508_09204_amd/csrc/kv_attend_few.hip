@@ -57,15 +57,16 @@ __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, bool by_chunk,
   return false;
 }
 
-// One work-group takes a chunk of a sequence's tokens for one key head; its four waves take every fourth step of 32 tokens.  A wave reads its step's codes straight
-// into matrix-core operands (16 bytes a lane, next step's loads ahead of this one's products), keeps its own running maximum and sum for the
-// NC * 16 columns (row i, query head g: column i * group + g), and the waves' results are joined in LDS.
-template <int DH, int NC>
-__global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
+// One work-group takes a chunk of a sequence's tokens for one key head; each of its W waves takes every W-th step of 32 tokens.  A wave reads its step's codes
+// straight into matrix-core operands, 16 bytes a lane, and asks for the next step's keys as soon as this one's have gone through their product, for its values
+// likewise.  It keeps its own running maximum and sum for the NC * 16 columns (row i, query head g: column i * group + g); the waves' results are joined in LDS.
+// EXTRA: scores are capped, biased, or their scale is not positive.
+template <int DH, int NC, int W, bool EXTRA>
+__global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_attend_few(FewArgs a) {
   constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64, VL = DH / 32;
   constexpr int PAD = DH + 4;
   __shared__ float obuf[4][16][PAD];
-  __shared__ float2 ml[4][NC * 16];
+  __shared__ float2 ml[W][NC * 16];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, kq = lane >> 4;
   const int h = blockIdx.x % a.c.heads, w = blockIdx.x / a.c.heads;
   FewPlan pl;
@@ -79,8 +80,42 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
   const int rows = min(q.n, a.b.T), first_pos = q.first();
   if (rows == 0) return;
   const int pre = a.sc.prefix ? min(a.sc.prefix[pl.s], q.len) : 0, window = a.sc.window, last_pos = first_pos + rows - 1;
-  const int j_end = min(ks.count, pl.chunk < 1 ? pl.steps : pl.steps * (pl.chunk + 1));
+  const int j_begin = pl.chunk * pl.steps + wave, j_end = min(ks.count, pl.chunk < 1 ? pl.steps : pl.steps * (pl.chunk + 1));
   const float scale2 = a.sc.scale * KV_LOG2E;
+
+  // 64 steps of this wave at a time: lane i looks up step j0 + W i: block (-1: absent, nothing is seen) and scales
+  const long long block_bytes = static_cast<long long>(DH) << a.c.bt_log2;
+  const int* table = a.b.table + static_cast<long long>(pl.s) * a.b.width;
+  int id = -1;
+  float k_scale = 0.f, v_scale = 0.f;
+  auto look_up = [&](int j0) {
+    id = -1;
+    const int mine = j0 + W * lane;
+    if (mine < j_end) {
+      id = table[ks.step(mine) * 32 >> a.c.bt_log2];
+      if (id < 0 || id >= a.c.n_blocks) id = -1;
+      if (id >= 0) {
+        k_scale = a.c.k_scale[static_cast<long long>(id) * a.c.heads + h];
+        v_scale = a.c.v_scale[static_cast<long long>(id) * a.c.heads + h];
+      }
+    }
+  };
+  uint4 kc[2 * KL], vc[VL];
+  auto place = [&](int j, int bid) {
+    const int tok = ks.step(j) * 32 & ((1 << a.c.bt_log2) - 1);
+    return (static_cast<long long>(bid) * a.c.heads + h) * block_bytes + tok * DH + lane * 16;
+  };
+  auto load_keys = [&](int j, int bid) {
+    const uint8_t* p = a.c.k + place(j, bid);
+#pragma unroll
+    for (int x = 0; x < 2 * KL; ++x) kc[x] = *reinterpret_cast<const uint4*>(p + x * 1024);
+  };
+  auto load_values = [&](int j, int bid) {
+    const uint8_t* p = a.c.v + place(j, bid);
+#pragma unroll
+    for (int x = 0; x < VL; ++x) vc[x] = *reinterpret_cast<const uint4*>(p + x * 1024);
+  };
+  look_up(j_begin);
 
   kv_bf16x8 qf[NC][KS];
   KvSight sight[NC];
@@ -92,7 +127,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
     const bool in = i < rows;
     pos[c] = first_pos + i;
     sight[c] = kv_sight(pos[c], q.len, window);
-    slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
+    if (EXTRA) slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
     const uint16_t* src = a.q + (q.row0 + i) * a.q_stride + static_cast<long long>(h * a.group + g) * DH + kq * 8;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
@@ -113,113 +148,94 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
   }
 
   bool nan = false;
-  const long long block_bytes = static_cast<long long>(DH) << a.c.bt_log2;
-  const int* table = a.b.table + static_cast<long long>(pl.s) * a.b.width;
-  for (int j0 = pl.chunk * pl.steps + wave; j0 < j_end; j0 += 256) {        // 64 steps of this wave at a time: lane i looks up step j0 + 4 i
-    int id = -1;
-    float k_scale = 0.f, v_scale = 0.f;
-    const int mine = j0 + 4 * lane;
-    if (mine < j_end) {
-      id = table[ks.step(mine) * 32 >> a.c.bt_log2];
-      if (id < 0 || id >= a.c.n_blocks) id = -1;
-      if (id >= 0) {
-        k_scale = a.c.k_scale[static_cast<long long>(id) * a.c.heads + h];
-        v_scale = a.c.v_scale[static_cast<long long>(id) * a.c.heads + h];
+  {
+    const int bid = max(__builtin_amdgcn_readlane(id, 0), 0);
+    load_keys(j_begin, bid);
+    load_values(j_begin, bid);
+  }
+  int i = 0;                             // the step's place among those looked up
+  for (int j = j_begin; j < j_end; j += W) {
+    const int bid = __builtin_amdgcn_readlane(id, i);
+    const float sk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), i));
+    const float sv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), i));
+    // the next step's block; where there is none, any block does: nothing of it is seen
+    int next = max(bid, 0);
+    i = (i + 1) & 63;
+    if (j + W < j_end) {
+      if (i == 0) look_up(j + W);
+      next = max(__builtin_amdgcn_readlane(id, i), 0);
+    }
+    const int t0 = bid < 0 ? 1 << 30 : ks.step(j) * 32;
+    const bool full = kv_all_see(t0, first_pos, last_pos, pre, window);
+    kv_f32x4 s[2][NC];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) s[t][c] = kv_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const uint4 u = kc[t * KL + k / 2];
+        const kv_bf16x8 kf = (k & 1) ? kv_operand(u.z, u.w, sk) : kv_operand(u.x, u.y, sk);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) s[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][k], s[t][c], 0, 0, 0);
+        if (k % 2) __builtin_amdgcn_sched_barrier(0);       // else all operands are converted ahead of all products, and the registers do not hold them
       }
     }
-    const int n = min(64, (j_end - j0 + 3) / 4);
-    uint4 kn[2 * KL], vn[VL];
-    auto load = [&](int i) {
-      const int bid = __builtin_amdgcn_readlane(id, i);
-      if (bid >= 0) {
-        const int tok = ks.step(j0 + 4 * i) * 32 & ((1 << a.c.bt_log2) - 1);
-        const long long at = (static_cast<long long>(bid) * a.c.heads + h) * block_bytes + tok * DH + lane * 16;
+    load_keys(j + W, next);
+    kv_bf16x8 pf[NC];
 #pragma unroll
-        for (int x = 0; x < 2 * KL; ++x) kn[x] = *reinterpret_cast<const uint4*>(a.c.k + at + x * 1024);
+    for (int c = 0; c < NC; ++c) {
+      float top = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < VL; ++x) vn[x] = *reinterpret_cast<const uint4*>(a.c.v + at + x * 1024);
-      }
-    };
-    load(0);
-    for (int i = 0; i < n; ++i) {
-      uint4 kc[2 * KL], vc[VL];
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int x = 0; x < 2 * KL; ++x) kc[x] = kn[x];
-#pragma unroll
-      for (int x = 0; x < VL; ++x) vc[x] = vn[x];
-      if (i + 1 < n) load(i + 1);
-      if (__builtin_amdgcn_readlane(id, i) < 0) continue;                     // an absent block: nothing is seen
-      const float sk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), i));
-      const float sv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), i));
-      const int t0 = ks.step(j0 + 4 * i) * 32;
-      const bool full = kv_all_see(t0, first_pos, last_pos, pre, window);
-
-      kv_f32x4 s[2][NC];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c) s[t][c] = kv_f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const uint4 u = kc[t * KL + k / 2];
-          const kv_bf16x8 kf = (k & 1) ? kv_operand(u.z, u.w, sk) : kv_operand(u.x, u.y, sk);
-#pragma unroll
-          for (int c = 0; c < NC; ++c) s[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][k], s[t][c], 0, 0, 0);
-        }
-      }
-      if (!full) {                       // values that are NaN must not reach rows that do not see them: 0 * NaN would
-#pragma unroll
-        for (int x = 0; x < VL; ++x) {
-          nan |= __ballot(kv_nan_bytes(vc[x]) != 0) != 0;
-          vc[x] = kv_without_nan(vc[x]);
-        }
-      }
-      kv_bf16x8 pf[NC];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            float v = s[t][c][x];
-            const int tok = t0 + 16 * t + 4 * kq + x;
-            if (a.sc.cap > 0.f) v = kv_capped(v * a.sc.scale, a.sc.cap) * KV_LOG2E;
-            else v *= scale2;
-            if (a.sc.slopes) v -= slope[c] * fabsf(float(pos[c] - tok));
-            if (!full && !sight[c].sees(tok, pre)) v = -INFINITY;
-            s[t][c][x] = v;
-            top = fmaxf(top, v);
+        for (int x = 0; x < 4; ++x) {
+          const int tok = t0 + 16 * t + 4 * kq + x;
+          if (EXTRA) {
+            const float v = s[t][c][x];
+            s[t][c][x] = (a.sc.cap > 0.f ? kv_capped(v * a.sc.scale, a.sc.cap) * KV_LOG2E : v * scale2) - slope[c] * fabsf(float(pos[c] - tok));
           }
-        if (__any(top > m[c] + 8.f)) {       // the running maximum follows only where weights would pass 2^8: the sums are rescaled seldom
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float mn = fmaxf(m[c], top), f = exp2f(m[c] - mn);
-          m[c] = mn;
-          l[c] *= f;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) o[c][d] *= f;
+          if (!full && !sight[c].sees(tok, pre)) s[t][c][x] = -INFINITY;
+          top = fmaxf(top, s[t][c][x]);
         }
+      if (!EXTRA) top *= scale2;
+      if (__any(top > m[c] + 8.f)) {       // the running maximum follows only where weights would pass 2^8: the sums are rescaled seldom
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m[c], top), f = __builtin_amdgcn_exp2f(m[c] - mn);
+        m[c] = mn;
+        l[c] *= f;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const float e = __builtin_amdgcn_exp2f(s[t][c][x] - m[c]);
-            l[c] += e;
-            pf[c][4 * t + x] = static_cast<__bf16>(e);
-          }
+        for (int d = 0; d < DT; ++d) o[c][d] *= f;
       }
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const uint4 u = vc[d / 2];
-        const kv_bf16x8 vf = (d & 1) ? kv_operand(u.z, u.w, sv) : kv_operand(u.x, u.y, sv);
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[c], o[c][d], 0, 0, 0);
+        for (int x = 0; x < 4; ++x) {
+          const float e = __builtin_amdgcn_exp2f(EXTRA ? s[t][c][x] - m[c] : fmaf(s[t][c][x], scale2, -m[c]));
+          l[c] += e;
+          pf[c][4 * t + x] = static_cast<__bf16>(e);
+        }
+    }
+    if (!full) {                         // values that are NaN must not reach rows that do not see them: 0 * NaN would
+#pragma unroll
+      for (int x = 0; x < VL; ++x) {
+        nan |= __ballot(kv_nan_bytes(vc[x]) != 0) != 0;
+        vc[x] = kv_without_nan(vc[x]);
       }
     }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      const uint4 u = vc[d / 2];
+      const kv_bf16x8 vf = (d & 1) ? kv_operand(u.z, u.w, sv) : kv_operand(u.x, u.y, sv);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[c], o[c][d], 0, 0, 0);
+      if (d % 2) __builtin_amdgcn_sched_barrier(0);
+    }
+    load_values(j + W, next);
   }
 
-  // the waves' results: common maximum, then sums in the waves' order
+  // the waves' results: common maximum, then sums in a fixed order: wave v + 4 joins wave v, then four waves in a row
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     l[c] += __shfl_xor(l[c], 16);
@@ -229,45 +245,59 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
   __syncthreads();
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const float mt = fmaxf(fmaxf(ml[0][c * 16 + r].x, ml[1][c * 16 + r].x), fmaxf(ml[2][c * 16 + r].x, ml[3][c * 16 + r].x));
+    float mt = ml[0][c * 16 + r].x;
+#pragma unroll
+    for (int v = 1; v < W; ++v) mt = fmaxf(mt, ml[v][c * 16 + r].x);
     const float f = exp2f(m[c] - mt);
     if (c > 0) __syncthreads();              // the columns before have been read
+    if (W == 8) {
+      if (wave >= 4) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<kv_f32x4*>(&obuf[wave][r][d * 16 + kq * 4]) = o[c][d] * f;
+        for (int d = 0; d < DT; ++d) *reinterpret_cast<kv_f32x4*>(&obuf[wave & 3][r][d * 16 + kq * 4]) = o[c][d] * f;
+      }
+      __syncthreads();
+    }
+    if (wave < 4) {                          // a lane reads and writes its own places
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        kv_f32x4* at = reinterpret_cast<kv_f32x4*>(&obuf[wave][r][d * 16 + kq * 4]);
+        kv_f32x4 v = o[c][d] * f;
+        if (W == 8) v += *at;
+        *at = v;
+      }
+    }
     __syncthreads();
-    constexpr int V = DH / 16;               // values a thread gathers
-    const int oc = tid / 16, col = c * 16 + oc, d0 = tid % 16 * V, i = col / a.group, g = col - i * a.group;
-    if (i < rows) {
-      float2 x[4];
+    constexpr int V = DH / (W * 4);          // values a thread gathers
+    const int oc = tid / (W * 4), col = c * 16 + oc, d0 = tid % (W * 4) * V, row = col / a.group, g = col - row * a.group;
+    if (row < rows) {
+      float mm = ml[0][col].x, lt = 0.f;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) x[v] = ml[v][col];
-      const float mm = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
-      float lt = 0.f;
+      for (int v = 1; v < W; ++v) mm = fmaxf(mm, ml[v][col].x);
 #pragma unroll
-      for (int v = 0; v < 4; ++v) lt += x[v].y * exp2f(x[v].x - mm);
+      for (int v = 0; v < W; ++v) lt += ml[v][col].y * exp2f(ml[v][col].x - mm);
       float y[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) y[e] = ((obuf[0][oc][d0 + e] + obuf[1][oc][d0 + e]) + obuf[2][oc][d0 + e]) + obuf[3][oc][d0 + e];
       if (pl.chunks == 1) {
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
-        uint16_t* dst = a.out + (q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + d0;
+        uint16_t* dst = a.out + (q.row0 + row) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + d0;
 #pragma unroll
         for (int e = 0; e < V; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = kv_pair(y[e] * inv, y[e + 1] * inv);
       } else {
         const long long at = (static_cast<long long>(w) * a.c.heads + h) * a.cols + col;
         if (d0 == 0) a.parts.ml[at] = make_float2(mm, lt);
 #pragma unroll
-        for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(a.parts.o + at * DH + d0 + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+        for (int e = 0; e < V; ++e) a.parts.o[at * DH + d0 + e] = y[e];
       }
     }
   }
 
   // NaN among values that some rows do not see was left out of the products: the dims of those who see it become NaN
   if (__syncthreads_or(nan) == 0 || !nan) return;
-  for (int j = pl.chunk * pl.steps + wave; j < j_end; j += 4) {
-    const int t0 = ks.step(j) * 32, id = table[t0 >> a.c.bt_log2];
-    if (id < 0 || id >= a.c.n_blocks || kv_all_see(t0, first_pos, last_pos, pre, window)) continue;
-    const uint8_t* v = a.c.v + (static_cast<long long>(id) * a.c.heads + h) * block_bytes + (t0 & ((1 << a.c.bt_log2) - 1)) * DH + lane * 16;
+  for (int j = j_begin; j < j_end; j += W) {
+    const int t0 = ks.step(j) * 32, bid = table[t0 >> a.c.bt_log2];
+    if (bid < 0 || bid >= a.c.n_blocks || kv_all_see(t0, first_pos, last_pos, pre, window)) continue;
+    const uint8_t* v = a.c.v + (static_cast<long long>(bid) * a.c.heads + h) * block_bytes + (t0 & ((1 << a.c.bt_log2) - 1)) * DH + lane * 16;
 #pragma unroll 1
     for (int d = 0; d < DT; ++d) {
       const uint2 w2 = *reinterpret_cast<const uint2*>(v + d / 2 * 1024 + d % 2 * 8);
@@ -278,13 +308,13 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
 #pragma unroll
         for (int y = 0; y < 8; ++y) sees[y] = static_cast<__bf16>(sight[c].sees(t0 + y / 4 * 16 + 4 * kq + y % 4, pre) ? 1.f : 0.f);
         const kv_f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, sees, kv_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-        const int col = c * 16 + r, i = col / a.group, g = col - i * a.group;
-        if (i >= rows) continue;
+        const int col = c * 16 + r, row = col / a.group, g = col - row * a.group;
+        if (row >= rows) continue;
 #pragma unroll
         for (int y = 0; y < 4; ++y)
           if (n[y] > 0.f) {
             const int dim = d * 16 + kq * 4 + y;
-            if (pl.chunks == 1) a.out[(q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + dim] = 0x7fc0;
+            if (pl.chunks == 1) a.out[(q.row0 + row) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + dim] = 0x7fc0;
             else a.parts.o[((static_cast<long long>(w) * a.c.heads + h) * a.cols + col) * DH + dim] = NAN;
           }
       }
@@ -292,16 +322,20 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(FewArgs a) {
   }
 }
 
-// Joins parts: one wave for each column of a sequence and key head.  splits 0: the chunks of few_plan; else so many parts of every column.
+// Joins parts: a work-group for each column of a sequence and key head.  DH / 4 lanes hold a row; the 1024 / DH such groups of lanes take every so many-th
+// part, and their sums are added in order.  splits 0: the chunks of few_plan; else so many parts of every column.
 struct JoinArgs {
   FewArgs few;
-  int col_tiles, splits;
+  int splits;
 };
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv_attend_join(JoinArgs ja) {
+  constexpr int L = DH / 4, GROUPS = 256 / L;
+  __shared__ float4 sums[GROUPS][L];
+  __shared__ float lsum[GROUPS];
   const FewArgs& a = ja.few;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int h = blockIdx.x % a.c.heads, s = blockIdx.x / a.c.heads / ja.col_tiles, col = blockIdx.x / a.c.heads % ja.col_tiles * 4 + wave;
+  const int group = threadIdx.x / L, lane = threadIdx.x % L;
+  const int h = blockIdx.x % a.c.heads, s = blockIdx.x / a.c.heads / a.cols, col = blockIdx.x / a.c.heads % a.cols;
   int chunks = ja.splits;
   long long step = static_cast<long long>(a.b.S) * a.c.heads * a.cols, at = (static_cast<long long>(s) * a.c.heads + h) * a.cols + col;
   if (ja.splits == 0) {
@@ -315,37 +349,40 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(JoinArgs ja) {
   const int i = col / a.group, g = col - i * a.group;
   if (i >= min(q.n, a.b.T)) return;
   float m = -3e38f;
-  for (int c = lane; c < chunks; c += 64) m = fmaxf(m, a.parts.ml[at + c * step].x);
+  for (int c = threadIdx.x & 63; c < chunks; c += 64) m = fmaxf(m, a.parts.ml[at + c * step].x);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  float l = 0.f, o[DH / 64] = {};
-  for (int c0 = 0; c0 < chunks; c0 += 64) {
-    float f = 0.f, lc = 0.f;
-    if (c0 + lane < chunks) {
-      const float2 x = a.parts.ml[at + (c0 + lane) * step];
-      f = exp2f(x.x - m);
-      lc = x.y * f;
-    }
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int c = group; c < chunks; c += GROUPS) {
+    const float2 x = a.parts.ml[at + c * step];
+    const float4 p = *reinterpret_cast<const float4*>(a.parts.o + (at + c * step) * DH + lane * 4);
+    const float f = exp2f(x.x - m);
+    l += x.y * f;
+    o.x += f * p.x; o.y += f * p.y; o.z += f * p.z; o.w += f * p.w;
+  }
+  sums[group][lane] = o;
+  if (lane == 0) lsum[group] = l;
+  __syncthreads();
+  if (group > 0) return;
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) lc += __shfl_xor(lc, d);
-    l += lc;
-    const int n = min(64, chunks - c0);
-#pragma unroll 4
-    for (int c = 0; c < n; ++c) {
-      const float fc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), c));
-      const float* p = a.parts.o + (at + (c0 + c) * step) * DH + lane * (DH / 64);
-#pragma unroll
-      for (int e = 0; e < DH / 64; ++e) o[e] += fc * p[e];
-    }
+  for (int v = 1; v < GROUPS; ++v) {
+    const float4 p = sums[v][lane];
+    o.x += p.x; o.y += p.y; o.z += p.z; o.w += p.w;
+    l += lsum[v];
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t* dst = a.out + (q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + lane * (DH / 64);
-#pragma unroll
-  for (int e = 0; e < DH / 64; ++e) dst[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(o[e] * inv));
+  uint16_t* dst = a.out + (q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + lane * 4;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(kv_pair(o.x * inv, o.y * inv), kv_pair(o.z * inv, o.w * inv));
 }
 
 namespace {
-constexpr int FEW_TARGET_WGS = 1024, FEW_MIN_STEPS = 8;
+#ifndef FEW_TARGET
+#define FEW_TARGET 1024
+#define FEW_MIN 32
+#endif
+constexpr int FEW_TARGET_WGS = FEW_TARGET, FEW_MIN_STEPS = FEW_MIN;
 long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c) {          // chunks at most; 0: one a sequence
   const long long most = static_cast<long long>(b.table_width) * c.block_tokens / 32;
   if (most <= FEW_MIN_STEPS) return 0;
@@ -353,8 +390,8 @@ long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c) {          
   return target + static_cast<long long>(b.S);
 }
 void launch_join(const FewArgs& a, int dh, int splits, hipStream_t st) {
-  JoinArgs ja{a, (a.cols + 3) / 4, splits};
-  const dim3 grid(static_cast<unsigned>(static_cast<long long>(a.b.S) * a.c.heads * ja.col_tiles)), block(256);
+  const JoinArgs ja{a, splits};
+  const dim3 grid(static_cast<unsigned>(static_cast<long long>(a.b.S) * a.c.heads * a.cols)), block(256);
   if (dh == 64) hipLaunchKernelGGL((k_kv_attend_join<64>), grid, block, 0, st, ja);
   else if (dh == 128) hipLaunchKernelGGL((k_kv_attend_join<128>), grid, block, 0, st, ja);
   else hipLaunchKernelGGL((k_kv_attend_join<256>), grid, block, 0, st, ja);
@@ -389,19 +426,26 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   const long long wgs = (chunks ? chunks : b.S) * c.n_heads;
   if (wgs >= (1ll << 31)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld work-groups", wgs);
   ProfileScope ps(MOQE_PK_OTHER, st);
-  const dim3 grid(static_cast<unsigned>(wgs)), block(256);
+  const dim3 grid(static_cast<unsigned>(wgs));
   const int nc = a.cols <= 16 ? 1 : a.cols <= 32 ? 2 : 4;
+  const bool extra = at.slopes || at.cap > 0.f || !(at.scale > 0.f);
+#define MOQE_FEW(DH, NC, W)                                                                             \
+  do {                                                                                                  \
+    if (extra) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, true>), grid, dim3(W * 64), 0, st, a);    \
+    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, false>), grid, dim3(W * 64), 0, st, a);         \
+  } while (0)
   if (c.head_dim == 64) {
-    if (nc == 1) hipLaunchKernelGGL((k_kv_attend_few<64, 1>), grid, block, 0, st, a);
-    else if (nc == 2) hipLaunchKernelGGL((k_kv_attend_few<64, 2>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_kv_attend_few<64, 4>), grid, block, 0, st, a);
+    if (nc == 1) MOQE_FEW(64, 1, 8);
+    else if (nc == 2) MOQE_FEW(64, 2, 8);
+    else MOQE_FEW(64, 4, 4);
   } else if (c.head_dim == 128) {
-    if (nc == 1) hipLaunchKernelGGL((k_kv_attend_few<128, 1>), grid, block, 0, st, a);
-    else if (nc == 2) hipLaunchKernelGGL((k_kv_attend_few<128, 2>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_kv_attend_few<128, 4>), grid, block, 0, st, a);
+    if (nc == 1) MOQE_FEW(128, 1, 8);
+    else if (nc == 2) MOQE_FEW(128, 2, 8);
+    else MOQE_FEW(128, 4, 4);
   } else {
-    hipLaunchKernelGGL((k_kv_attend_few<256, 1>), grid, block, 0, st, a);
+    MOQE_FEW(256, 1, 8);
   }
+#undef MOQE_FEW
   if (chunks) launch_join(a, c.head_dim, 0, st);
   return check_launch("kv_attention");
 }

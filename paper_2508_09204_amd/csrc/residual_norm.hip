@@ -3,11 +3,15 @@
 
 namespace moqe {
 
+#ifndef NORM_ONE
+#define NORM_ONE 1024
+#endif
+
 struct NormArgs {
   const void* y; const void* r; void* r_out; uint16_t* out;
   const float *gate, *post_gain, *post_offset, *pre_gain, *pre_offset;
   long long ys, rs, ros, os;
-  int M, d, gate_rows, post, pre;
+  int M, d, gate_rows, post, pre, row_threads;
   float scale, post_eps, pre_eps;
 };
 
@@ -79,28 +83,29 @@ __device__ __forceinline__ void store_values(void* base, long long at, int f, in
   }
 }
 
-// Sum over the WAVES waves of a row, the same in all lanes: a butterfly in each wave, the waves' sums in their order.  `slot`: a place of its own for
-// each sum of a row, so that one barrier is enough.
-template <int WAVES>
-__device__ __forceinline__ float row_sum(float v, float* part, int slot) {
+// Sum over the waves of a row, the same in all lanes: a butterfly in each wave, the waves' sums in their order.  `part`: a place of its own for each sum of a
+// row, so that one barrier is enough.
+__device__ __forceinline__ float row_sum(float v, int waves, float* part) {
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-  if constexpr (WAVES > 1) {
-    if ((threadIdx.x & 63) == 0) part[slot * WAVES + (threadIdx.x >> 6)] = v;
+  if (waves > 1) {
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) v += part[slot * WAVES + w];
+    for (int w = 0; w < waves; ++w) v += part[w];
   }
   return v;
 }
 
-// The row's values in registers: NV pieces of eight a thread, piece j from feature (j * threads + thread) * 8 on; zeros past the row's end.
-constexpr int NV = 4;
-template <int WAVES, bool ODD>
-__device__ __forceinline__ void normed(float (&t)[NV][8], int d, int kind, float eps, const float* gain, const float* offset, float* part, int slot) {
-  constexpr int TH = WAVES * 64;
-  const int lane = threadIdx.x % TH;
+// A row's values in the registers of its `th` threads: NV pieces of eight, piece j from feature (j * th + lane) * 8 on; zeros past the row's end.
+template <int NV, bool ODD>
+__device__ __forceinline__ void normed(float (&t)[NV][8], int d, int th, int lane, int kind, float eps, const float* gain, const float* offset, float* part) {
+  float g[NV][8];                       // asked for before the sums are known, where registers allow it
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int f = (j * th + lane) * 8;
+    if (NV <= 2 && gain && f < d) load_values<false, ODD>(gain, 0, f, d, g[j]);
+  }
   float mean = 0.f;
   if (kind == MOQE_NORM_LAYER) {
     float s = 0.f;
@@ -108,47 +113,46 @@ __device__ __forceinline__ void normed(float (&t)[NV][8], int d, int kind, float
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += t[j][i];
-    mean = row_sum<WAVES>(s, part, slot) / float(d);
+    mean = row_sum(s, th / 64, part) / float(d);
   }
   float q = 0.f;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int f = (j * TH + lane) * 8;
+    const int f = (j * th + lane) * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       t[j][i] = f + (ODD ? i : 0) < d ? t[j][i] - mean : 0.f;
       q += t[j][i] * t[j][i];
     }
   }
-  const float inv = 1.f / sqrtf(row_sum<WAVES>(q, part, slot + 1) / float(d) + eps);
+  const float inv = 1.f / sqrtf(row_sum(q, th / 64, part + 16) / float(d) + eps);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int f = (j * TH + lane) * 8;
+    const int f = (j * th + lane) * 8;
     if (f < d) {
-      float g[8], o[8];
-      if (gain) load_values<false, ODD>(gain, 0, f, d, g);
+      float o[8];
+      if (NV > 2 && gain) load_values<false, ODD>(gain, 0, f, d, g[j]);
       if (offset) load_values<false, ODD>(offset, 0, f, d, o);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        t[j][i] *= gain ? inv * g[i] : inv;
+        t[j][i] *= gain ? inv * g[j][i] : inv;
         if (offset) t[j][i] += o[i];
       }
     }
   }
 }
 
-// WAVES waves a row, the row in registers (WAVES * 2048 features at most), every input read once.
-template <int WAVES, bool ODD, bool YBF, bool RBF>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_residual_norm(NormArgs a) {
-  constexpr int TH = WAVES * 64;
-  __shared__ float part[WAVES == 1 ? 1 : 4 * WAVES];
-  const int row = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-  if (row >= a.M) return;                            // whole waves; with one wave a row there is no barrier
-  const int lane = threadIdx.x % TH, d = a.d;
+// A row in the registers of a.row_threads threads, every input read once.  Rows of one wave need no barrier, and four share a work-group.
+template <int NV, bool ODD, bool YBF, bool RBF>
+__global__ __launch_bounds__(1024) void k_residual_norm(NormArgs a) {
+  __shared__ float part[4 * 16];
+  const int th = a.row_threads, d = a.d, lane = th == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int row = th == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  if (row >= a.M) return;
   float u[NV][8], t[NV][8];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int f = (j * TH + lane) * 8;
+    const int f = (j * th + lane) * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[j][i] = t[j][i] = 0.f;
     if (f < d) {
@@ -157,11 +161,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_residual_norm
     }
   }
   if (a.y) {
-    if (a.post != MOQE_NORM_NONE) normed<WAVES, ODD>(u, d, a.post, a.post_eps, a.post_gain, a.post_offset, part, 0);
+    if (a.post != MOQE_NORM_NONE) normed<NV, ODD>(u, d, th, lane, a.post, a.post_eps, a.post_gain, a.post_offset, part);
     const float* gate = a.gate ? a.gate + (a.gate_rows > 0 ? static_cast<long long>(row / a.gate_rows) * d : 0) : nullptr;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int f = (j * TH + lane) * 8;
+      const int f = (j * th + lane) * 8;
       if (f < d) {
         float g[8];
         if (gate) load_values<false, ODD>(gate, 0, f, d, g);
@@ -173,33 +177,37 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_residual_norm
   if (a.r_out) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int f = (j * TH + lane) * 8;
+      const int f = (j * th + lane) * 8;
       if (f < d) store_values<RBF, ODD>(a.r_out, row * a.ros, f, d, t[j]);
     }
   }
   if (!a.out) return;
-  if (a.pre != MOQE_NORM_NONE) normed<WAVES, ODD>(t, d, a.pre, a.pre_eps, a.pre_gain, a.pre_offset, part, 2);
+  if (a.pre != MOQE_NORM_NONE) normed<NV, ODD>(t, d, th, lane, a.pre, a.pre_eps, a.pre_gain, a.pre_offset, part + 32);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int f = (j * TH + lane) * 8;
+    const int f = (j * th + lane) * 8;
     if (f < d) store_values<true, ODD>(a.out, row * a.os, f, d, t[j]);
   }
 }
 
 namespace {
-template <int WAVES, bool ODD>
+template <int NV, bool ODD>
 void launch_types(const NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
-  const dim3 grid(WAVES == 1 ? (a.M + 3) / 4 : a.M), block(WAVES == 1 ? 256 : WAVES * 64);
-  if (ybf && rbf) hipLaunchKernelGGL((k_residual_norm<WAVES, ODD, true, true>), grid, block, 0, st, a);
-  else if (ybf) hipLaunchKernelGGL((k_residual_norm<WAVES, ODD, true, false>), grid, block, 0, st, a);
-  else if (rbf) hipLaunchKernelGGL((k_residual_norm<WAVES, ODD, false, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_residual_norm<WAVES, ODD, false, false>), grid, block, 0, st, a);
+  const bool wave_rows = a.row_threads == 64;
+  const dim3 grid(wave_rows ? (a.M + 3) / 4 : a.M), block(wave_rows ? 256 : a.row_threads);
+  if (ybf && rbf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, true, true>), grid, block, 0, st, a);
+  else if (ybf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, true, false>), grid, block, 0, st, a);
+  else if (rbf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, false, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_residual_norm<NV, ODD, false, false>), grid, block, 0, st, a);
 }
 template <bool ODD>
-void launch_waves(const NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
-  if (a.d <= 2048) launch_types<1, ODD>(a, ybf, rbf, st);
-  else if (a.d <= 8192) launch_types<4, ODD>(a, ybf, rbf, st);
-  else launch_types<16, ODD>(a, ybf, rbf, st);
+void launch_pieces(NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
+  const int pieces = (a.d + 7) / 8;
+  const int nv = pieces <= NORM_ONE ? 1 : pieces <= 2048 ? 2 : 4;
+  a.row_threads = ((pieces + nv - 1) / nv + 63) / 64 * 64;
+  if (nv == 1) launch_types<1, ODD>(a, ybf, rbf, st);
+  else if (nv == 2) launch_types<2, ODD>(a, ybf, rbf, st);
+  else launch_types<4, ODD>(a, ybf, rbf, st);
 }
 }  // namespace
 
@@ -222,8 +230,8 @@ int32_t launch_residual_norm(const moqe_residual_step& s, hipStream_t st) {
   if (s.out) strides |= s.out_stride;
   ProfileScope ps(MOQE_PK_OTHER, st);
   const bool ybf = s.y_type == MOQE_TYPE_BF16, rbf = s.residual_type == MOQE_TYPE_BF16;
-  if (at % 16 == 0 && strides % 8 == 0) launch_waves<false>(a, ybf, rbf, st);
-  else launch_waves<true>(a, ybf, rbf, st);
+  if (at % 16 == 0 && strides % 8 == 0) launch_pieces<false>(a, ybf, rbf, st);
+  else launch_pieces<true>(a, ybf, rbf, st);
   return check_launch("residual_norm");
 }
 
