@@ -80,8 +80,9 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
   const int rows = min(q.n, a.b.T), first_pos = q.first();
   if (rows == 0) return;
   const int pre = a.sc.prefix ? min(a.sc.prefix[pl.s], q.len) : 0, window = a.sc.window, last_pos = first_pos + rows - 1;
+  const KvRange all_see = kv_all_see(first_pos, last_pos, pre, window);
   const int j_begin = pl.chunk * pl.steps + wave, j_end = min(ks.count, pl.chunk < 1 ? pl.steps : pl.steps * (pl.chunk + 1));
-  const float scale2 = a.sc.scale * KV_LOG2E;
+  const float scale2 = a.sc.scale2;
 
   // 64 steps of this wave at a time: lane i looks up step j0 + W i: block (-1: absent, nothing is seen) and scales
   const long long block_bytes = static_cast<long long>(DH) << a.c.bt_log2;
@@ -148,6 +149,7 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
   }
 
   bool nan = false;
+  __builtin_amdgcn_s_waitcnt(0);         // the queries have come: else the loop would wait for all loads under way before its first product, every time
   {
     const int bid = max(__builtin_amdgcn_readlane(id, 0), 0);
     load_keys(j_begin, bid);
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
       next = max(__builtin_amdgcn_readlane(id, i), 0);
     }
     const int t0 = bid < 0 ? 1 << 30 : ks.step(j) * 32;
-    const bool full = kv_all_see(t0, first_pos, last_pos, pre, window);
+    const bool full = all_see.has(t0);
     kv_f32x4 s[2][NC];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -191,10 +193,7 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int tok = t0 + 16 * t + 4 * kq + x;
-          if (EXTRA) {
-            const float v = s[t][c][x];
-            s[t][c][x] = (a.sc.cap > 0.f ? kv_capped(v * a.sc.scale, a.sc.cap) * KV_LOG2E : v * scale2) - slope[c] * fabsf(float(pos[c] - tok));
-          }
+          if (EXTRA) s[t][c][x] = kv_extra_score(a.sc, s[t][c][x], slope[c], pos[c] - tok);
           if (!full && !sight[c].sees(tok, pre)) s[t][c][x] = -INFINITY;
           top = fmaxf(top, s[t][c][x]);
         }
@@ -211,15 +210,14 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float e = __builtin_amdgcn_exp2f(EXTRA ? s[t][c][x] - m[c] : fmaf(s[t][c][x], scale2, -m[c]));
-          l[c] += e;
-          pf[c][4 * t + x] = static_cast<__bf16>(e);
-        }
+        for (int x = 0; x < 4; ++x)
+          pf[c][4 * t + x] = static_cast<__bf16>(__builtin_amdgcn_exp2f(EXTRA ? s[t][c][x] - m[c] : fmaf(s[t][c][x], scale2, -m[c])));
+      l[c] = kv_add8(pf[c], l[c]);
     }
     if (!full) {                         // values that are NaN must not reach rows that do not see them: 0 * NaN would
 #pragma unroll
       for (int x = 0; x < VL; ++x) {
+        vc[x] = kv_before(vc[x], t0 + 4 * kq, q.len);
         nan |= __ballot(kv_nan_bytes(vc[x]) != 0) != 0;
         vc[x] = kv_without_nan(vc[x]);
       }
@@ -296,7 +294,7 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
   if (__syncthreads_or(nan) == 0 || !nan) return;
   for (int j = j_begin; j < j_end; j += W) {
     const int t0 = ks.step(j) * 32, bid = table[t0 >> a.c.bt_log2];
-    if (bid < 0 || bid >= a.c.n_blocks || kv_all_see(t0, first_pos, last_pos, pre, window)) continue;
+    if (bid < 0 || bid >= a.c.n_blocks || all_see.has(t0)) continue;
     const uint8_t* v = a.c.v + (static_cast<long long>(bid) * a.c.heads + h) * block_bytes + (t0 & ((1 << a.c.bt_log2) - 1)) * DH + lane * 16;
 #pragma unroll 1
     for (int d = 0; d < DT; ++d) {
@@ -416,7 +414,7 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
   a.b = kv_batch_args(b);
   a.c = kv_cache_args(c);
-  a.sc = KvScore{at.slopes, at.prefix, at.scale, at.cap, at.window};
+  a.sc = kv_score(at);
   a.group = at.n_heads / c.n_heads;
   a.cols = b.T * a.group;
   a.target = FEW_TARGET_WGS / c.n_heads > 0 ? FEW_TARGET_WGS / c.n_heads : 1;
@@ -428,7 +426,7 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   ProfileScope ps(MOQE_PK_OTHER, st);
   const dim3 grid(static_cast<unsigned>(wgs));
   const int nc = a.cols <= 16 ? 1 : a.cols <= 32 ? 2 : 4;
-  const bool extra = at.slopes || at.cap > 0.f || !(at.scale > 0.f);
+  const bool extra = kv_extra(at);
 #define MOQE_FEW(DH, NC, W)                                                                             \
   do {                                                                                                  \
     if (extra) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, true>), grid, dim3(W * 64), 0, st, a);    \

@@ -3,6 +3,10 @@
 
 namespace moqe {
 
+// LDS reads issued before this point stay before the matrix products after it: the scheduler would put each read next to its product and wait for it there.
+// Other arithmetic may cross.
+#define KEEP_READS_AHEAD() __builtin_amdgcn_sched_barrier(0x406)
+
 struct RowsArgs {
   const uint16_t* q; uint16_t* out;
   long long q_stride, out_stride;
@@ -12,18 +16,18 @@ struct RowsArgs {
   KvParts parts;                // [split][sequence][key head][column]
 };
 
-// One work-group takes 128 columns (row i, query head g of the key head's group: column i * group + g), 32 for each of its four waves (64 and 16 where the head
-// is 256 wide: more does not fit the registers), through the
-// tokens in tiles of 64.  The tile's codes become bf16 operands once, on their way into LDS (two buffers, one barrier a tile; the codes of the tile after
-// next are already under way in registers), in the order in which a wave reads them: 16 bytes a lane in a row, no bank conflicts.  Scores stay in registers:
-// the layout of S^T = K Q^T is the operand layout of O^T = V^T P^T.
+// One work-group takes 128 columns (row i, query head g of the key head's group: column i * group + g), 32 for each of its four waves, through the tokens in
+// tiles of 64.  The tile's codes become bf16 operands once, on their way into LDS (two buffers, one barrier a tile; the codes of the tile after next are already
+// under way in registers), in the order in which a wave reads them: 16 bytes a lane in a row, no bank conflicts.  Products are 32 x 32 x 16, half as many
+// instructions as 16 x 16 x 32 at the same rate: a SIMD issues them and the softmax's arithmetic through one port, and that port is what it runs out of.
+// Scores stay in registers: the layout of S^T = K Q^T is the operand layout of O^T = V^T P^T if 16 tokens of values go 0..3, 8..11 | 4..7, 12..15.
 // EXTRA: scores are capped, biased, or their scale is not positive.
 template <int DH, bool EXTRA>
-__global__ __launch_bounds__(256, 2) void k_kv_attend_rows(RowsArgs a) {
-  constexpr int NC = DH == 256 ? 1 : 2, COLS = NC * 64, KS = DH / 32, DT = DH / 16, U = DH / 64;   // U: 16-byte units of keys (and of values) a thread brings in
+__global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsArgs a) {
+  constexpr int COLS = 128, KS = DH / 16, DT = DH / 32, U = DH / 64;           // U: 16-byte units of keys (and of values) a thread brings in
   constexpr int HALF = 64 * DH * 2;                                            // bytes of a tile's keys in bf16
   extern __shared__ __align__(16) uint8_t lds[];                               // [2][keys, values]
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, kq = lane >> 4;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, kq = lane >> 4, c32 = lane & 31, half = lane >> 5;
   // work-groups of one sequence and key head stay on one XCD (round robin over 8): its L2 holds their keys and values; the longest tiles go first
   const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
   const int per = a.tiles * a.splits, sh = slot / per * 8 + xcd;
@@ -36,43 +40,39 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(RowsArgs a) {
   const int i_last = min((tile * COLS + COLS - 1) / a.group, rows - 1);
   const int p_first = first_pos + i_first, p_last = first_pos + i_last;
   const int pre = a.sc.prefix ? min(a.sc.prefix[s], q.len) : 0, window = a.sc.window;
-  const KvSteps ks = kv_steps(q.len, min(q.len, max(max(p_last + 1, pre), 0)), p_first, window, pre);
-  const float scale2 = a.sc.scale * KV_LOG2E;
-  // the wave's own rows
-  const int col0 = tile * COLS + wave * NC * 16;
-  const int w_first = first_pos + min(col0 / a.group, rows - 1), w_last = first_pos + min((col0 + NC * 16 - 1) / a.group, rows - 1);
+  const int seen = min(q.len, max(max(p_last + 1, pre), 0));                   // tokens from here on are seen by no row of the work-group
+  const KvSteps ks = kv_steps(q.len, seen, p_first, window, pre);
+  const float scale2 = a.sc.scale2;
+  // the wave's own rows, and this lane's: both halves of a wave hold the same 32 columns
+  const int col0 = tile * COLS + wave * 32;
+  const int w_first = first_pos + min(col0 / a.group, rows - 1), w_last = first_pos + min((col0 + 31) / a.group, rows - 1);
   const bool idle = col0 / a.group >= rows;
+  const KvRange wg_all = kv_all_see(p_first, p_last, pre, window), all_see = kv_all_see(w_first, w_last, pre, window),
+                some_see = kv_some_see(w_first, w_last, pre, window);
+  const int col = col0 + c32, row = col / a.group, head = h * a.group + col - row * a.group;
+  const bool mine = row < rows;
+  const int pos = first_pos + row;
+  const KvSight sight = kv_sight(pos, q.len, window);
+  const float slope = EXTRA && mine && a.sc.slopes ? a.sc.slopes[head] * KV_LOG2E : 0.f;
 
-  kv_bf16x8 qf[NC][KS];
-  KvSight sight[NC];
-  int pos[NC];
-  float slope[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int col = col0 + c * 16 + r, i = col / a.group, g = col - i * a.group;
-    const bool in = i < rows;
-    pos[c] = first_pos + i;
-    sight[c] = kv_sight(pos[c], q.len, window);
-    if (EXTRA) slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
-    const uint16_t* src = a.q + (q.row0 + i) * a.q_stride + static_cast<long long>(h * a.group + g) * DH + kq * 8;
+  kv_bf16x8 qf[KS];
+  {
+    const uint16_t* src = a.q + (q.row0 + row) * a.q_stride + static_cast<long long>(head) * DH + half * 8;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       uint4 v = make_uint4(0, 0, 0, 0);
-      if (in) v = *reinterpret_cast<const uint4*>(src + k * 32);
-      qf[c][k] = __builtin_bit_cast(kv_bf16x8, v);
+      if (mine) v = *reinterpret_cast<const uint4*>(src + k * 16);
+      qf[k] = __builtin_bit_cast(kv_bf16x8, v);
     }
   }
-  kv_f32x4 o[NC][DT];
-  float m[NC], l[NC];
+  kv_f32x16 o[DT];
+  float m = -3e38f, l = 0.f;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    m[c] = -3e38f;
-    l[c] = 0.f;
+  for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[c][d] = kv_f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+    for (int y = 0; y < 16; ++y) o[d][y] = 0.f;
 
-  const long long block_bytes = static_cast<long long>(DH) << a.c.bt_log2;
+  const uint32_t head_bytes = uint32_t(DH) << a.c.bt_log2;
   const int* table = a.b.table + static_cast<long long>(s) * a.b.width;
   const int all_tiles = (ks.count + 1) / 2;
   const int t_begin = static_cast<int>(static_cast<long long>(all_tiles) * split / a.splits);
@@ -93,50 +93,60 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(RowsArgs a) {
     }
   };
   look_up();
-  // The tile under way: its codes, and of its two steps the scales and the first token (2^30: absent, seen by nobody).
+  // A wave's n-th 64 units of a tile: their step, and the place of the first among that step's 2 * DH.
+  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+  auto unit_step = [&](int n) { return DH == 64 ? wave_u >> 1 : n * 128 / DH; };
+  auto unit_place = [&](int n) { return DH == 64 ? (wave_u & 1) * 64 : n * 256 % (2 * DH) + wave_u * 64; };
+  // The tile under way: its codes, and of its two steps the scales and the first token (2^30: absent, seen by nobody; any block's codes do for it).
   uint4 kc[U], vc[U];
   float sk[2], sv[2];
   int t0n[2];
   auto fetch = [&](int t) {
     if (2 * t >= look + 64) { look += 64; look_up(); }
-    int id[2];
+    const uint8_t *kp[2], *vp[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      id[e] = __builtin_amdgcn_readlane(ids, 2 * t + e - look);
-      sk[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), 2 * t + e - look));
-      sv[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), 2 * t + e - look));
-      t0n[e] = id[e] >= 0 ? ks.step(2 * t + e) * 32 : 1 << 30;
+      const int at = 2 * t + e - look, id = __builtin_amdgcn_readlane(ids, at), first = ks.step(2 * t + e) * 32;
+      sk[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), at));
+      sv[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), at));
+      t0n[e] = id >= 0 ? first : 1 << 30;
+      const long long off = static_cast<long long>(max(id, 0) * static_cast<long long>(a.c.heads) + h) * head_bytes + (first & ((1 << a.c.bt_log2) - 1)) * DH;
+      kp[e] = a.c.k + off;
+      vp[e] = a.c.v + off;
     }
 #pragma unroll
     for (int n = 0; n < U; ++n) {
-      const int u = n * 256 + tid, e = __builtin_amdgcn_readfirstlane(n * 256 + (tid & ~63)) / (2 * DH);    // the step of this wave's units
-      const int bid = e ? id[1] : id[0];
-      kc[n] = vc[n] = make_uint4(0, 0, 0, 0);
-      if (bid >= 0) {
-        const int tok = (e ? t0n[1] : t0n[0]) & ((1 << a.c.bt_log2) - 1);
-        const long long at = (static_cast<long long>(bid) * a.c.heads + h) * block_bytes + tok * DH + (u % (2 * DH)) * 16;
-        kc[n] = *reinterpret_cast<const uint4*>(a.c.k + at);
-        vc[n] = *reinterpret_cast<const uint4*>(a.c.v + at);
-      }
+      const uint32_t at = (unit_place(n) + lane) * 16;
+      kc[n] = *reinterpret_cast<const uint4*>((unit_step(n) ? kp[1] : kp[0]) + at);
+      vc[n] = *reinterpret_cast<const uint4*>((unit_step(n) ? vp[1] : vp[0]) + at);
     }
   };
-  bool nan = false;                    // a value that is NaN lies where some row does not see it
+  bool nan = false;                    // a value that is NaN lies where some row does not see it and another may
   auto put = [&](int buf) {
     uint8_t* kb = lds + buf * 2 * HALF;
     uint8_t* vb = kb + HALF;
 #pragma unroll
     for (int n = 0; n < U; ++n) {
-      const int u = n * 256 + tid, e = __builtin_amdgcn_readfirstlane(n * 256 + (tid & ~63)) / (2 * DH);
+      const int e = unit_step(n), in = unit_place(n);
       const float fk = e ? sk[1] : sk[0], fv = e ? sv[1] : sv[0];
-      const int at = (u >> 6) * 2048 + lane * 16;           // a unit is two operands, 1 KB apart
-      *reinterpret_cast<kv_bf16x8*>(kb + at) = kv_operand(kc[n].x, kc[n].y, fk);
-      *reinterpret_cast<kv_bf16x8*>(kb + at + 1024) = kv_operand(kc[n].z, kc[n].w, fk);
-      if (!kv_all_see(e ? t0n[1] : t0n[0], p_first, p_last, pre, window)) {
+      // keys: 16-token tile in / DH, dims 64 * pair + 32 * st + 8 * kq ..: product k = dims / 16, lane (dims / 8 % 2) * 32 + token
+      const int a16 = in / DH, pair = in % DH / 64;
+      uint8_t* k0 = kb + (e * KS + 4 * pair) * 1024 + kq / 2 * 1024 + ((kq & 1) * 32 + 16 * a16 + r) * 16;
+      *reinterpret_cast<kv_bf16x8*>(k0) = kv_operand(kc[n].x, kc[n].y, fk);
+      *reinterpret_cast<kv_bf16x8*>(k0 + 2048) = kv_operand(kc[n].z, kc[n].w, fk);
+      const int t0 = e ? t0n[1] : t0n[0];
+      if (!wg_all.has(t0)) {
+        vc[n] = kv_before(vc[n], t0 + 4 * kq, seen);
         nan |= __ballot(kv_nan_bytes(vc[n]) != 0) != 0;
         vc[n] = kv_without_nan(vc[n]);
       }
-      *reinterpret_cast<kv_bf16x8*>(vb + at) = kv_operand(vc[n].x, vc[n].y, fv);
-      *reinterpret_cast<kv_bf16x8*>(vb + at + 1024) = kv_operand(vc[n].z, vc[n].w, fv);
+      // values: dims 32 * dpair + 16 * dt + r, tokens 16 * s + 4 * kq ..: product 2 e + s, lane (kq % 2) * 32 + dim, its first or second four tokens
+      const int dpair = in / 64;
+      uint8_t* v0 = vb + (2 * e * DT + dpair) * 1024 + ((kq & 1) * 32 + r) * 16 + kq / 2 * 8;
+      *reinterpret_cast<uint2*>(v0) = kv_four(vc[n].x, fv);
+      *reinterpret_cast<uint2*>(v0 + DT * 1024) = kv_four(vc[n].y, fv);
+      *reinterpret_cast<uint2*>(v0 + 256) = kv_four(vc[n].z, fv);
+      *reinterpret_cast<uint2*>(v0 + DT * 1024 + 256) = kv_four(vc[n].w, fv);
     }
   };
 
@@ -145,8 +155,9 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(RowsArgs a) {
     fetch(t_begin);
     put(0);
     t0c[0] = t0n[0]; t0c[1] = t0n[1];
-    if (t_begin + 1 < t_end) fetch(t_begin + 1);
   }
+  __builtin_amdgcn_s_waitcnt(0);       // the queries have come: else the loop would wait for all loads under way before its first product, every time
+  if (t_begin + 1 < t_end) fetch(t_begin + 1);
   __syncthreads();
   for (int t = t_begin; t < t_end; ++t) {
     const int buf = (t - t_begin) & 1;
@@ -156,143 +167,132 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(RowsArgs a) {
       t0c[0] = t0n[0]; t0c[1] = t0n[1];
       if (t + 2 < t_end) fetch(t + 2);
     }
-    const bool some = kv_some_see(t0[0], w_first, w_last, pre, window) || kv_some_see(t0[1], w_first, w_last, pre, window);
+    const bool some = some_see.has(t0[0]) || some_see.has(t0[1]);
     if (!idle && some) {
-      const bool full = kv_all_see(t0[0], w_first, w_last, pre, window) && kv_all_see(t0[1], w_first, w_last, pre, window);
+      const bool full = all_see.has(t0[0]) && all_see.has(t0[1]);
       const uint8_t* kb = lds + buf * 2 * HALF + lane * 16;
       const uint8_t* vb = kb + HALF;
-      kv_f32x4 sc[4][NC];
+      kv_f32x16 sc[2];
+      kv_bf16x8 kf[2][4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
+      for (int y = 0; y < 4; ++y) kf[0][y] = *reinterpret_cast<const kv_bf16x8*>(kb + (y % 2 * KS + y / 2) * 1024);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) sc[x][c] = kv_f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < KS / 2; ++n) {                // four of the 2 * KS operands (16 dims, step) at a time, the two steps' sums in turn
+        if (n + 1 < KS / 2) {
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const kv_bf16x8 kf = *reinterpret_cast<const kv_bf16x8*>(kb + (x * KS + k) * 1024);
-#pragma unroll
-          for (int c = 0; c < NC; ++c) sc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][k], sc[x][c], 0, 0, 0);
+          for (int y = 0; y < 4; ++y) kf[(n + 1) & 1][y] = *reinterpret_cast<const kv_bf16x8*>(kb + (y % 2 * KS + 2 * (n + 1) + y / 2) * 1024);
         }
-      }
-      kv_bf16x8 pf[NC][2];
+        KEEP_READS_AHEAD();
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (EXTRA) {
+        for (int y = 0; y < 4; ++y) {
+          const int e = y % 2, k = 2 * n + y / 2;
+          if (k == 0) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              float v = sc[x][c][y];
-              v = a.sc.cap > 0.f ? kv_capped(v * a.sc.scale, a.sc.cap) * KV_LOG2E : v * scale2;
-              sc[x][c][y] = v - slope[c] * fabsf(float(pos[c] - (t0[x / 2] + 16 * (x & 1) + 4 * kq + y)));
-            }
-        }
-        if (!full) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-              if (!sight[c].sees(t0[x / 2] + 16 * (x & 1) + 4 * kq + y, pre)) sc[x][c][y] = -INFINITY;
-        }
-        float top = sc[0][c][0];
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) top = fmaxf(top, sc[x][c][y]);
-        if (!EXTRA) top *= scale2;
-        if (__any(top > m[c] + 8.f)) {       // the running maximum follows only where weights would pass 2^8: the sums are rescaled seldom
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float mn = fmaxf(m[c], top), f = __builtin_amdgcn_exp2f(m[c] - mn);
-          m[c] = mn;
-          l[c] *= f;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) o[c][d] *= f;
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const float e = __builtin_amdgcn_exp2f(EXTRA ? sc[x][c][y] - m[c] : fmaf(sc[x][c][y], scale2, -m[c]));
-            l[c] += e;
-            pf[c][x / 2][4 * (x & 1) + y] = static_cast<__bf16>(e);
+            for (int z = 0; z < 16; ++z) sc[e][z] = 0.f;
           }
-      }
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const kv_bf16x8 vf = *reinterpret_cast<const kv_bf16x8*>(vb + (g * DT + d) * 1024);
-#pragma unroll
-          for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[c][g], o[c][d], 0, 0, 0);
+          sc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[n & 1][y], qf[k], sc[e], 0, 0, 0);
         }
+      }
+      kv_bf16x8 vf[2][4];
+#pragma unroll
+      for (int d = 0; d < 4; ++d) vf[0][d] = *reinterpret_cast<const kv_bf16x8*>(vb + d * 1024);
+      KEEP_READS_AHEAD();
+      // score y of step e belongs to token t0[e] + 8 * (y / 4) + 4 * half + y % 4
+      if (EXTRA) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int y = 0; y < 16; ++y) sc[e][y] = kv_extra_score(a.sc, sc[e][y], slope, pos - (t0[e] + y / 4 * 8 + half * 4 + y % 4));
+      }
+      if (!full) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int y = 0; y < 16; ++y)
+            if (!sight.sees(t0[e] + y / 4 * 8 + half * 4 + y % 4, pre)) sc[e][y] = -INFINITY;
+      }
+      float top = sc[0][0];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int y = 0; y < 16; ++y) top = fmaxf(top, sc[e][y]);
+      if (!EXTRA) top *= scale2;
+      if (__any(top > m + 8.f)) {          // the running maximum follows only where weights would pass 2^8: the sums are rescaled seldom
+        const float mn = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), f = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= f;
+      }
+      kv_bf16x8 pf[2][2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int y = 0; y < 16; ++y) pf[e][y / 8][y % 8] = static_cast<__bf16>(__builtin_amdgcn_exp2f(EXTRA ? sc[e][y] - m : fmaf(sc[e][y], scale2, -m)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) l = kv_add8(pf[e / 2][e % 2], l);
+#pragma unroll
+      for (int n = 0; n < DT; ++n) {                   // four of the 4 * DT operands (16 tokens, 32 dims) at a time
+        if (n + 1 < DT) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) vf[(n + 1) & 1][y] = *reinterpret_cast<const kv_bf16x8*>(vb + (4 * (n + 1) + y) * 1024);
+        }
+        KEEP_READS_AHEAD();
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int g = (4 * n + y) / DT, d = (4 * n + y) % DT;
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n & 1][y], pf[g / 2][g % 2], o[d], 0, 0, 0);
+        }
+      }
     }
     __syncthreads();
   }
 
   const bool part = a.splits > 1;
-  float* po[NC];
-  uint16_t* dst[NC];
-  bool mine[NC];
+  l += __shfl_xor(l, 32);
+  const float inv = part ? 1.f : l == 0.f ? 0.f : 1.f / l;
+  uint16_t* dst = a.out + (q.row0 + row) * a.out_stride + static_cast<long long>(head) * DH + half * 4;
+  const long long at = ((static_cast<long long>(split) * a.b.S + s) * a.c.heads + h) * a.cols + col;
+  float* po = a.parts.o + at * DH + half * 4;
+  if (mine) {
+    if (part && half == 0) a.parts.ml[at] = make_float2(m, l);
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    l[c] += __shfl_xor(l[c], 16);
-    l[c] += __shfl_xor(l[c], 32);
-    const float inv = part ? 1.f : l[c] == 0.f ? 0.f : 1.f / l[c];
-    const int col = col0 + c * 16 + r, i = col / a.group, g = col - i * a.group;
-    mine[c] = i < rows;
-    dst[c] = a.out + (q.row0 + i) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + kq * 4;
-    const long long at = ((static_cast<long long>(split) * a.b.S + s) * a.c.heads + h) * a.cols + col;
-    po[c] = a.parts.o + at * DH + kq * 4;
-    if (!mine[c]) continue;
-    if (part && kq == 0) a.parts.ml[at] = make_float2(m[c], l[c]);
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      const kv_f32x4 v = o[c][d] * inv;
-      if (part) {
-        *reinterpret_cast<kv_f32x4*>(po[c] + d * 16) = v;
-      } else {
-        uint32_t w[2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) w[y] = kv_pair(v[2 * y], v[2 * y + 1]);
-        *reinterpret_cast<uint2*>(dst[c] + d * 16) = make_uint2(w[0], w[1]);
+      for (int y = 0; y < 4; ++y) {                    // dims 32 d + 8 y + 4 half ..
+        const float v[4] = {o[d][4 * y] * inv, o[d][4 * y + 1] * inv, o[d][4 * y + 2] * inv, o[d][4 * y + 3] * inv};
+        if (part) *reinterpret_cast<float4*>(po + d * 32 + y * 8) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint2*>(dst + d * 32 + y * 8) = make_uint2(kv_pair(v[0], v[1]), kv_pair(v[2], v[3]));
       }
-    }
   }
 
   // Values that are NaN and that some rows do not see were left out of the products (0 * NaN would reach everybody): the dims of those who see them become NaN.
   if (__syncthreads_or(nan) == 0) return;
   for (int j = 2 * t_begin; j < min(2 * t_end, ks.count); ++j) {
     const int t0 = ks.step(j) * 32, id = table[t0 >> a.c.bt_log2];
-    if (id < 0 || id >= a.c.n_blocks || kv_all_see(t0, p_first, p_last, pre, window)) continue;
-    const uint8_t* v = a.c.v + (static_cast<long long>(id) * a.c.heads + h) * block_bytes + (t0 & ((1 << a.c.bt_log2) - 1)) * DH + lane * 16;
-#pragma unroll 1
-    for (int d = 0; d < DT; ++d) {
-      const uint2 w = *reinterpret_cast<const uint2*>(v + d / 2 * 1024 + d % 2 * 8);
-      const kv_bf16x8 bad = kv_operand(kv_nan_bytes(w.x) * 0x38u, kv_nan_bytes(w.y) * 0x38u, 1.f);      // 1 where the code is NaN
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        kv_bf16x8 sees;
-#pragma unroll
-        for (int y = 0; y < 8; ++y) sees[y] = static_cast<__bf16>(sight[c].sees(t0 + y / 4 * 16 + 4 * kq + y % 4, pre) ? 1.f : 0.f);
-        const kv_f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, sees, kv_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          if (mine[c] && n[y] > 0.f) {
-            if (part) po[c][d * 16 + y] = NAN;
-            else dst[c][d * 16 + y] = 0x7fc0;
-          }
+    if (id < 0 || id >= a.c.n_blocks || wg_all.has(t0)) continue;
+    const uint8_t* v = a.c.v + (static_cast<long long>(id) * a.c.heads + h) * head_bytes + (t0 & ((1 << a.c.bt_log2) - 1)) * DH;
+    for (int tok = 0; tok < 32; ++tok) {
+      const bool sees = mine && sight.sees(t0 + tok, pre);
+      if (!__any(sees)) continue;
+      for (int d = 0; d < DH / 2; ++d) {               // the dims that this lane has written
+        const int dim = d / 4 * 8 + half * 4 + d % 4;
+        if (sees && (v[kv_value_at(tok, dim, DH)] & 0x7f) == 0x7f) {
+          if (part) po[dim - half * 4] = NAN;
+          else dst[dim - half * 4] = 0x7fc0;
+        }
       }
     }
   }
 }
 
 namespace {
-int rows_cols(int dh) { return dh == 256 ? 64 : 128; }
+constexpr int ROWS_COLS = 128;
 struct RowsPlan { long long tiles, wgs; int splits; };
 // Work-groups of a column tile each; where they are less than two to a CU (the bounds of the call say so), its tokens are divided, down to 1024 tokens a part.
 RowsPlan rows_plan(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c) {
   RowsPlan p;
-  p.tiles = (static_cast<long long>(b.T) * (at.n_heads / c.n_heads) + rows_cols(c.head_dim) - 1) / rows_cols(c.head_dim);
+  p.tiles = (static_cast<long long>(b.T) * (at.n_heads / c.n_heads) + ROWS_COLS - 1) / ROWS_COLS;
   const long long sh = static_cast<long long>(b.S) * c.n_heads, tokens = static_cast<long long>(b.table_width) * c.block_tokens;
   const long long want = 512 / (sh * p.tiles), most = tokens / 1024;
   p.splits = static_cast<int>(want < most ? want : most);
@@ -315,7 +315,7 @@ int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_atte
   a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
   a.b = kv_batch_args(b);
   a.c = kv_cache_args(c);
-  a.sc = KvScore{at.slopes, at.prefix, at.scale, at.cap, at.window};
+  a.sc = kv_score(at);
   a.group = at.n_heads / c.n_heads;
   a.cols = b.T * a.group;
   const RowsPlan p = rows_plan(at, b, c);
@@ -325,7 +325,7 @@ int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_atte
   if (p.splits > 1) a.parts = kv_parts(ws, size_t(p.splits) * b.S * c.n_heads * a.cols);
   const int lds = 64 * c.head_dim * 2 * 4;
   const dim3 grid(static_cast<unsigned>(p.wgs)), block(256);
-  const bool extra = at.slopes || at.cap > 0.f || !(at.scale > 0.f);
+  const bool extra = kv_extra(at);
   if (c.head_dim == 256) {
     const void* k = extra ? reinterpret_cast<const void*>(k_kv_attend_rows<256, true>) : reinterpret_cast<const void*>(k_kv_attend_rows<256, false>);
     const int32_t rc = ensure_dynamic_lds(extra ? LDSK_ATTEND_ROWS_EXTRA : LDSK_ATTEND_ROWS, k, lds, "moqe_kv_attention");

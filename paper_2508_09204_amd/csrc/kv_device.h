@@ -24,6 +24,7 @@ struct KvSeq {
 };
 __device__ __forceinline__ KvSeq kv_seq(const KvBatch& b, int s, int bt_log2) {
   KvSeq q;
+  const int len = b.kv_len[s];
   q.row0 = s * b.T;
   q.n = b.T;
   if (b.cu_rows) {
@@ -31,7 +32,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvBatch& b, int s, int bt_log2) {
     q.row0 = min(max(c0, 0), b.M);
     q.n = max(min(max(c1, 0), b.M) - q.row0, 0);
   }
-  q.len = static_cast<int>(min(static_cast<long long>(max(b.kv_len[s], 0)), static_cast<long long>(b.width) << bt_log2));
+  q.len = static_cast<int>(min(static_cast<long long>(max(len, 0)), static_cast<long long>(b.width) << bt_log2));
   return q;
 }
 
@@ -45,8 +46,13 @@ inline KvCache kv_cache_args(const moqe_kv_cache& c) {
 typedef __bf16 kv_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 kv_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float kv_f32x4 __attribute__((ext_vector_type(4)));
+typedef float kv_f32x16 __attribute__((ext_vector_type(16)));
 
-// Eight codes times their scale, exact in bf16: the scale is a power of two and the conversion takes it along.
+// Four and eight codes times their scale, exact in bf16: the scale is a power of two and the conversion takes it along.
+__device__ __forceinline__ uint2 kv_four(uint32_t w, float scale) {
+  return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)));
+}
 __device__ __forceinline__ kv_bf16x8 kv_operand(uint32_t lo, uint32_t hi, float scale) {
   union { kv_bf16x2 p[4]; kv_bf16x8 v; } u;
   u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
@@ -61,17 +67,34 @@ __device__ __forceinline__ uint32_t kv_pair(float lo, float hi) {          // tw
   return uint32_t(__builtin_bit_cast(uint16_t, l)) | uint32_t(__builtin_bit_cast(uint16_t, h)) << 16;
 }
 
+// Adds eight bf16 weights to a sum in fp32, two an instruction.  The sum is of the weights as they multiply the values, so that their rounding partly cancels.
+__device__ __forceinline__ float kv_add8(kv_bf16x8 w, float sum) {
+  union { kv_bf16x8 v; kv_bf16x2 p[4]; } u;
+  u.v = w;
+  const kv_bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2_f32_bf16(u.p[i], ones, sum, false);
+  return sum;
+}
+
 // What turns q . k into the score's base-2 exponent, and who sees what.
 struct KvScore {
   const float* slopes; const int32_t* prefix;
-  float scale, cap;                          // as the caller gave them; cap <= 0: none
+  float scale2;                              // scale * log2 e
+  float cap2, turn;                          // cap * log2 e (0: none), 2 log2 e * scale / cap
   int window;
 };
 constexpr float KV_LOG2E = 1.4426950408889634f;
-
-// cap * tanh(a / cap) as cap * (1 - 2 / (1 + e^(2 a / cap))): its error is some 2^-23 of cap, wherever a lies.
-__device__ __forceinline__ float kv_capped(float a, float cap) {
-  return cap - 2.f * cap / (1.f + exp2f(a * (2.f * KV_LOG2E) / cap));
+inline KvScore kv_score(const moqe_attention& a) {
+  const bool capped = a.cap > 0.f;
+  return KvScore{a.slopes, a.prefix, a.scale * KV_LOG2E, capped ? a.cap * KV_LOG2E : 0.f, capped ? 2.f * KV_LOG2E * a.scale / a.cap : 0.f, a.window};
+}
+// Scores that need more than one multiplication.
+inline bool kv_extra(const moqe_attention& a) { return a.slopes || a.cap > 0.f || !(a.scale > 0.f); }
+// cap * tanh(x / cap) as cap * (1 - 2 / (1 + e^(2 x / cap))), from the product d = q . k: its error is some 2^-22 of cap, wherever x lies.
+__device__ __forceinline__ float kv_extra_score(const KvScore& sc, float d, float slope, int distance) {
+  const float v = sc.cap2 > 0.f ? fmaf(-2.f * sc.cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(d * sc.turn)), sc.cap2) : d * sc.scale2;
+  return v - slope * fabsf(float(distance));
 }
 
 // What a row at position p sees: tokens below `pre` and `span` tokens from `lo` on.
@@ -84,13 +107,13 @@ __device__ __forceinline__ KvSight kv_sight(int p, int len, int window) {
   const int hi = min(len, p + 1), lo = window > 0 ? max(p - window + 1, 0) : 0;
   return KvSight{lo, uint32_t(max(hi - lo, 0))};
 }
-// Whether rows at positions p0 .. p1 all see, or may see any of, the 32 tokens from t0 on.
-__device__ __forceinline__ bool kv_all_see(int t0, int p0, int p1, int pre, int window) {
-  return t0 + 31 < pre || (t0 + 31 <= p0 && (window <= 0 || p1 - t0 < window));
-}
-__device__ __forceinline__ bool kv_some_see(int t0, int p0, int p1, int pre, int window) {
-  return t0 < pre || (t0 <= p1 && (window <= 0 || p0 - (t0 + 31) < window));
-}
+// First tokens t0 of 32-token steps that rows at positions p0 .. p1 see all of, or may see any of.
+struct KvRange {
+  int lo, hi, pre;
+  __device__ __forceinline__ bool has(int t0) const { return (t0 >= lo && t0 < hi) || t0 < pre; }
+};
+__device__ __forceinline__ KvRange kv_all_see(int p0, int p1, int pre, int window) { return KvRange{window > 0 ? p1 - window + 1 : 0, p0 - 30, pre - 31}; }
+__device__ __forceinline__ KvRange kv_some_see(int p0, int p1, int pre, int window) { return KvRange{window > 0 ? p0 - window - 30 : 0, p1 + 1, pre}; }
 
 // Bytes of NaN among four codes, as 1 in their lowest bits.
 __device__ __forceinline__ uint32_t kv_nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7; }
@@ -98,6 +121,13 @@ __device__ __forceinline__ uint32_t kv_nan_bytes(uint4 w) { return kv_nan_bytes(
 __device__ __forceinline__ uint4 kv_without_nan(uint4 w) {
   return make_uint4(w.x & ~(kv_nan_bytes(w.x) * 0xffu), w.y & ~(kv_nan_bytes(w.y) * 0xffu), w.z & ~(kv_nan_bytes(w.z) * 0xffu),
                     w.w & ~(kv_nan_bytes(w.w) * 0xffu));
+}
+
+// A lane's 16 bytes of values (tokens t .. t + 3 and t + 16 .. t + 19 of two dims) with those from token `end` on, which nobody sees, as zeros.
+__device__ __forceinline__ uint4 kv_before(uint4 w, int t, int end) {
+  auto mask = [](int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; };
+  const uint32_t a = mask(end - t), b = mask(end - t - 16);
+  return make_uint4(w.x & a, w.y & b, w.z & a, w.w & b);
 }
 
 // Joins parts of rows: kv_attend_few.hip.
