@@ -320,29 +320,19 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
   }
 }
 
-// Joins parts: a work-group for each column of a sequence and key head.  DH / 4 lanes hold a row; the 1024 / DH such groups of lanes take every so many-th
-// part, and their sums are added in order.  splits 0: the chunks of few_plan; else so many parts of every column.
-struct JoinArgs {
-  FewArgs few;
-  int splits;
-};
+// Joins the chunks: a work-group for each column of a sequence and key head.  DH / 4 lanes hold a row; the 1024 / DH such groups of lanes take every so many-th
+// chunk, and their sums are added in order.
 template <int DH>
-__global__ __launch_bounds__(256) void k_kv_attend_join(JoinArgs ja) {
+__global__ __launch_bounds__(256) void k_kv_attend_join(FewArgs a) {
   constexpr int L = DH / 4, GROUPS = 256 / L;
   __shared__ float4 sums[GROUPS][L];
   __shared__ float lsum[GROUPS];
-  const FewArgs& a = ja.few;
   const int group = threadIdx.x / L, lane = threadIdx.x % L;
   const int h = blockIdx.x % a.c.heads, s = blockIdx.x / a.c.heads / a.cols, col = blockIdx.x / a.c.heads % a.cols;
-  int chunks = ja.splits;
-  long long step = static_cast<long long>(a.b.S) * a.c.heads * a.cols, at = (static_cast<long long>(s) * a.c.heads + h) * a.cols + col;
-  if (ja.splits == 0) {
-    FewPlan pl;
-    if (!few_plan(a, s, false, &pl) || pl.chunks == 1) return;
-    chunks = pl.chunks;
-    step = static_cast<long long>(a.c.heads) * a.cols;
-    at = pl.first * step + static_cast<long long>(h) * a.cols + col;
-  }
+  FewPlan pl;
+  if (!few_plan(a, s, false, &pl) || pl.chunks == 1) return;
+  const int chunks = pl.chunks;
+  const long long step = static_cast<long long>(a.c.heads) * a.cols, at = pl.first * step + static_cast<long long>(h) * a.cols + col;
   const KvSeq q = kv_seq(a.b, s, a.c.bt_log2);
   const int i = col / a.group, g = col - i * a.group;
   if (i >= min(q.n, a.b.T)) return;
@@ -387,21 +377,7 @@ long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c) {          
   const int target = FEW_TARGET_WGS / c.n_heads > 0 ? FEW_TARGET_WGS / c.n_heads : 1;
   return target + static_cast<long long>(b.S);
 }
-void launch_join(const FewArgs& a, int dh, int splits, hipStream_t st) {
-  const JoinArgs ja{a, splits};
-  const dim3 grid(static_cast<unsigned>(static_cast<long long>(a.b.S) * a.c.heads * a.cols)), block(256);
-  if (dh == 64) hipLaunchKernelGGL((k_kv_attend_join<64>), grid, block, 0, st, ja);
-  else if (dh == 128) hipLaunchKernelGGL((k_kv_attend_join<128>), grid, block, 0, st, ja);
-  else hipLaunchKernelGGL((k_kv_attend_join<256>), grid, block, 0, st, ja);
-}
 }  // namespace
-
-void launch_kv_join(const KvParts& parts, const KvBatch& b, const KvCache& c, int dh, int group, int cols, int splits, uint16_t* out, long long out_stride,
-                    hipStream_t st) {
-  FewArgs a{};
-  a.out = out; a.out_stride = out_stride; a.b = b; a.c = c; a.group = group; a.cols = cols; a.parts = parts;
-  launch_join(a, dh, splits, st);
-}
 
 size_t kv_attend_few_ws_bytes(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c) {
   const size_t rows = size_t(few_chunks(b, c)) * c.n_heads * (size_t(b.T) * (at.n_heads / c.n_heads));
@@ -444,7 +420,12 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
     MOQE_FEW(256, 1, 8);
   }
 #undef MOQE_FEW
-  if (chunks) launch_join(a, c.head_dim, 0, st);
+  if (chunks) {
+    const dim3 jgrid(static_cast<unsigned>(static_cast<long long>(b.S) * c.n_heads * a.cols));
+    if (c.head_dim == 64) hipLaunchKernelGGL((k_kv_attend_join<64>), jgrid, dim3(256), 0, st, a);
+    else if (c.head_dim == 128) hipLaunchKernelGGL((k_kv_attend_join<128>), jgrid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_kv_attend_join<256>), jgrid, dim3(256), 0, st, a);
+  }
   return check_launch("kv_attention");
 }
 

@@ -7,14 +7,39 @@ namespace moqe {
 // Other arithmetic may cross.
 #define KEEP_READS_AHEAD() __builtin_amdgcn_sched_barrier(0x406)
 
+constexpr int ROWS_W = 4;                  // waves of a work-group (eight: 880 instead of 905 us for 2 x 2048 rows on 16384 tokens, 109 instead of 100 for 16 prompts of 512)
+
 struct RowsArgs {
   const uint16_t* q; uint16_t* out;
   long long q_stride, out_stride;
   KvBatch b; KvCache c; KvScore sc;
-  int group, tiles, cols;       // query heads to a key head; column tiles, and columns, of a sequence and key head at most
-  int splits;                   // parts that the tokens of every column tile are divided into
-  KvParts parts;                // [split][sequence][key head][column]
+  int group, tiles;             // query heads to a key head; column tiles of a sequence and key head at most
+  int whole, split_tiles, splits;   // of each XCD's column tiles: so many are done by one work-group each, the tokens of the next are divided into `splits` parts
+  KvParts parts;                // [split][split tile][XCD][column of the tile]
 };
+
+// Column tile number x of an XCD (work-groups go round robin over 8).  Sequences and key heads are dealt out to the XCDs, all tiles of one to one XCD, whose L2 then holds their
+// keys and values; the longest tiles go first.  The tiles of what is left over from eights, in a row, are cut into eight equal stretches: within a head every eighth
+// tile comes in turn, so that a stretch that takes a part of a head gets long and short ones.
+struct RowsTile { int s, h, tile; };
+__device__ __forceinline__ bool rows_tile(const RowsArgs& a, int xcd, int x, RowsTile* t) {
+  const int all = a.b.S * a.c.heads, dealt = all / 8 * a.tiles, rest = all % 8 * a.tiles;
+  int sh, rank;                                  // rank: from the longest tile of the head on
+  if (x < dealt) {
+    sh = x / a.tiles * 8 + xcd;
+    rank = x % a.tiles;
+  } else {
+    const int f = static_cast<int>(static_cast<long long>(rest) * xcd / 8) + x - dealt;
+    if (f >= static_cast<int>(static_cast<long long>(rest) * (xcd + 1) / 8)) return false;
+    const int y = f % a.tiles, n = a.tiles / 8, more = a.tiles % 8 * (n + 1);        // the first tiles % 8 of the eight turns have one more
+    sh = all / 8 * 8 + f / a.tiles;
+    rank = y < more ? y % (n + 1) * 8 + y / (n + 1) : (y - more) % n * 8 + a.tiles % 8 + (y - more) / n;
+  }
+  t->s = sh / a.c.heads;
+  t->h = sh % a.c.heads;
+  t->tile = a.tiles - 1 - rank;
+  return true;
+}
 
 // One work-group takes 128 columns (row i, query head g of the key head's group: column i * group + g), 32 for each of its four waves, through the tokens in
 // tiles of 64.  The tile's codes become bf16 operands once, on their way into LDS (two buffers, one barrier a tile; the codes of the tile after next are already
@@ -23,16 +48,17 @@ struct RowsArgs {
 // Scores stay in registers: the layout of S^T = K Q^T is the operand layout of O^T = V^T P^T if 16 tokens of values go 0..3, 8..11 | 4..7, 12..15.
 // EXTRA: scores are capped, biased, or their scale is not positive.
 template <int DH, bool EXTRA>
-__global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsArgs a) {
-  constexpr int COLS = 128, KS = DH / 16, DT = DH / 32, U = DH / 64;           // U: 16-byte units of keys (and of values) a thread brings in
+__global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsArgs a) {
+  constexpr int W = ROWS_W, COLS = W * 32, KS = DH / 16, DT = DH / 32, U = DH / (W * 16);   // U: 16-byte units of keys (and of values) a thread brings in
   constexpr int HALF = 64 * DH * 2;                                            // bytes of a tile's keys in bf16
   extern __shared__ __align__(16) uint8_t lds[];                               // [2][keys, values]
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, kq = lane >> 4, c32 = lane & 31, half = lane >> 5;
-  // work-groups of one sequence and key head stay on one XCD (round robin over 8): its L2 holds their keys and values; the longest tiles go first
   const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-  const int per = a.tiles * a.splits, sh = slot / per * 8 + xcd;
-  if (sh >= a.b.S * a.c.heads) return;
-  const int h = sh % a.c.heads, s = sh / a.c.heads, split = slot % a.splits, tile = a.tiles - 1 - slot % per / a.splits;
+  const bool part = slot >= a.whole;
+  const int x = part ? a.whole + (slot - a.whole) / a.splits : slot, split = part ? (slot - a.whole) % a.splits : 0, splits = part ? a.splits : 1;
+  RowsTile rt;
+  if (!rows_tile(a, xcd, x, &rt)) return;
+  const int s = rt.s, h = rt.h, tile = rt.tile;
   const KvSeq q = kv_seq(a.b, s, a.c.bt_log2);
   const int rows = min(q.n, a.b.T), first_pos = q.first();
   const int i_first = tile * COLS / a.group;
@@ -75,8 +101,8 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsA
   const uint32_t head_bytes = uint32_t(DH) << a.c.bt_log2;
   const int* table = a.b.table + static_cast<long long>(s) * a.b.width;
   const int all_tiles = (ks.count + 1) / 2;
-  const int t_begin = static_cast<int>(static_cast<long long>(all_tiles) * split / a.splits);
-  const int t_end = static_cast<int>(static_cast<long long>(all_tiles) * (split + 1) / a.splits);
+  const int t_begin = static_cast<int>(static_cast<long long>(all_tiles) * split / splits);
+  const int t_end = static_cast<int>(static_cast<long long>(all_tiles) * (split + 1) / splits);
   // lane i looks up step `look + i`: block (-1: absent) and scales
   int look = 2 * t_begin, ids = -1;
   float k_scales = 1.f, v_scales = 1.f;
@@ -95,8 +121,9 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsA
   look_up();
   // A wave's n-th 64 units of a tile: their step, and the place of the first among that step's 2 * DH.
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
-  auto unit_step = [&](int n) { return DH == 64 ? wave_u >> 1 : n * 128 / DH; };
-  auto unit_place = [&](int n) { return DH == 64 ? (wave_u & 1) * 64 : n * 256 % (2 * DH) + wave_u * 64; };
+  constexpr int STEP_U = 2 * DH / 64;                   // waves' worth of units in a step
+  auto unit_step = [&](int n) { return STEP_U >= W ? n * W / STEP_U : n * (W / STEP_U) + wave_u / STEP_U; };
+  auto unit_place = [&](int n) { return STEP_U >= W ? (n * W % STEP_U + wave_u) * 64 : wave_u % STEP_U * 64; };
   // The tile under way: its codes, and of its two steps the scales and the first token (2^30: absent, seen by nobody; any block's codes do for it).
   uint4 kc[U], vc[U];
   float sk[2], sv[2];
@@ -169,6 +196,7 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsA
     }
     const bool some = some_see.has(t0[0]) || some_see.has(t0[1]);
     if (!idle && some) {
+      __builtin_amdgcn_s_setprio(1);       // staging steps back for products and softmax: 2 x 2048 rows on 16384 tokens 961 -> 903 us
       const bool full = all_see.has(t0[0]) && all_see.has(t0[1]);
       const uint8_t* kb = lds + buf * 2 * HALF + lane * 16;
       const uint8_t* vb = kb + HALF;
@@ -244,15 +272,15 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsA
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n & 1][y], pf[g / 2][g % 2], o[d], 0, 0, 0);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
     }
     __syncthreads();
   }
 
-  const bool part = a.splits > 1;
   l += __shfl_xor(l, 32);
   const float inv = part ? 1.f : l == 0.f ? 0.f : 1.f / l;
   uint16_t* dst = a.out + (q.row0 + row) * a.out_stride + static_cast<long long>(head) * DH + half * 4;
-  const long long at = ((static_cast<long long>(split) * a.b.S + s) * a.c.heads + h) * a.cols + col;
+  const long long at = ((static_cast<long long>(split) * a.split_tiles + x - a.whole) * 8 + xcd) * COLS + wave * 32 + c32;
   float* po = a.parts.o + at * DH + half * 4;
   if (mine) {
     if (part && half == 0) a.parts.ml[at] = make_float2(m, l);
@@ -286,26 +314,66 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsA
   }
 }
 
+// Joins the parts of the divided tiles: DH / 4 lanes for each column.
+template <int DH>
+__global__ __launch_bounds__(256) void k_kv_rows_join(RowsArgs a) {
+  constexpr int COLS = ROWS_W * 32, L = DH / 4;
+  const int c = blockIdx.x * (256 / L) + threadIdx.x / L, lane = threadIdx.x % L;      // column among those of all divided tiles
+  const int xcd = c / COLS & 7, ti = c / COLS >> 3;
+  RowsTile rt;
+  if (ti >= a.split_tiles || !rows_tile(a, xcd, a.whole + ti, &rt)) return;
+  const KvSeq q = kv_seq(a.b, rt.s, a.c.bt_log2);
+  const int col = rt.tile * COLS + c % COLS, row = col / a.group, head = rt.h * a.group + col - row * a.group;
+  if (row >= min(q.n, a.b.T)) return;
+  const long long step = static_cast<long long>(a.split_tiles) * 8 * COLS;
+  float m = -3e38f;
+  for (int p = 0; p < a.splits; ++p) m = fmaxf(m, a.parts.ml[c + p * step].x);
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int p = 0; p < a.splits; ++p) {
+    const float2 x = a.parts.ml[c + p * step];
+    const float4 v = *reinterpret_cast<const float4*>(a.parts.o + (c + p * step) * DH + lane * 4);
+    const float f = exp2f(x.x - m);
+    l += x.y * f;
+    o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* dst = a.out + (q.row0 + row) * a.out_stride + static_cast<long long>(head) * DH + lane * 4;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(kv_pair(o.x * inv, o.y * inv), kv_pair(o.z * inv, o.w * inv));
+}
+
 namespace {
-constexpr int ROWS_COLS = 128;
-struct RowsPlan { long long tiles, wgs; int splits; };
-// Work-groups of a column tile each; where they are less than two to a CU (the bounds of the call say so), its tokens are divided, down to 1024 tokens a part.
+struct RowsPlan { long long tiles, whole, split_tiles, wgs; int splits; };
+// An XCD's column tiles (as many as the bounds of the call allow) go over its 32 CUs, two at a time on each.  If 32 or fewer are left over from full rounds of 64, each has
+// a CU to itself, or CUs have none, and that takes 0.68 of the time of two side by side: so the tokens of those tiles are divided into as many parts as fill the 64
+// places, of at least 512 tokens.  2 x T rows of 7 query heads on 14336 tokens and themselves, tiles an XCD, whole / divided (us): 16 tiles
+// 338 / 137, 32 349 / 260, 80 900 / 656, 96 913 / 792.
+// More than 32 left over are not divided: 48 tiles 427 / 462, 112 tiles 942 / 968.
 RowsPlan rows_plan(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c) {
-  RowsPlan p;
-  p.tiles = (static_cast<long long>(b.T) * (at.n_heads / c.n_heads) + ROWS_COLS - 1) / ROWS_COLS;
-  const long long sh = static_cast<long long>(b.S) * c.n_heads, tokens = static_cast<long long>(b.table_width) * c.block_tokens;
-  const long long want = 512 / (sh * p.tiles), most = tokens / 1024;
-  p.splits = static_cast<int>(want < most ? want : most);
-  if (p.splits < 1) p.splits = 1;
-  p.wgs = (sh + 7) / 8 * 8 * p.tiles * p.splits;
+  constexpr int COLS = ROWS_W * 32, CUS = 32;
+  RowsPlan p{};
+  p.tiles = (static_cast<long long>(b.T) * (at.n_heads / c.n_heads) + COLS - 1) / COLS;
+  const long long heads = static_cast<long long>(b.S) * c.n_heads;
+  p.whole = heads / 8 * p.tiles + (heads % 8 * p.tiles + 7) / 8;
+  p.splits = 1;
+  const long long left = p.whole % (2 * CUS), most = static_cast<long long>(b.table_width) * c.block_tokens / 512;
+  if (left > 0 && left <= CUS) {
+    const long long k = 2 * CUS / left < most ? 2 * CUS / left : most;
+    if (k >= 2) {
+      p.splits = static_cast<int>(k < 16 ? k : 16);
+      p.split_tiles = left;
+      p.whole -= left;
+    }
+  }
+  p.wgs = 8 * (p.whole + p.split_tiles * p.splits);
   return p;
 }
+size_t rows_parts(const RowsPlan& p) { return size_t(p.splits) * p.split_tiles * 8 * ROWS_W * 32; }
 }  // namespace
 
 size_t kv_attend_rows_ws_bytes(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c) {
-  const RowsPlan p = rows_plan(at, b, c);
-  if (p.splits == 1) return 0;
-  const size_t rows = size_t(p.splits) * b.S * c.n_heads * (size_t(b.T) * (at.n_heads / c.n_heads));
+  const size_t rows = rows_parts(rows_plan(at, b, c));
   return align256(rows * 8) + align256(rows * c.head_dim * 4);
 }
 
@@ -317,14 +385,15 @@ int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_atte
   a.c = kv_cache_args(c);
   a.sc = kv_score(at);
   a.group = at.n_heads / c.n_heads;
-  a.cols = b.T * a.group;
   const RowsPlan p = rows_plan(at, b, c);
   if (p.wgs >= (1ll << 31)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld work-groups", p.wgs);
   a.tiles = int(p.tiles);
+  a.whole = int(p.whole);
+  a.split_tiles = int(p.split_tiles);
   a.splits = p.splits;
-  if (p.splits > 1) a.parts = kv_parts(ws, size_t(p.splits) * b.S * c.n_heads * a.cols);
+  if (p.split_tiles) a.parts = kv_parts(ws, rows_parts(p));
   const int lds = 64 * c.head_dim * 2 * 4;
-  const dim3 grid(static_cast<unsigned>(p.wgs)), block(256);
+  const dim3 grid(static_cast<unsigned>(p.wgs)), block(ROWS_W * 64);
   const bool extra = kv_extra(at);
   if (c.head_dim == 256) {
     const void* k = extra ? reinterpret_cast<const void*>(k_kv_attend_rows<256, true>) : reinterpret_cast<const void*>(k_kv_attend_rows<256, false>);
@@ -341,7 +410,12 @@ int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_atte
   else if (c.head_dim == 128) MOQE_ROWS(128);
   else MOQE_ROWS(256);
 #undef MOQE_ROWS
-  if (p.splits > 1) launch_kv_join(a.parts, a.b, a.c, c.head_dim, a.group, a.cols, p.splits, a.out, out_stride, st);
+  if (p.split_tiles) {
+    const dim3 jgrid(static_cast<unsigned>(p.split_tiles * 8 * ROWS_W * 32 * (c.head_dim / 4) / 256));
+    if (c.head_dim == 64) hipLaunchKernelGGL((k_kv_rows_join<64>), jgrid, dim3(256), 0, st, a);
+    else if (c.head_dim == 128) hipLaunchKernelGGL((k_kv_rows_join<128>), jgrid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_kv_rows_join<256>), jgrid, dim3(256), 0, st, a);
+  }
   return check_launch("kv_attention");
 }
 

@@ -130,14 +130,12 @@ __device__ __forceinline__ uint4 kv_before(uint4 w, int t, int end) {
   return make_uint4(w.x & a, w.y & b, w.z & a, w.w & b);
 }
 
-// Joins parts of rows: kv_attend_few.hip.
+// Parts of rows, to be joined.
 struct KvParts {
-  float2* ml; float* o;         // [part][..][column] maximum and sum, [..][head_dim] rows that are not divided by the sum; NULL: there is one part
+  float2* ml; float* o;         // [part][..] maximum and sum, [..][head_dim] rows that are not divided by the sum; NULL: there is one part
 };
 inline KvParts kv_parts(void* ws, size_t rows) {
   return KvParts{static_cast<float2*>(ws), reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(rows * 8))};
 }
-void launch_kv_join(const KvParts& parts, const KvBatch& b, const KvCache& c, int dh, int group, int cols, int splits, uint16_t* out, long long out_stride,
-                    hipStream_t st);
 
 }  // namespace moqe

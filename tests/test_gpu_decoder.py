@@ -351,6 +351,19 @@ def test_attention_masks(i, rows):
     _check_attention(rows, [90, 333, 150], 8, 2, 64 if i % 2 else 128, 32, seed=300 + i, **MASKS[i])
 
 
+LONG = [  # contexts so long that the tokens of a column tile are divided over work-groups
+    dict(rows=[70], lens=[3000], heads=2, kv=1, dh=128, bt=64), dict(rows=[100, 30], lens=[2500, 6000], heads=4, kv=2, dh=64, bt=32),
+    dict(rows=[17, 0, 90], lens=[5000, 100, 95], heads=8, kv=2, dh=256, bt=128), dict(rows=[100, 70], lens=[4000, 1500], heads=3, kv=1, dh=128, bt=64, window=700, prefix=[90, 1200]),
+    dict(rows=[66], lens=[2100], heads=2, kv=2, dh=64, bt=64, cap=9.0, slopes=True), dict(rows=[80, 80], lens=[3000, 1100], heads=2, kv=1, dh=128, bt=128, absent=[(0, 3), (0, 23), (1, 8)]),
+    dict(rows=[130], lens=[2049], heads=5, kv=1, dh=128, bt=32, window=3),
+]
+
+
+@pytest.mark.parametrize("i", range(len(LONG)))
+def test_attention_many_rows_on_long_contexts(i):
+    _check_attention(seed=700 + i, **LONG[i])
+
+
 @pytest.mark.parametrize("rows", [[1, 1, 1], [80, 80, 80]])
 def test_attention_absent_blocks(rows):
     """Blocks given back are not seen; a sequence that has none gives zeros, also where the window leaves it only absent ones."""
@@ -371,16 +384,16 @@ def test_attention_of_many_sequences(rows):
     _check_attention([1 + (s * 7) % rows for s in range(n)], [1 + (s * 37) % 400 + rows for s in range(n)], 2, 1, 64, 32, seed=600)
 
 
-@pytest.mark.parametrize("rows,window", [([1], 100), ([4], 0), ([90], 0), ([90], 30)])
-def test_nan_in_the_cache_reaches_those_who_see_it(rows, window):
-    """Token 150 of 180 is NaN in one dim of its values, token 100 in one of its keys: only rows that see them have NaN, in the dims concerned."""
+@pytest.mark.parametrize("rows,window,L", [([1], 100, 180), ([4], 0, 180), ([90], 0, 180), ([90], 30, 180), ([90], 0, 2100), ([3], 0, 2100)])
+def test_nan_in_the_cache_reaches_those_who_see_it(rows, window, L):
+    """The 30th token from the end is NaN in one dim of its values, the 80th in one of its keys: only rows that see them have NaN, in the dims concerned."""
     rng = np.random.default_rng(9)
-    dh, bt, L, H = 64, 32, 180, 2
-    lens = [L if rows[0] > 1 else 149 + 1]
+    dh, bt, H = 64, 32, 2
+    lens = [L if rows[0] > 1 else L - 30]
     for bad_key in (False, True):
         table, n_blocks = _lay_out(rng, [L], bt)
         cache = _random_cache(rng, n_blocks, H, bt, dh)
-        tok, dim = (100, 3) if bad_key else (150, 40)
+        tok, dim = (L - 80, 3) if bad_key else (L - 30, 40)
         which = "k" if bad_key else "v"
         cache.codes(which)[table[0, tok // bt], 1][cache.at[which][tok % bt, dim]] = 0x7f
         batch, seqs, T = _batch(table, lens, rows)
