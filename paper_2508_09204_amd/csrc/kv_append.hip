@@ -10,239 +10,378 @@ struct AppendArgs {
   const double* inv_freq; const float *q_gain, *k_gain;
   float eps, mscale;
   int heads, rot, inter;
-  int seq_blocks;               // blocks that a sequence of T rows can touch
+  int seq_blocks;               // cache part: blocks that a sequence of T rows can touch, ...
+  int key_groups, group_heads;  // ... key heads in groups that a work-group goes through
   int row_tiles, rows_log2;     // query part: tiles of 2^rows_log2 rows of a sequence, ...
   int splits, split_heads;      // ... its heads in parts
 };
 
-// A slot is two 8-dim pieces of a head vector that hold whole pairs: (j, j + rot/2) pieces in the half layout, neighbours otherwise.
-template <int DH>
+// Rows are taken in pieces of 16 bytes: PIECE values.  A slot is two pieces of a head vector that hold whole pairs of the rotation; a head's DH / (2 PIECE) slots
+// lie in neighbouring lanes, so that a load of first (second) pieces covers a stretch of memory without holes.
+template <bool BF16> constexpr int PIECE = BF16 ? 8 : 4;
+template <int DH, bool BF16> constexpr int SLOTS = DH / (2 * PIECE<BF16>);
+
+template <int DH, bool BF16>
 __device__ __forceinline__ void slot_dims(const AppendArgs& a, int slot, int* da, int* db) {
-  const bool halves = !a.inter && slot * 16 < a.rot;
-  *da = halves ? slot * 8 : slot * 16;
-  *db = halves ? slot * 8 + a.rot / 2 : slot * 16 + 8;
-}
-
-// cos and sin of the slot's eight angles at position p.  They are reduced to a fraction of a turn in 64 bits, where 32 would lose 2^-24 of p * inv_freq; what the
-// fraction loses when it is rounded to 32 comes back to first order: without that, keys that lie between two codes took the wrong one more than twice as often.
-__device__ __forceinline__ void slot_angles(const AppendArgs& a, int slot, int p, float* cs, float* sn) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    double turns = double(p) * (a.inv_freq[slot * 8 + i] * 0.15915494309189535);
-    turns -= rint(turns);
-    const float hi = float(turns), lo = float(turns - double(hi)) * 6.2831853f;
-    float s, c;
-    sincospif(2.f * hi, &s, &c);
-    cs[i] = a.mscale * fmaf(-lo, s, c);
-    sn[i] = a.mscale * fmaf(lo, c, s);
-  }
-}
-
-__device__ __forceinline__ void turn(bool inter, const float* cs, const float* sn, float* x) {
-  if (inter) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float u = x[2 * i], v = x[2 * i + 1];
-      x[2 * i] = u * cs[i] - v * sn[i];
-      x[2 * i + 1] = v * cs[i] + u * sn[i];
-    }
+  constexpr int P = PIECE<BF16>;
+  if (a.inter || a.rot == DH) {                 // pairs within pieces, or of pieces half a head apart
+    *da = slot * P;
+    *db = slot * P + DH / 2;
+  } else if (slot * 2 * P < a.rot) {            // pairs of pieces rot / 2 apart
+    *da = slot * P;
+    *db = slot * P + a.rot / 2;
   } else {
+    *da = slot * 2 * P;
+    *db = slot * 2 * P + P;
+  }
+}
+
+// cos and sin of angle number j at position p.  It is reduced to a fraction of a turn in 64 bits, where 32 would lose 2^-24 of p * inv_freq; what the fraction loses when it
+// is rounded to 32 comes back to first order: without that, the keys' codes had more than half as much error again as those of exact angles rounded to 32 bits.
+__device__ __forceinline__ void angle(const AppendArgs& a, int j, int p, float* cs, float* sn) {
+  double turns = double(p) * (a.inv_freq[j] * 0.15915494309189535);
+  turns -= rint(turns);
+  const float hi = float(turns), lo = float(turns - double(hi)) * 6.2831853f;
+  float s, c;
+  sincospif(2.f * hi, &s, &c);
+  *cs = a.mscale * fmaf(-lo, s, c);
+  *sn = a.mscale * fmaf(lo, c, s);
+}
+template <int P>
+__device__ __forceinline__ void slot_angles(const AppendArgs& a, int da, int db, int p, float* cs, float* sn) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float u = x[i], v = x[8 + i];
-      x[i] = u * cs[i] - v * sn[i];
-      x[8 + i] = v * cs[i] + u * sn[i];
+  for (int i = 0; i < P; ++i) {
+    const bool second = a.inter && i >= P / 2;
+    const int dim = a.inter ? (second ? db : da) + 2 * (i % (P / 2)) : da + i;
+    cs[i] = 1.f;
+    sn[i] = 0.f;
+    if (dim < (a.inter ? a.rot : a.rot / 2)) angle(a, a.inter ? dim / 2 : dim, p, &cs[i], &sn[i]);
+    __builtin_amdgcn_sched_barrier(0);           // one after the other: side by side they would take the registers of two more waves
+  }
+}
+
+template <int P>
+__device__ __forceinline__ void turn(bool inter, const float* cs, const float* sn, float* x) {
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int s = i, t = P + i;                                       // half layout
+    const int u = i / (P / 2) * P + 2 * (i % (P / 2));                // neighbours
+    if (inter) {
+      const float e = x[u], f = x[u + 1];
+      x[u] = e * cs[i] - f * sn[i];
+      x[u + 1] = f * cs[i] + e * sn[i];
+    } else {
+      const float e = x[s], f = x[t];
+      x[s] = e * cs[i] - f * sn[i];
+      x[t] = f * cs[i] + e * sn[i];
     }
   }
 }
 
-template <bool BF16> struct Piece;         // eight values as they lie in memory
-template <> struct Piece<true> { uint4 q; };
-template <> struct Piece<false> { float4 a, b; };
-__device__ __forceinline__ void load_piece(const void* base, long long at, Piece<true>* p) {
-  p->q = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
+template <bool BF16>
+__device__ __forceinline__ uint4 load_piece(const void* base, long long at) {
+  return *reinterpret_cast<const uint4*>(static_cast<const char*>(base) + at * (BF16 ? 2 : 4));
 }
-__device__ __forceinline__ void load_piece(const void* base, long long at, Piece<false>* p) {
-  const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
-  p->a = f[0];
-  p->b = f[1];
-}
-__device__ __forceinline__ void piece_values(const Piece<true>& p, float* x) {
-  const uint32_t w[4] = {p.q.x, p.q.y, p.q.z, p.q.w};
+template <bool BF16>
+__device__ __forceinline__ void piece_values(const uint4& p, float* x) {
+  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-__device__ __forceinline__ void piece_values(const Piece<false>& p, float* x) {
-  x[0] = p.a.x; x[1] = p.a.y; x[2] = p.a.z; x[3] = p.a.w; x[4] = p.b.x; x[5] = p.b.y; x[6] = p.b.z; x[7] = p.b.w;
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+      x[i] = __uint_as_float(w[i]);
+    }
+  }
 }
 
-// RMS norm of a head vector whose DH / 16 slots lie in neighbouring lanes.
-template <int DH>
+// RMS norm of a head vector whose slots lie in neighbouring lanes.
+template <int DH, bool BF16>
 __device__ __forceinline__ void head_norm(const float* gain, float eps, int da, int db, float* x) {
+  constexpr int P = PIECE<BF16>;
   float q = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) q += x[i] * x[i];
+  for (int i = 0; i < 2 * P; ++i) q += x[i] * x[i];
 #pragma unroll
-  for (int d = 1; d < DH / 16; d *= 2) q += __shfl_xor(q, d);
+  for (int d = 1; d < SLOTS<DH, BF16>; d *= 2) q += __shfl_xor(q, d);
   const float inv = 1.f / sqrtf(q / float(DH) + eps);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < P; ++i) {
     x[i] *= inv * gain[da + i];
-    x[8 + i] *= inv * gain[db + i];
+    x[P + i] *= inv * gain[db + i];
   }
 }
 
-__device__ __forceinline__ uint32_t codes4(const float* x, float inv) {      // to nearest even; NaN stays, past 464 gets NaN
-  uint32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
-  return __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, w, true);
+// Codes of x / scale for a power of two, to nearest even; NaN stays, past 464 gets NaN.
+__device__ __forceinline__ uint32_t codes4(const float* x, float scale) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  s16x2 w = {0, 0};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[0], x[1], scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[2], x[3], scale, true);
+  return __builtin_bit_cast(uint32_t, w);
 }
 __device__ __forceinline__ uint32_t rescaled4(uint32_t w, float by) {
-  const float x[4] = {__builtin_amdgcn_cvt_f32_fp8(w, 0), __builtin_amdgcn_cvt_f32_fp8(w, 1), __builtin_amdgcn_cvt_f32_fp8(w, 2),
-                      __builtin_amdgcn_cvt_f32_fp8(w, 3)};
-  return codes4(x, by);
+  const float x[4] = {__builtin_amdgcn_cvt_f32_fp8(w, 0) * by, __builtin_amdgcn_cvt_f32_fp8(w, 1) * by, __builtin_amdgcn_cvt_f32_fp8(w, 2) * by,
+                      __builtin_amdgcn_cvt_f32_fp8(w, 3) * by};
+  return codes4(x, 1.f);
 }
-// Keys (VALUES false) or values of one block and head: the new tokens lo .. hi of block `blk` of the sequence, which lies in cache block `id`.
-template <int DH, bool BF16, bool VALUES>
-__device__ __forceinline__ void append_block(const AppendArgs& a, const KvSeq& q, int head, int blk, int id, int lo, int hi, uint8_t* lds, uint32_t* wave_max) {
-  constexpr int SL = DH / 16, NS = 2;
-  const int bt = 1 << a.c.bt_log2, first = blk << a.c.bt_log2;
-  const int slots = (hi - lo) * SL, tid = threadIdx.x, th = blockDim.x;
-  const bool held = lo > first;
-  const long long bh = static_cast<long long>(id) * a.c.heads + head;
-  uint8_t* codes = (VALUES ? a.c.v : a.c.k) + bh * (static_cast<long long>(DH) << a.c.bt_log2);
-  float* scale = (VALUES ? a.c.v_scale : a.c.k_scale) + bh;
-  const float old = held ? *scale : 0.f;
-  const long long col = (a.heads + head + (VALUES ? a.c.heads : 0)) * DH;
 
-  Piece<BF16> pa[NS], pb[NS];
-  int da, db;
-  slot_dims<DH>(a, tid % SL, &da, &db);
-  if (VALUES) { da = tid % SL * 16; db = da + 8; }
+// The codes of the tokens before `lo` of a block and head (first token `first`) move to a scale that is 1 / by times as large.
+template <int DH>
+__device__ __forceinline__ void rescale_block(uint8_t* codes, bool values, int bt, int first, int lo, float by) {
+  for (int u = threadIdx.x; u < bt * DH / 16; u += blockDim.x) {
+    // values: dword j of a unit is tokens t0 + 16 (j & 1) + 0 .. 3; keys: all of a unit is one token
+    const int t0 = values ? first + u / (2 * DH) * 32 + u % 64 / 16 * 4 : first + u / DH * 16 + u % 16;
+    if (t0 >= lo) continue;
+    uint4* p = reinterpret_cast<uint4*>(codes) + u;
+    uint4 w = *p;
+    uint32_t* d = &w.x;
 #pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    const int u = n * th + tid;
-    if (u < slots) {
-      const long long at = (q.row0 + (lo + u / SL - q.first())) * a.qkv_stride + col;
-      load_piece(a.qkv, at + da, &pa[n]);
-      load_piece(a.qkv, at + db, &pb[n]);
+    for (int j = 0; j < 4; ++j) {
+      const int left = values ? lo - (t0 + 16 * (j & 1)) : 4;
+      const uint32_t keep = left >= 4 ? 0u : left <= 0 ? ~0u : ~0u << (8 * left);
+      d[j] = (rescaled4(d[j], by) & ~keep) | (d[j] & keep);
     }
+    *p = w;
   }
-  float x[NS][16];
-  uint32_t top = 0;
-  bool infinite = false;
+}
+
+// What the threads of a work-group find out about one block and head: the new scale, and what earlier codes have to be multiplied with (1: nothing).  top: the largest
+// finite |x| of the thread.
+struct BlockScale { float scale, by; };
+__device__ __forceinline__ BlockScale block_scale(float top, bool held, float old, float* at, float* wave_max) {
 #pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    const int u = n * th + tid;
-    if (u < slots) {
-      piece_values(pa[n], x[n]);
-      piece_values(pb[n], x[n] + 8);
-      if (!VALUES) {
-        if (a.k_gain) head_norm<DH>(a.k_gain, a.eps, da, db, x[n]);        // whole head vectors are in or out: their slots share u / SL
-        if (tid % SL * 16 < a.rot) {
-          float cs[8], sn[8];
-          slot_angles(a, tid % SL, lo + u / SL, cs, sn);
-          turn(a.inter, cs, sn, x[n]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t bits = __float_as_uint(x[n][i]) & 0x7fffffffu;
-        top = max(top, bits < 0x7f800000u ? bits : 0u);
-        infinite |= bits == 0x7f800000u;
-      }
-    }
-  }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) top = max(top, uint32_t(__shfl_xor(int(top), d)));
-  if ((tid & 63) == 0) wave_max[tid >> 6] = top;
+  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = top;
   __syncthreads();                               // also: everybody has read the old scale
-  for (int w = 0; w < th / 64; ++w) top = max(top, wave_max[w]);
-  const float need = __uint_as_float(uint32_t(kv_scale_exponent(top) + 127) << 23);
-  const float s = held && !(old < need) ? old : need;
-  const float inv = 1.f / s;                     // a power of two: exact
-  if (tid == 0) *scale = s;
-  if (infinite) {                                // the conversion would make NaN of them
+  for (int w = 0; w < int(blockDim.x) / 64; ++w) top = fmaxf(top, wave_max[w]);
+  const float need = __uint_as_float(uint32_t(kv_scale_exponent(__float_as_uint(top)) + 127) << 23);
+  BlockScale s;
+  s.scale = held && !(old < need) ? old : need;
+  s.by = held && s.scale > old ? old * (1.f / s.scale) : 1.f;
+  if (threadIdx.x == 0) *at = s.scale;
+  return s;
+}
+// The largest finite |x| (NaN is passed over), and whether any is infinite: the conversion would make NaN of those.
+template <int N>
+__device__ __forceinline__ void largest(const float (&x)[N], float* top, bool* infinite) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(x[i]));
+  if (m == INFINITY) {
+    *infinite = true;
+    m = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (fabsf(x[i]) < INFINITY) m = fmaxf(m, fabsf(x[i]));
+  }
+  *top = fmaxf(*top, m);
+}
+template <int N>
+__device__ __forceinline__ void no_infinities(float (&x)[N], bool infinite, float scale) {
+  if (!infinite) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (fabsf(x[i]) == INFINITY) x[i] = copysignf(448.f * scale, x[i]);
+}
+
+// A block of a sequence that a call writes to: its new tokens lo .. hi, its first token, its place in the cache.
+struct BlockTokens {
+  int lo, hi, first, id;
+  long long row;                // of token lo
+  bool held;                    // it held earlier tokens
+};
+__device__ __forceinline__ bool block_tokens(const AppendArgs& a, int s, int n, BlockTokens* b) {
+  const KvSeq q = kv_seq(a.b, s, a.c.bt_log2);
+  const int p0 = max(q.first(), 0), end = min(q.len, q.first() + min(q.n, a.b.T));
+  const int blk = (p0 >> a.c.bt_log2) + n;
+  b->first = blk << a.c.bt_log2;
+  b->lo = max(p0, b->first);
+  b->hi = min(end, b->first + (1 << a.c.bt_log2));
+  if (b->lo >= b->hi) return false;
+  b->id = a.b.table[static_cast<long long>(s) * a.b.width + blk];
+  b->row = q.row0 + (b->lo - q.first());
+  b->held = b->lo > b->first;
+  return b->id >= 0 && b->id < a.c.n_blocks;
+}
+
+// Keys of one block for some heads in turn.  A thread has 32 values in slots, the same tokens and dims for every head, so that it works out its angles once for all of them.
+template <int DH, bool BF16>
+__device__ __forceinline__ void append_keys(const AppendArgs& a, const BlockTokens& b, int head0, int head1, float (*wave_max)[16]) {
+  constexpr int P = PIECE<BF16>, SL = SLOTS<DH, BF16>, NS = 16 / P;
+  const int slots = (b.hi - b.lo) * SL, tid = threadIdx.x, th = blockDim.x;
+  int da, db;
+  slot_dims<DH, BF16>(a, tid % SL, &da, &db);
+  uint4 pa[NS], pb[NS];
+  auto load = [&](int head) {
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      const int u = n * th + tid;
+      if (u < slots) {
+        const long long at = (b.row + u / SL) * a.qkv_stride + static_cast<long long>(a.heads + head) * DH;
+        pa[n] = load_piece<BF16>(a.qkv, at + da);
+        pb[n] = load_piece<BF16>(a.qkv, at + db);
+      }
+    }
+  };
+  load(head0);
+  float cs[NS][P], sn[NS][P];
+  if (a.rot > 0) {
 #pragma unroll
     for (int n = 0; n < NS; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (fabsf(x[n][i]) == INFINITY) x[n][i] = copysignf(448.f * s, x[n][i]);
+      if (n * th + tid < slots) slot_angles<P>(a, da, db, b.lo + (n * th + tid) / SL, cs[n], sn[n]);
   }
-
-  if (held && s > old) {                         // the codes of earlier tokens move to the new scale
-    const float by = old * inv;
-    for (int u = tid; u < bt * DH / 16; u += th) {
-      uint4* p = reinterpret_cast<uint4*>(codes) + u;
-      uint4 w = *p;
-      uint32_t* d = reinterpret_cast<uint32_t*>(&w);
-      if (VALUES) {
-        const int t0 = first + u / (2 * DH) * 32 + u % 64 / 16 * 4;               // dword j of a unit: tokens t0 + 16 (j & 1) + 0 .. 3
-        if (t0 >= lo) continue;
+  for (int head = head0; head < head1; ++head) {
+    const long long bh = static_cast<long long>(b.id) * a.c.heads + head;
+    uint8_t* codes = a.c.k + bh * (static_cast<long long>(DH) << a.c.bt_log2);
+    const float old = b.held ? a.c.k_scale[bh] : 0.f;
+    float x[NS][2 * P];
+    float top = 0.f;
+    bool infinite = false;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int left = lo - (t0 + 16 * (j & 1));
-          const uint32_t keep = left >= 4 ? 0u : left <= 0 ? ~0u : ~0u << (8 * left);
-          d[j] = (rescaled4(d[j], by) & ~keep) | (d[j] & keep);
-        }
-      } else {
-        if (first + u / DH * 16 + u % 16 >= lo) continue;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d[j] = rescaled4(d[j], by);
+    for (int n = 0; n < NS; ++n) {
+      if (n * th + tid < slots) {
+        piece_values<BF16>(pa[n], x[n]);
+        piece_values<BF16>(pb[n], x[n] + P);
+        if (a.k_gain) head_norm<DH, BF16>(a.k_gain, a.eps, da, db, x[n]);        // a head vector's slots are all in or all out
+        if (a.rot > 0) turn<P>(a.inter, cs[n], sn[n], x[n]);
+        largest(x[n], &top, &infinite);
       }
-      *p = w;
     }
+    if (head + 1 < head1) load(head + 1);
+    const BlockScale s = block_scale(top, b.held, old, a.c.k_scale + bh, wave_max[(head - head0) & 1]);
+    if (s.by != 1.f) {
+      rescale_block<DH>(codes, false, 1 << a.c.bt_log2, b.first, b.lo, s.by);
+      __syncthreads();                           // before parts of the same units are written
+    }
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      const int u = n * th + tid;
+      if (u >= slots) continue;
+      no_infinities(x[n], infinite, s.scale);
+      const uint32_t t = uint32_t(b.lo - b.first + u / SL);
+      uint8_t* ka = codes + kv_key_at(t, uint32_t(da), DH);
+      uint8_t* kb = codes + kv_key_at(t, uint32_t(db), DH);
+      if constexpr (BF16) {
+        *reinterpret_cast<uint2*>(ka) = make_uint2(codes4(x[n], s.scale), codes4(x[n] + 4, s.scale));
+        *reinterpret_cast<uint2*>(kb) = make_uint2(codes4(x[n] + 8, s.scale), codes4(x[n] + 12, s.scale));
+      } else {
+        *reinterpret_cast<uint32_t*>(ka) = codes4(x[n], s.scale);
+        *reinterpret_cast<uint32_t*>(kb) = codes4(x[n] + 4, s.scale);
+      }
+    }
+  }
+}
+
+// Values of one block and head.  Their codes lie four tokens to a dword.  Where all 32 tokens of a group are new, a thread takes a piece of four rows and writes whole dwords,
+// through LDS; the tokens of other groups go byte by byte.
+template <int DH, bool BF16>
+__device__ __forceinline__ void append_values(const AppendArgs& a, const BlockTokens& b, int head, uint32_t* lds, float* wave_max) {
+  constexpr int P = PIECE<BF16>, PCS = DH / P, NQ = BF16 ? 1 : 2;
+  const int tid = threadIdx.x, th = blockDim.x;
+  const long long bh = static_cast<long long>(b.id) * a.c.heads + head;
+  uint8_t* codes = a.c.v + bh * (static_cast<long long>(DH) << a.c.bt_log2);
+  const long long col = static_cast<long long>(a.heads + a.c.heads + head) * DH;
+  // groups g_lo .. g_hi are new altogether, the other new tokens are `before` from lo on and those from `behind` on
+  const int g_lo = (b.lo - b.first + 31) / 32, g_hi = (b.hi - b.first) / 32;
+  const bool whole = g_hi > g_lo;
+  const int quads = whole ? (g_hi - g_lo) * 8 * PCS : 0;
+  const int before = whole ? b.first + 32 * g_lo - b.lo : b.hi - b.lo, behind = whole ? b.first + 32 * g_hi : b.hi;
+  const int rest = (before + b.hi - behind) * PCS;
+  auto rest_token = [&](int u) { const int v = u / PCS; return v < before ? b.lo + v : behind + v - before; };
+  auto rest_piece = [&](int u) { return load_piece<BF16>(a.qkv, (b.row + rest_token(u) - b.lo) * a.qkv_stride + col + u % PCS * P); };
+  uint4 vq[NQ][4], vr;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int u = n * th + tid;
+    if (u < quads) {
+      const long long at = (b.row + b.first + 32 * g_lo + u / PCS * 4 - b.lo) * a.qkv_stride + col + u % PCS * P;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) vq[n][t] = load_piece<BF16>(a.qkv, at + t * a.qkv_stride);
+    }
+  }
+  if (tid < rest) vr = rest_piece(tid);
+  const float old = b.held ? a.c.v_scale[bh] : 0.f;
+  float top = 0.f;
+  bool infinite = false;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    if (n * th + tid < quads) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        float x[P];
+        piece_values<BF16>(vq[n][t], x);
+        largest(x, &top, &infinite);
+      }
+    }
+  }
+  for (int u = tid; u < rest; u += th) {
+    float x[P];
+    piece_values<BF16>(u == tid ? vr : rest_piece(u), x);
+    largest(x, &top, &infinite);
+  }
+  const BlockScale s = block_scale(top, b.held, old, a.c.v_scale + bh, wave_max);
+  if (s.by != 1.f) {
+    rescale_block<DH>(codes, true, 1 << a.c.bt_log2, b.first, b.lo, s.by);
     __syncthreads();                             // before single bytes of the same units are written
   }
-
-  // values of groups of 32 tokens that are new altogether are put in order in LDS, others go byte by byte
-  const int g_lo = (lo - first + 31) / 32, g_hi = (hi - first) / 32;
 #pragma unroll
-  for (int n = 0; n < NS; ++n) {
+  for (int n = 0; n < NQ; ++n) {
     const int u = n * th + tid;
-    if (u >= slots) continue;
-    const uint32_t w[4] = {codes4(x[n], inv), codes4(x[n] + 4, inv), codes4(x[n] + 8, inv), codes4(x[n] + 12, inv)};
-    const uint32_t t = uint32_t(lo - first + u / SL);
-    if (VALUES) {
-      const bool whole = int(t) / 32 >= g_lo && int(t) / 32 < g_hi;
+    if (u < quads) {
+      uint32_t* to = lds + kv_value_at(uint32_t(32 * g_lo + u / PCS * 4), uint32_t(u % PCS * P), DH) / 4;
+      float x[4][P];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t at = kv_value_at(t, uint32_t(da + i), DH);
-        const uint8_t c = uint8_t(w[i / 4] >> (8 * (i % 4)));
-        if (whole) lds[at] = c;
-        else codes[at] = c;
+      for (int t = 0; t < 4; ++t) {
+        piece_values<BF16>(vq[n][t], x[t]);
+        no_infinities(x[t], infinite, s.scale);
       }
-    } else {
-      *reinterpret_cast<uint2*>(codes + kv_key_at(t, uint32_t(da), DH)) = make_uint2(w[0], w[1]);
-      *reinterpret_cast<uint2*>(codes + kv_key_at(t, uint32_t(db), DH)) = make_uint2(w[2], w[3]);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {              // neighbouring dims of 16 lie 16 bytes apart
+        const float y[4] = {x[0][i], x[1][i], x[2][i], x[3][i]};
+        to[4 * i] = codes4(y, s.scale);
+      }
     }
   }
-  if (VALUES && g_hi > g_lo) {
+  for (int u = tid; u < rest; u += th) {
+    float x[P];
+    piece_values<BF16>(u == tid ? vr : rest_piece(u), x);
+    no_infinities(x, infinite, s.scale);
+    uint8_t* to = codes + kv_value_at(uint32_t(rest_token(u) - b.first), uint32_t(u % PCS * P), DH);
+#pragma unroll
+    for (int i = 0; i < P; i += 4) {
+      const uint32_t w = codes4(x + i, s.scale);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) to[16 * (i + t)] = uint8_t(w >> (8 * t));
+    }
+  }
+  if (whole) {
     __syncthreads();
     for (int u = g_lo * 2 * DH + tid; u < g_hi * 2 * DH; u += th) reinterpret_cast<uint4*>(codes)[u] = reinterpret_cast<const uint4*>(lds)[u];
   }
 }
 
-// Work-groups of the cache part (one for each block a sequence can touch and key head), then of the query part (a row tile and some heads each).
-template <int DH, bool BF16>
-__global__ __launch_bounds__(1024) void k_kv_append(AppendArgs a) {
-  extern __shared__ uint8_t lds[];
-  __shared__ uint32_t wave_max[2][16];
-  constexpr int SL = DH / 16;
+// Work-groups of the keys (one for each block a sequence can touch and group of heads), of the values (one for each block and head), then of the queries (a row tile
+// and some heads each).  At most TH threads: 1024 for blocks of 128 tokens of 256 dims, whose work-groups have to do with 128 registers.
+// Bound by memory: 16 prompts of 512 tokens with 32 heads of 128 (336 MB) 74 us,
+// rows of mixed lengths in fp32 with 28 (475 MB) 103 us, where a copy of as many bytes takes 68 and 96.
+template <int DH, bool BF16, int TH>
+__global__ __launch_bounds__(TH, TH > 512 ? 1 : BF16 ? 4 : 3) void k_kv_append(AppendArgs a) {
+  extern __shared__ __align__(16) uint32_t lds[];
+  __shared__ float wave_max[2][16];
+  constexpr int P = PIECE<BF16>, SL = SLOTS<DH, BF16>;
   const int tid = threadIdx.x;
   int w = blockIdx.x;
-  const int cache_wgs = a.b.S * a.seq_blocks * a.c.heads;
+  const int key_wgs = a.b.S * a.seq_blocks * a.key_groups, cache_wgs = key_wgs + a.b.S * a.seq_blocks * a.c.heads;
   if (w < cache_wgs) {
-    const int head = w % a.c.heads, s = w / a.c.heads / a.seq_blocks;
-    const KvSeq q = kv_seq(a.b, s, a.c.bt_log2);
-    const int p0 = max(q.first(), 0), end = min(q.len, q.first() + min(q.n, a.b.T));
-    const int blk = (p0 >> a.c.bt_log2) + w / a.c.heads % a.seq_blocks, first = blk << a.c.bt_log2;
-    if (first >= end) return;
-    const int id = a.b.table[static_cast<long long>(s) * a.b.width + blk];
-    if (id < 0 || id >= a.c.n_blocks) return;
-    const int lo = max(p0, first), hi = min(end, first + (1 << a.c.bt_log2));
-    if (lo >= hi) return;
-    append_block<DH, BF16, false>(a, q, head, blk, id, lo, hi, lds, wave_max[0]);
-    append_block<DH, BF16, true>(a, q, head, blk, id, lo, hi, lds, wave_max[1]);
+    const bool keys = w < key_wgs;
+    w -= keys ? 0 : key_wgs;
+    const int per = keys ? a.key_groups : a.c.heads, part = w % per, n = w / per;
+    BlockTokens b;
+    if (!block_tokens(a, n / a.seq_blocks, n % a.seq_blocks, &b)) return;
+    if (keys) append_keys<DH, BF16>(a, b, part * a.group_heads, min(a.c.heads, (part + 1) * a.group_heads), wave_max);
+    else append_values<DH, BF16>(a, b, part, lds, wave_max[0]);
     return;
   }
   w -= cache_wgs;
@@ -252,40 +391,46 @@ __global__ __launch_bounds__(1024) void k_kv_append(AppendArgs a) {
   const int i = (w / a.splits % a.row_tiles << a.rows_log2) + lane_row;
   if (i >= min(q.n, a.b.T)) return;
   int da, db;
-  slot_dims<DH>(a, tid % SL, &da, &db);
-  const bool turned = tid % SL * 16 < a.rot;
-  float cs[8], sn[8];
-  if (turned) slot_angles(a, tid % SL, q.first() + i, cs, sn);
+  slot_dims<DH, BF16>(a, tid % SL, &da, &db);
   const long long row = static_cast<long long>(q.row0 + i) * a.qkv_stride, to = (q.row0 + i) * a.q_stride;
   const int h_end = min(a.heads, (split + 1) * a.split_heads);
-  constexpr int B = BF16 ? 4 : 2;                // heads in flight
+  constexpr int B = 4;                           // heads in flight
+  float cs[P], sn[P];
+  bool known = false;
   for (int h0 = split * a.split_heads + group; h0 < h_end; h0 += B * groups) {
-    Piece<BF16> pa[B], pb[B];
+    uint4 pa[B], pb[B];
 #pragma unroll
     for (int n = 0; n < B; ++n) {
       const int h = h0 + n * groups;
       if (h < h_end) {
-        load_piece(a.qkv, row + h * DH + da, &pa[n]);
-        load_piece(a.qkv, row + h * DH + db, &pb[n]);
+        pa[n] = load_piece<BF16>(a.qkv, row + h * DH + da);
+        pb[n] = load_piece<BF16>(a.qkv, row + h * DH + db);
       }
     }
+    if (!known && a.rot > 0) slot_angles<P>(a, da, db, q.first() + i, cs, sn);
+    known = true;
 #pragma unroll
     for (int n = 0; n < B; ++n) {
       const int h = h0 + n * groups;
       if (h >= h_end) continue;
-      float x[16];
-      piece_values(pa[n], x);
-      piece_values(pb[n], x + 8);
-      if (a.q_gain) head_norm<DH>(a.q_gain, a.eps, da, db, x);
-      if (turned) turn(a.inter, cs, sn, x);
-      uint32_t o[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = kv_pair(x[2 * j], x[2 * j + 1]);
-      *reinterpret_cast<uint4*>(a.q + to + h * DH + da) = make_uint4(o[0], o[1], o[2], o[3]);
-      *reinterpret_cast<uint4*>(a.q + to + h * DH + db) = make_uint4(o[4], o[5], o[6], o[7]);
+      float x[2 * P];
+      piece_values<BF16>(pa[n], x);
+      piece_values<BF16>(pb[n], x + P);
+      if (a.q_gain) head_norm<DH, BF16>(a.q_gain, a.eps, da, db, x);
+      if (a.rot > 0) turn<P>(a.inter, cs, sn, x);
+      uint16_t* oa = a.q + to + h * DH + da;
+      uint16_t* ob = a.q + to + h * DH + db;
+      if constexpr (BF16) {
+        *reinterpret_cast<uint4*>(oa) = make_uint4(kv_pair(x[0], x[1]), kv_pair(x[2], x[3]), kv_pair(x[4], x[5]), kv_pair(x[6], x[7]));
+        *reinterpret_cast<uint4*>(ob) = make_uint4(kv_pair(x[8], x[9]), kv_pair(x[10], x[11]), kv_pair(x[12], x[13]), kv_pair(x[14], x[15]));
+      } else {
+        *reinterpret_cast<uint2*>(oa) = make_uint2(kv_pair(x[0], x[1]), kv_pair(x[2], x[3]));
+        *reinterpret_cast<uint2*>(ob) = make_uint2(kv_pair(x[4], x[5]), kv_pair(x[6], x[7]));
+      }
     }
   }
 }
+
 
 int32_t launch_kv_append(const void* qkv, bool bf16, long long qkv_stride, int heads, const moqe_rope& r, const moqe_kv_batch& b,
                          const moqe_kv_cache& c, void* q_out, long long q_stride, hipStream_t st) {
@@ -295,10 +440,17 @@ int32_t launch_kv_append(const void* qkv, bool bf16, long long qkv_stride, int h
   a.c = kv_cache_args(c);
   a.inv_freq = r.inv_freq; a.q_gain = r.q_gain; a.k_gain = r.k_gain; a.eps = r.eps; a.mscale = r.mscale;
   a.heads = heads; a.rot = r.rot_dim; a.inter = r.interleaved;
-  const int bt = c.block_tokens, dh = c.head_dim, sl = dh / 16, tokens = b.T < bt ? b.T : bt;
-  int th = 64;                                   // a thread takes two slots of a block's new tokens
-  while (th * 2 < tokens * sl) th *= 2;
+  const int bt = c.block_tokens, dh = c.head_dim, sl = dh / (bf16 ? 16 : 8), tokens = b.T < bt ? b.T : bt;
+  int th = 64;                                   // a thread of the cache part takes 32 values of a head's block
+  while (th * 32 < tokens * dh) th *= 2;
+  // keys: a work-group goes through several heads, whose angles are the same, where that still leaves two work-groups to a CU (16 prompts of 512 tokens, 32 heads: one head a
+  // work-group 103 us, eight 74, as with work-groups for all CUs twice)
   a.seq_blocks = (b.T + bt - 2) / bt + 1;
+  const long long blocks = static_cast<long long>(b.S) * a.seq_blocks;
+  const long long fewest = (511 + blocks) / blocks;
+  a.key_groups = int(fewest < c.n_heads ? fewest : c.n_heads);
+  a.group_heads = (c.n_heads + a.key_groups - 1) / a.key_groups;
+  a.key_groups = (c.n_heads + a.group_heads - 1) / a.group_heads;
   // query part: as many rows of a sequence side by side as there are, the other lanes take other heads; heads are split until the launch has about
   // four work-groups to a CU
   int rows = 1;
@@ -306,23 +458,24 @@ int32_t launch_kv_append(const void* qkv, bool bf16, long long qkv_stride, int h
   a.row_tiles = (b.T + rows - 1) / rows;
   const int side = th / sl / rows;               // heads side by side in a work-group
   const long long tiles = static_cast<long long>(b.S) * a.row_tiles;
-  long long parts = (1024 + tiles - 1) / tiles;
+  const long long parts = (1023 + tiles) / tiles;
   const int most = (heads + side - 1) / side;
   a.splits = int(parts < most ? parts : most);
   a.split_heads = (heads + a.splits - 1) / a.splits;
-  const long long wgs = static_cast<long long>(b.S) * a.seq_blocks * c.n_heads + tiles * a.splits;
+  const long long wgs = blocks * (a.key_groups + c.n_heads) + tiles * a.splits;
   if (wgs >= (1ll << 31)) return set_error(MOQE_E_SHAPE, "moqe_kv_append: %lld work-groups", wgs);
   const size_t lds = b.T >= 32 ? size_t(bt) * dh : 0;
   ProfileScope ps(MOQE_PK_OTHER, st);
   const dim3 grid(static_cast<unsigned>(wgs)), block(th);
-#define MOQE_APPEND(DH)                                                                        \
+#define MOQE_APPEND(DH, TH)                                                                    \
   do {                                                                                         \
-    if (bf16) hipLaunchKernelGGL((k_kv_append<DH, true>), grid, block, lds, st, a);            \
-    else hipLaunchKernelGGL((k_kv_append<DH, false>), grid, block, lds, st, a);                \
+    if (bf16) hipLaunchKernelGGL((k_kv_append<DH, true, TH>), grid, block, lds, st, a);         \
+    else hipLaunchKernelGGL((k_kv_append<DH, false, TH>), grid, block, lds, st, a);             \
   } while (0)
-  if (dh == 64) MOQE_APPEND(64);
-  else if (dh == 128) MOQE_APPEND(128);
-  else MOQE_APPEND(256);
+  if (dh == 64) MOQE_APPEND(64, 512);
+  else if (dh == 128) MOQE_APPEND(128, 512);
+  else if (th <= 512) MOQE_APPEND(256, 512);
+  else MOQE_APPEND(256, 1024);
 #undef MOQE_APPEND
   return check_launch("kv_append");
 }
