@@ -1,6 +1,8 @@
 // Attention over the 8-bit cache for few rows (decode steps, short continuations): bound by reading the cache once.
 #include "kv_device.h"
 
+#include <type_traits>
+
 namespace moqe {
 
 struct FewArgs {
@@ -60,8 +62,7 @@ __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, bool by_chunk,
 // One work-group takes a chunk of a sequence's tokens for one key head; each of its W waves takes every W-th step of 32 tokens.  A wave reads its step's codes
 // straight into matrix-core operands, 16 bytes a lane, and asks for the next step's keys as soon as this one's have gone through their product, for its values
 // likewise.  It keeps its own running maximum and sum for the NC * 16 columns (row i, query head g: column i * group + g); the waves' results are joined in LDS.
-// EXTRA: scores are capped, biased, or their scale is not positive.
-template <int DH, int NC, int W, bool EXTRA>
+template <int DH, int NC, int W, int EXTRA>
 __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_attend_few(FewArgs a) {
   constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64, VL = DH / 32;
   constexpr int PAD = DH + 4;
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
     const bool in = i < rows;
     pos[c] = first_pos + i;
     sight[c] = kv_sight(pos[c], q.len, window);
-    if (EXTRA) slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
+    if (EXTRA & KV_BIAS) slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
     const uint16_t* src = a.q + (q.row0 + i) * a.q_stride + static_cast<long long>(h * a.group + g) * DH + kq * 8;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
@@ -188,12 +189,13 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       float top = -INFINITY;
+      const float far = float(pos[c] - t0 - 4 * kq);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int tok = t0 + 16 * t + 4 * kq + x;
-          if (EXTRA) s[t][c][x] = kv_extra_score(a.sc, s[t][c][x], slope[c], pos[c] - tok);
+          if constexpr (EXTRA != KV_PLAIN) s[t][c][x] = kv_extra_score<EXTRA>(a.sc, s[t][c][x], slope[c], far - float(16 * t + x));
           if (!full && !sight[c].sees(tok, pre)) s[t][c][x] = -INFINITY;
           top = fmaxf(top, s[t][c][x]);
         }
@@ -402,24 +404,27 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   ProfileScope ps(MOQE_PK_OTHER, st);
   const dim3 grid(static_cast<unsigned>(wgs));
   const int nc = a.cols <= 16 ? 1 : a.cols <= 32 ? 2 : 4;
-  const bool extra = kv_extra(at);
-#define MOQE_FEW(DH, NC, W)                                                                             \
-  do {                                                                                                  \
-    if (extra) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, true>), grid, dim3(W * 64), 0, st, a);    \
-    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, false>), grid, dim3(W * 64), 0, st, a);         \
-  } while (0)
-  if (c.head_dim == 64) {
-    if (nc == 1) MOQE_FEW(64, 1, 8);
-    else if (nc == 2) MOQE_FEW(64, 2, 8);
-    else MOQE_FEW(64, 4, 4);
-  } else if (c.head_dim == 128) {
-    if (nc == 1) MOQE_FEW(128, 1, 8);
-    else if (nc == 2) MOQE_FEW(128, 2, 8);
-    else MOQE_FEW(128, 4, 4);
-  } else {
-    MOQE_FEW(256, 1, 8);
-  }
-#undef MOQE_FEW
+  const int extra = kv_extra(at);
+  auto launch = [&](auto dh, auto cols, auto waves) {
+    constexpr int DH = decltype(dh)::value, NC = decltype(cols)::value, W = decltype(waves)::value;
+    const dim3 block(W * 64);
+    if (extra == KV_PLAIN) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, KV_PLAIN>), grid, block, 0, st, a);
+    else if (extra == KV_CAP) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, KV_CAP>), grid, block, 0, st, a);
+    else if (extra == KV_BIAS) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, KV_BIAS>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, KV_CAP | KV_BIAS>), grid, block, 0, st, a);
+  };
+  auto launch_cols = [&](auto dh) {
+    const std::integral_constant<int, 4> four;
+    const std::integral_constant<int, 8> eight;
+    if (nc == 1) launch(dh, std::integral_constant<int, 1>(), eight);
+    if constexpr (decltype(dh)::value < 256) {
+      if (nc == 2) launch(dh, std::integral_constant<int, 2>(), eight);
+      if (nc == 4) launch(dh, four, four);
+    }
+  };
+  if (c.head_dim == 64) launch_cols(std::integral_constant<int, 64>());
+  else if (c.head_dim == 128) launch_cols(std::integral_constant<int, 128>());
+  else launch_cols(std::integral_constant<int, 256>());
   if (chunks) {
     const dim3 jgrid(static_cast<unsigned>(static_cast<long long>(b.S) * c.n_heads * a.cols));
     if (c.head_dim == 64) hipLaunchKernelGGL((k_kv_attend_join<64>), jgrid, dim3(256), 0, st, a);

@@ -1,6 +1,8 @@
 // Attention over the 8-bit cache for many rows (prompts, chunks of prompts): bound by the matrix cores and by the exponentials beside them.
 #include "kv_device.h"
 
+#include <type_traits>
+
 namespace moqe {
 
 // LDS reads issued before this point stay before the matrix products after it: the scheduler would put each read next to its product and wait for it there.
@@ -46,8 +48,7 @@ __device__ __forceinline__ bool rows_tile(const RowsArgs& a, int xcd, int x, Row
 // under way in registers), in the order in which a wave reads them: 16 bytes a lane in a row, no bank conflicts.  Products are 32 x 32 x 16, half as many
 // instructions as 16 x 16 x 32 at the same rate: a SIMD issues them and the softmax's arithmetic through one port, and that port is what it runs out of.
 // Scores stay in registers: the layout of S^T = K Q^T is the operand layout of O^T = V^T P^T if 16 tokens of values go 0..3, 8..11 | 4..7, 12..15.
-// EXTRA: scores are capped, biased, or their scale is not positive.
-template <int DH, bool EXTRA>
+template <int DH, int EXTRA>
 __global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_rows(RowsArgs a) {
   constexpr int W = ROWS_W, COLS = W * 32, KS = DH / 16, DT = DH / 32, U = DH / (W * 16);   // U: 16-byte units of keys (and of values) a thread brings in
   constexpr int HALF = 64 * DH * 2;                                            // bytes of a tile's keys in bf16
@@ -75,11 +76,12 @@ __global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_ro
   const bool idle = col0 / a.group >= rows;
   const KvRange wg_all = kv_all_see(p_first, p_last, pre, window), all_see = kv_all_see(w_first, w_last, pre, window),
                 some_see = kv_some_see(w_first, w_last, pre, window);
+  const int from = max(pre, window > 0 ? w_last - window + 1 : 0);             // steps from here on hide nothing from the wave's rows but what comes after them
   const int col = col0 + c32, row = col / a.group, head = h * a.group + col - row * a.group;
   const bool mine = row < rows;
   const int pos = first_pos + row;
   const KvSight sight = kv_sight(pos, q.len, window);
-  const float slope = EXTRA && mine && a.sc.slopes ? a.sc.slopes[head] * KV_LOG2E : 0.f;
+  const float slope = (EXTRA & KV_BIAS) && mine && a.sc.slopes ? a.sc.slopes[head] * KV_LOG2E : 0.f;
 
   kv_bf16x8 qf[KS];
   {
@@ -124,19 +126,19 @@ __global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_ro
   constexpr int STEP_U = 2 * DH / 64;                   // waves' worth of units in a step
   auto unit_step = [&](int n) { return STEP_U >= W ? n * W / STEP_U : n * (W / STEP_U) + wave_u / STEP_U; };
   auto unit_place = [&](int n) { return STEP_U >= W ? (n * W % STEP_U + wave_u) * 64 : wave_u % STEP_U * 64; };
-  // The tile under way: its codes, and of its two steps the scales and the first token (2^30: absent, seen by nobody; any block's codes do for it).
-  uint4 kc[U], vc[U];
-  float sk[2], sv[2];
-  int t0n[2];
-  auto fetch = [&](int t) {
+  // A tile under way: its codes, and of its two steps the scales and the first token (2^30: absent, seen by nobody; any block's codes do for it).  Two tiles are (one where
+  // the head is 256 wide and registers are short): loads have the time of two tiles to come.  2 x 2048 rows on 16384 tokens, one tile / two: 925 / 888 us.
+  constexpr int AHEAD = DH == 256 ? 1 : 2;
+  struct Staged { uint4 kc[U], vc[U]; float sk[2], sv[2]; int t0[2]; } way[2];
+  auto fetch = [&](int t, Staged& g) {
     if (2 * t >= look + 64) { look += 64; look_up(); }
     const uint8_t *kp[2], *vp[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int at = 2 * t + e - look, id = __builtin_amdgcn_readlane(ids, at), first = ks.step(2 * t + e) * 32;
-      sk[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), at));
-      sv[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), at));
-      t0n[e] = id >= 0 ? first : 1 << 30;
+      g.sk[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), at));
+      g.sv[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), at));
+      g.t0[e] = id >= 0 ? first : 1 << 30;
       const long long off = static_cast<long long>(max(id, 0) * static_cast<long long>(a.c.heads) + h) * head_bytes + (first & ((1 << a.c.bt_log2) - 1)) * DH;
       kp[e] = a.c.k + off;
       vp[e] = a.c.v + off;
@@ -144,55 +146,57 @@ __global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_ro
 #pragma unroll
     for (int n = 0; n < U; ++n) {
       const uint32_t at = (unit_place(n) + lane) * 16;
-      kc[n] = *reinterpret_cast<const uint4*>((unit_step(n) ? kp[1] : kp[0]) + at);
-      vc[n] = *reinterpret_cast<const uint4*>((unit_step(n) ? vp[1] : vp[0]) + at);
+      g.kc[n] = *reinterpret_cast<const uint4*>((unit_step(n) ? kp[1] : kp[0]) + at);
+      g.vc[n] = *reinterpret_cast<const uint4*>((unit_step(n) ? vp[1] : vp[0]) + at);
     }
   };
   bool nan = false;                    // a value that is NaN lies where some row does not see it and another may
-  auto put = [&](int buf) {
+  auto put = [&](int buf, Staged& g) {
     uint8_t* kb = lds + buf * 2 * HALF;
     uint8_t* vb = kb + HALF;
 #pragma unroll
     for (int n = 0; n < U; ++n) {
       const int e = unit_step(n), in = unit_place(n);
-      const float fk = e ? sk[1] : sk[0], fv = e ? sv[1] : sv[0];
+      const float fk = e ? g.sk[1] : g.sk[0], fv = e ? g.sv[1] : g.sv[0];
       // keys: 16-token tile in / DH, dims 64 * pair + 32 * st + 8 * kq ..: product k = dims / 16, lane (dims / 8 % 2) * 32 + token
       const int a16 = in / DH, pair = in % DH / 64;
       uint8_t* k0 = kb + (e * KS + 4 * pair) * 1024 + kq / 2 * 1024 + ((kq & 1) * 32 + 16 * a16 + r) * 16;
-      *reinterpret_cast<kv_bf16x8*>(k0) = kv_operand(kc[n].x, kc[n].y, fk);
-      *reinterpret_cast<kv_bf16x8*>(k0 + 2048) = kv_operand(kc[n].z, kc[n].w, fk);
-      const int t0 = e ? t0n[1] : t0n[0];
+      *reinterpret_cast<kv_bf16x8*>(k0) = kv_operand(g.kc[n].x, g.kc[n].y, fk);
+      *reinterpret_cast<kv_bf16x8*>(k0 + 2048) = kv_operand(g.kc[n].z, g.kc[n].w, fk);
+      const int t0 = e ? g.t0[1] : g.t0[0];
       if (!wg_all.has(t0)) {
-        vc[n] = kv_before(vc[n], t0 + 4 * kq, seen);
-        nan |= __ballot(kv_nan_bytes(vc[n]) != 0) != 0;
-        vc[n] = kv_without_nan(vc[n]);
+        g.vc[n] = kv_before(g.vc[n], t0 + 4 * kq, seen);
+        nan |= __ballot(kv_nan_bytes(g.vc[n]) != 0) != 0;
+        g.vc[n] = kv_without_nan(g.vc[n]);
       }
       // values: dims 32 * dpair + 16 * dt + r, tokens 16 * s + 4 * kq ..: product 2 e + s, lane (kq % 2) * 32 + dim, its first or second four tokens
       const int dpair = in / 64;
       uint8_t* v0 = vb + (2 * e * DT + dpair) * 1024 + ((kq & 1) * 32 + r) * 16 + kq / 2 * 8;
-      *reinterpret_cast<uint2*>(v0) = kv_four(vc[n].x, fv);
-      *reinterpret_cast<uint2*>(v0 + DT * 1024) = kv_four(vc[n].y, fv);
-      *reinterpret_cast<uint2*>(v0 + 256) = kv_four(vc[n].z, fv);
-      *reinterpret_cast<uint2*>(v0 + DT * 1024 + 256) = kv_four(vc[n].w, fv);
+      *reinterpret_cast<uint2*>(v0) = kv_four(g.vc[n].x, fv);
+      *reinterpret_cast<uint2*>(v0 + DT * 1024) = kv_four(g.vc[n].y, fv);
+      *reinterpret_cast<uint2*>(v0 + 256) = kv_four(g.vc[n].z, fv);
+      *reinterpret_cast<uint2*>(v0 + DT * 1024 + 256) = kv_four(g.vc[n].w, fv);
     }
   };
 
   int t0c[2] = {0, 0};
   if (t_begin < t_end) {
-    fetch(t_begin);
-    put(0);
-    t0c[0] = t0n[0]; t0c[1] = t0n[1];
+    fetch(t_begin, way[0]);
+    if (AHEAD == 2 && t_begin + 1 < t_end) fetch(t_begin + 1, way[1]);
+    put(0, way[0]);
+    t0c[0] = way[0].t0[0]; t0c[1] = way[0].t0[1];
   }
   __builtin_amdgcn_s_waitcnt(0);       // the queries have come: else the loop would wait for all loads under way before its first product, every time
-  if (t_begin + 1 < t_end) fetch(t_begin + 1);
+  if (t_begin + AHEAD < t_end) fetch(t_begin + AHEAD, way[0]);
   __syncthreads();
-  for (int t = t_begin; t < t_end; ++t) {
-    const int buf = (t - t_begin) & 1;
+  auto tile_step = [&](int t, auto odd) {
+    constexpr int buf = decltype(odd)::value;
     const int t0[2] = {t0c[0], t0c[1]};
     if (t + 1 < t_end) {
-      put(buf ^ 1);
-      t0c[0] = t0n[0]; t0c[1] = t0n[1];
-      if (t + 2 < t_end) fetch(t + 2);
+      Staged& g = way[AHEAD == 2 ? buf ^ 1 : 0];
+      put(buf ^ 1, g);
+      t0c[0] = g.t0[0]; t0c[1] = g.t0[1];
+      if (t + 1 + AHEAD < t_end) fetch(t + 1 + AHEAD, g);
     }
     const bool some = some_see.has(t0[0]) || some_see.has(t0[1]);
     if (!idle && some) {
@@ -226,18 +230,30 @@ __global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_ro
       for (int d = 0; d < 4; ++d) vf[0][d] = *reinterpret_cast<const kv_bf16x8*>(vb + d * 1024);
       KEEP_READS_AHEAD();
       // score y of step e belongs to token t0[e] + 8 * (y / 4) + 4 * half + y % 4
-      if (EXTRA) {
+      if constexpr (EXTRA != KV_PLAIN) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e) {
+          const float far = float(pos - t0[e] - 4 * half);
 #pragma unroll
-          for (int y = 0; y < 16; ++y) sc[e][y] = kv_extra_score(a.sc, sc[e][y], slope, pos - (t0[e] + y / 4 * 8 + half * 4 + y % 4));
+          for (int y = 0; y < 16; ++y) sc[e][y] = kv_extra_score<EXTRA>(a.sc, sc[e][y], slope, far - float(y / 4 * 8 + y % 4));
+        }
       }
       if (!full) {
+        if (t0[0] >= from && t0[1] >= from) {          // only by order
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+          for (int e = 0; e < 2; ++e) {
+            const int last = pos - t0[e] - 4 * half;
 #pragma unroll
-          for (int y = 0; y < 16; ++y)
-            if (!sight.sees(t0[e] + y / 4 * 8 + half * 4 + y % 4, pre)) sc[e][y] = -INFINITY;
+            for (int y = 0; y < 16; ++y)
+              if (y / 4 * 8 + y % 4 > last) sc[e][y] = -INFINITY;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int y = 0; y < 16; ++y)
+              if (!sight.sees(t0[e] + y / 4 * 8 + half * 4 + y % 4, pre)) sc[e][y] = -INFINITY;
+        }
       }
       float top = sc[0][0];
 #pragma unroll
@@ -275,6 +291,10 @@ __global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_ro
       __builtin_amdgcn_s_setprio(0);
     }
     __syncthreads();
+  };
+  for (int t = t_begin; t < t_end; t += 2) {
+    tile_step(t, std::integral_constant<int, 0>());
+    if (t + 1 < t_end) tile_step(t + 1, std::integral_constant<int, 1>());
   }
 
   l += __shfl_xor(l, 32);
@@ -394,22 +414,24 @@ int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_atte
   if (p.split_tiles) a.parts = kv_parts(ws, rows_parts(p));
   const int lds = 64 * c.head_dim * 2 * 4;
   const dim3 grid(static_cast<unsigned>(p.wgs)), block(ROWS_W * 64);
-  const bool extra = kv_extra(at);
-  if (c.head_dim == 256) {
-    const void* k = extra ? reinterpret_cast<const void*>(k_kv_attend_rows<256, true>) : reinterpret_cast<const void*>(k_kv_attend_rows<256, false>);
-    const int32_t rc = ensure_dynamic_lds(extra ? LDSK_ATTEND_ROWS_EXTRA : LDSK_ATTEND_ROWS, k, lds, "moqe_kv_attention");
-    if (rc) return rc;
-  }
+  const int extra = kv_extra(at);
+  int32_t rc = MOQE_OK;
   ProfileScope ps(MOQE_PK_OTHER, st);
-#define MOQE_ROWS(DH)                                                                         \
-  do {                                                                                        \
-    if (extra) hipLaunchKernelGGL((k_kv_attend_rows<DH, true>), grid, block, lds, st, a);     \
-    else hipLaunchKernelGGL((k_kv_attend_rows<DH, false>), grid, block, lds, st, a);          \
-  } while (0)
-  if (c.head_dim == 64) MOQE_ROWS(64);
-  else if (c.head_dim == 128) MOQE_ROWS(128);
-  else MOQE_ROWS(256);
-#undef MOQE_ROWS
+  auto launch = [&](auto dh, auto ex) {
+    constexpr int DH = decltype(dh)::value, EX = decltype(ex)::value;
+    if (DH == 256) rc = ensure_dynamic_lds(LDSK_ATTEND_ROWS + EX, reinterpret_cast<const void*>(k_kv_attend_rows<DH, EX>), lds, "moqe_kv_attention");
+    if (!rc) hipLaunchKernelGGL((k_kv_attend_rows<DH, EX>), grid, block, lds, st, a);
+  };
+  auto launch_dh = [&](auto dh) {
+    if (extra == KV_PLAIN) launch(dh, std::integral_constant<int, KV_PLAIN>());
+    else if (extra == KV_CAP) launch(dh, std::integral_constant<int, KV_CAP>());
+    else if (extra == KV_BIAS) launch(dh, std::integral_constant<int, KV_BIAS>());
+    else launch(dh, std::integral_constant<int, KV_CAP | KV_BIAS>());
+  };
+  if (c.head_dim == 64) launch_dh(std::integral_constant<int, 64>());
+  else if (c.head_dim == 128) launch_dh(std::integral_constant<int, 128>());
+  else launch_dh(std::integral_constant<int, 256>());
+  if (rc) return rc;
   if (p.split_tiles) {
     const dim3 jgrid(static_cast<unsigned>(p.split_tiles * 8 * ROWS_W * 32 * (c.head_dim / 4) / 256));
     if (c.head_dim == 64) hipLaunchKernelGGL((k_kv_rows_join<64>), jgrid, dim3(256), 0, st, a);

@@ -89,12 +89,19 @@ inline KvScore kv_score(const moqe_attention& a) {
   const bool capped = a.cap > 0.f;
   return KvScore{a.slopes, a.prefix, a.scale * KV_LOG2E, capped ? a.cap * KV_LOG2E : 0.f, capped ? 2.f * KV_LOG2E * a.scale / a.cap : 0.f, a.window};
 }
-// Scores that need more than one multiplication.
-inline bool kv_extra(const moqe_attention& a) { return a.slopes || a.cap > 0.f || !(a.scale > 0.f); }
-// cap * tanh(x / cap) as cap * (1 - 2 / (1 + e^(2 x / cap))), from the product d = q . k: its error is some 2^-22 of cap, wherever x lies.
-__device__ __forceinline__ float kv_extra_score(const KvScore& sc, float d, float slope, int distance) {
-  const float v = sc.cap2 > 0.f ? fmaf(-2.f * sc.cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(d * sc.turn)), sc.cap2) : d * sc.scale2;
-  return v - slope * fabsf(float(distance));
+// What a score needs beyond its scale: KV_CAP, KV_BIAS (by distance; also where the scale is not positive, since the kernels take the largest product for the largest score).
+enum : int { KV_PLAIN = 0, KV_CAP = 1, KV_BIAS = 2 };
+inline int kv_extra(const moqe_attention& a) {
+  const bool capped = a.cap > 0.f;
+  return (capped ? KV_CAP : 0) | (a.slopes || (!capped && !(a.scale > 0.f)) ? KV_BIAS : 0);
+}
+// From the product d = q . k.  cap * tanh(x / cap) is cap * (1 - 2 / (1 + e^(2 x / cap))): its error is some 2^-22 of cap, wherever x lies.
+template <int EXTRA>
+__device__ __forceinline__ float kv_extra_score(const KvScore& sc, float d, float slope, float distance) {
+  float v = d * sc.scale2;
+  if constexpr ((EXTRA & KV_CAP) != 0) v = fmaf(-2.f * sc.cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(d * sc.turn)), sc.cap2);
+  if constexpr ((EXTRA & KV_BIAS) != 0) v = fmaf(-slope, fabsf(distance), v);
+  return v;
 }
 
 // What a row at position p sees: tokens below `pre` and `span` tokens from `lo` on.
