@@ -36,16 +36,20 @@ __device__ __forceinline__ void slot_dims(const AppendArgs& a, int slot, int* da
   }
 }
 
-// cos and sin of angle number j at position p.  It is reduced to a fraction of a turn in 64 bits, where 32 would lose 2^-24 of p * inv_freq; what the fraction loses when it
-// is rounded to 32 comes back to first order: without that, the keys' codes had more than half as much error again as those of exact angles rounded to 32 bits.
+// cos and sin of angle number j at position p, rounded once: all is done in 64 bits, where 32 would lose 2^-24 of p * inv_freq, and an error in the last places of cos and sin
+// moves keys over the borders between codes.  The angle is taken to its fraction of a turn, that to the nearest quarter; on what is left, up to pi / 4, the power series
+// to x^11 and x^10 leave 2^-33.
 __device__ __forceinline__ void angle(const AppendArgs& a, int j, int p, float* cs, float* sn) {
   double turns = double(p) * (a.inv_freq[j] * 0.15915494309189535);
   turns -= rint(turns);
-  const float hi = float(turns), lo = float(turns - double(hi)) * 6.2831853f;
-  float s, c;
-  sincospif(2.f * hi, &s, &c);
-  *cs = a.mscale * fmaf(-lo, s, c);
-  *sn = a.mscale * fmaf(lo, c, s);
+  const double quarters = rint(4.0 * turns), x = fma(-0.25, quarters, turns) * 6.283185307179586, z = x * x;
+  const double s = x * fma(z, fma(z, fma(z, fma(z, fma(z, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6), 1.0);
+  const double c = fma(z, fma(z, fma(z, fma(z, fma(z, -1.0 / 3628800, 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5), 1.0);
+  const int n = static_cast<int>(quarters) & 3;
+  const float fs = float(s * double(a.mscale)), fc = float(c * double(a.mscale));
+  const float u = n & 1 ? fs : fc, v = n & 1 ? fc : fs;
+  *cs = n == 1 || n == 2 ? -u : u;
+  *sn = n >= 2 ? -v : v;
 }
 template <int P>
 __device__ __forceinline__ void slot_angles(const AppendArgs& a, int da, int db, int p, float* cs, float* sn) {
@@ -60,7 +64,15 @@ __device__ __forceinline__ void slot_angles(const AppendArgs& a, int da, int db,
   }
 }
 
-template <int P>
+// e cos - f sin.  EXACT: with what the rounding of f sin leaves, so that the result is rounded once.
+template <bool EXACT>
+__device__ __forceinline__ float turned(float e, float f, float cs, float sn) {
+  const float w = f * sn, r = fmaf(e, cs, -w);
+  if (!EXACT) return r;
+  const float x = r - fmaf(f, sn, -w);
+  return x == x ? x : r;                         // an infinite f leaves NaN
+}
+template <int P, bool EXACT>
 __device__ __forceinline__ void turn(bool inter, const float* cs, const float* sn, float* x) {
 #pragma unroll
   for (int i = 0; i < P; ++i) {
@@ -68,12 +80,12 @@ __device__ __forceinline__ void turn(bool inter, const float* cs, const float* s
     const int u = i / (P / 2) * P + 2 * (i % (P / 2));                // neighbours
     if (inter) {
       const float e = x[u], f = x[u + 1];
-      x[u] = e * cs[i] - f * sn[i];
-      x[u + 1] = f * cs[i] + e * sn[i];
+      x[u] = turned<EXACT>(e, f, cs[i], sn[i]);
+      x[u + 1] = turned<EXACT>(f, e, cs[i], -sn[i]);
     } else {
       const float e = x[s], f = x[t];
-      x[s] = e * cs[i] - f * sn[i];
-      x[t] = f * cs[i] + e * sn[i];
+      x[s] = turned<EXACT>(e, f, cs[i], sn[i]);
+      x[t] = turned<EXACT>(f, e, cs[i], -sn[i]);
     }
   }
 }
@@ -96,8 +108,8 @@ __device__ __forceinline__ void piece_values(const uint4& p, float* x) {
   }
 }
 
-// RMS norm of a head vector whose slots lie in neighbouring lanes.
-template <int DH, bool BF16>
+// RMS norm of a head vector whose slots lie in neighbouring lanes.  EXACT: what follows the sum of squares is rounded twice only.
+template <int DH, bool BF16, bool EXACT>
 __device__ __forceinline__ void head_norm(const float* gain, float eps, int da, int db, float* x) {
   constexpr int P = PIECE<BF16>;
   float q = 0.f;
@@ -105,11 +117,19 @@ __device__ __forceinline__ void head_norm(const float* gain, float eps, int da, 
   for (int i = 0; i < 2 * P; ++i) q += x[i] * x[i];
 #pragma unroll
   for (int d = 1; d < SLOTS<DH, BF16>; d *= 2) q += __shfl_xor(q, d);
-  const float inv = 1.f / sqrtf(q / float(DH) + eps);
+  float hi, lo = 0.f;
+  if constexpr (EXACT) {
+    const double inv = 1.0 / sqrt(double(q) / DH + double(eps));
+    hi = float(inv);
+    lo = float(inv - double(hi));
+  } else {
+    hi = 1.f / sqrtf(q / float(DH) + eps);
+  }
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    x[i] *= inv * gain[da + i];
-    x[P + i] *= inv * gain[db + i];
+    const float ga = gain[da + i], gb = gain[db + i];
+    x[i] *= EXACT ? fmaf(hi, ga, lo * ga) : hi * ga;
+    x[P + i] *= EXACT ? fmaf(hi, gb, lo * gb) : hi * gb;
   }
 }
 
@@ -206,7 +226,7 @@ __device__ __forceinline__ bool block_tokens(const AppendArgs& a, int s, int n, 
   return b->id >= 0 && b->id < a.c.n_blocks;
 }
 
-// Keys of one block for some heads in turn.  A thread has 32 values in slots, the same tokens and dims for every head, so that it works out its angles once for all of them.
+// Keys of one block for some heads in turn.  Their norm and rotation are kept to few roundings in fp32: each one moves some keys over the border between two codes.  A thread has 32 values in slots, the same tokens and dims for every head, so that it works out its angles once for all of them.
 template <int DH, bool BF16>
 __device__ __forceinline__ void append_keys(const AppendArgs& a, const BlockTokens& b, int head0, int head1, float (*wave_max)[16]) {
   constexpr int P = PIECE<BF16>, SL = SLOTS<DH, BF16>, NS = 16 / P;
@@ -244,8 +264,8 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const BlockToke
       if (n * th + tid < slots) {
         piece_values<BF16>(pa[n], x[n]);
         piece_values<BF16>(pb[n], x[n] + P);
-        if (a.k_gain) head_norm<DH, BF16>(a.k_gain, a.eps, da, db, x[n]);        // a head vector's slots are all in or all out
-        if (a.rot > 0) turn<P>(a.inter, cs[n], sn[n], x[n]);
+        if (a.k_gain) head_norm<DH, BF16, true>(a.k_gain, a.eps, da, db, x[n]);        // a head vector's slots are all in or all out
+        if (a.rot > 0) turn<P, true>(a.inter, cs[n], sn[n], x[n]);
         largest(x[n], &top, &infinite);
       }
     }
@@ -364,7 +384,7 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, const BlockTo
 
 // Work-groups of the keys (one for each block a sequence can touch and group of heads), of the values (one for each block and head), then of the queries (a row tile
 // and some heads each).  At most TH threads: 1024 for blocks of 128 tokens of 256 dims, whose work-groups have to do with 128 registers.
-// Bound by memory: 16 prompts of 512 tokens with 32 heads of 128 (336 MB) 74 us,
+// Bound by memory: 16 prompts of 512 tokens with 32 heads of 128 (336 MB) 75 us,
 // rows of mixed lengths in fp32 with 28 (475 MB) 103 us, where a copy of as many bytes takes 68 and 96.
 template <int DH, bool BF16, int TH>
 __global__ __launch_bounds__(TH, TH > 512 ? 1 : BF16 ? 4 : 3) void k_kv_append(AppendArgs a) {
@@ -416,8 +436,8 @@ __global__ __launch_bounds__(TH, TH > 512 ? 1 : BF16 ? 4 : 3) void k_kv_append(A
       float x[2 * P];
       piece_values<BF16>(pa[n], x);
       piece_values<BF16>(pb[n], x + P);
-      if (a.q_gain) head_norm<DH, BF16>(a.q_gain, a.eps, da, db, x);
-      if (a.rot > 0) turn<P>(a.inter, cs, sn, x);
+      if (a.q_gain) head_norm<DH, BF16, false>(a.q_gain, a.eps, da, db, x);
+      if (a.rot > 0) turn<P, false>(a.inter, cs, sn, x);
       uint16_t* oa = a.q + to + h * DH + da;
       uint16_t* ob = a.q + to + h * DH + db;
       if constexpr (BF16) {
@@ -463,7 +483,7 @@ int32_t launch_kv_append(const void* qkv, bool bf16, long long qkv_stride, int h
   a.splits = int(parts < most ? parts : most);
   a.split_heads = (heads + a.splits - 1) / a.splits;
   const long long wgs = blocks * (a.key_groups + c.n_heads) + tiles * a.splits;
-  if (wgs >= (1ll << 31)) return set_error(MOQE_E_SHAPE, "moqe_kv_append: %lld work-groups", wgs);
+  if (wgs * th >= (1ll << 32)) return set_error(MOQE_E_SHAPE, "moqe_kv_append: %lld work-groups", wgs);
   const size_t lds = b.T >= 32 ? size_t(bt) * dh : 0;
   ProfileScope ps(MOQE_PK_OTHER, st);
   const dim3 grid(static_cast<unsigned>(wgs)), block(th);

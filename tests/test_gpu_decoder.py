@@ -513,3 +513,26 @@ def test_other_streams_and_graphs(rows):
     replayed = steps(3, graph.replay)
     for a, b, c in zip(want, got, replayed):
         assert all(torch.equal(x, y) and torch.equal(x, z) for x, y, z in zip(a, b, c))
+
+
+def test_append_turns_infinities():
+    """An infinite key value makes its pair infinite, hence the largest codes; NaN makes its pair NaN; the others are the oracle's codes."""
+    dh, bt, rows = 64, 32, 5
+    rng = np.random.default_rng(31)
+    host = rng.normal(size=(rows, 3 * dh))
+    host[1, dh + 5], host[2, dh + 40], host[3, dh + 7], host[4, dh + 33] = np.inf, -np.inf, np.nan, np.inf
+    x = dev(host, F32)
+    for inter in (False, True):
+        for t in (F32, BF):
+            f = 100.0 ** (-2.0 * np.arange(32) / 64)
+            cache, batch = do.Cache(1, 1, bt, dh), mq.KvBatch(dev(np.zeros((1, 1), np.int32)), dev(np.array([rows], np.int32)), 1, rows, rows)
+            d, q = _on_device(cache), torch.empty((rows, dh), dtype=BF, device=DEV)
+            mq.moqe_kv_append(x.to(t), 1, mq.Rope(dev(f), 64, inter), batch, d, q)
+            sync()
+            with np.errstate(invalid="ignore"):
+                do.kv_append(f64(x.to(t)), 1, cache, np.zeros((1, 1), int), do.sequences(1, rows, rows, [rows], 1, bt), rows, f, 64, inter)
+            at = cache.at["k"][:rows]
+            got, want = do.e4m3_value(d.k.cpu().numpy()[0, 0][at]), do.e4m3_value(cache.k[0, 0][at])
+            assert float(d.k_scale[0, 0]) == cache.k_scale[0, 0]
+            assert np.array_equal(np.isnan(got), np.isnan(want)) and np.isnan(want).sum() == 2 and (np.abs(want) == 448).sum() >= 6
+            assert (got == want)[~np.isnan(want)].mean() > 0.98 and np.array_equal(np.abs(got) == 448, np.abs(want) == 448)
