@@ -36,6 +36,8 @@ int32_t check_batch(const moqe_kv_batch* b, const moqe_kv_cache& c, const char* 
     return set_error(MOQE_E_SHAPE, "%s: M=%d is not S*T=%lld", who, b->M, static_cast<long long>(b->S) * b->T);
   if (static_cast<long long>(b->table_width) * c.block_tokens > (1ll << 30) || b->T > (1 << 24) || static_cast<long long>(b->S) * b->T > (1ll << 30))
     return set_error(MOQE_E_SHAPE, "%s: more than 2^30 tokens a sequence, 2^24 rows a sequence or 2^30 rows", who);
+  if (static_cast<long long>(b->S) * b->table_width * c.block_tokens > (1ll << 35))
+    return set_error(MOQE_E_SHAPE, "%s: block tables of more than 2^35 tokens in all", who);
   if (b->S > 0 && (!b->block_table || !b->kv_len)) return set_error(MOQE_E_NULL, "%s: block_table or kv_len is NULL", who);
   if (!aligned(b->block_table, 4) || !aligned(b->kv_len, 4) || !aligned(b->cu_rows, 4))
     return set_error(MOQE_E_SHAPE, "%s: misaligned block_table, kv_len or cu_rows", who);

@@ -368,11 +368,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(FewArgs a) {
 }
 
 namespace {
-#ifndef FEW_TARGET
-#define FEW_TARGET 1024
-#define FEW_MIN 32
-#endif
-constexpr int FEW_TARGET_WGS = FEW_TARGET, FEW_MIN_STEPS = FEW_MIN;
+constexpr int FEW_TARGET_WGS = 1024, FEW_MIN_STEPS = 32;
 long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c) {          // chunks at most; 0: one a sequence
   const long long most = static_cast<long long>(b.table_width) * c.block_tokens / 32;
   if (most <= FEW_MIN_STEPS) return 0;
@@ -400,7 +396,8 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   const long long chunks = few_chunks(b, c);
   if (chunks) a.parts = kv_parts(ws, size_t(chunks) * c.n_heads * a.cols);
   const long long wgs = (chunks ? chunks : b.S) * c.n_heads;
-  if (wgs >= (1ll << 31)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld work-groups", wgs);
+  const long long join_wgs = chunks ? static_cast<long long>(b.S) * c.n_heads * a.cols : 0;
+  if (wgs >= (1ll << 23) || join_wgs >= (1ll << 24)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld and %lld work-groups", wgs, join_wgs);
   ProfileScope ps(MOQE_PK_OTHER, st);
   const dim3 grid(static_cast<unsigned>(wgs));
   const int nc = a.cols <= 16 ? 1 : a.cols <= 32 ? 2 : 4;
@@ -426,7 +423,7 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   else if (c.head_dim == 128) launch_cols(std::integral_constant<int, 128>());
   else launch_cols(std::integral_constant<int, 256>());
   if (chunks) {
-    const dim3 jgrid(static_cast<unsigned>(static_cast<long long>(b.S) * c.n_heads * a.cols));
+    const dim3 jgrid(static_cast<unsigned>(join_wgs));
     if (c.head_dim == 64) hipLaunchKernelGGL((k_kv_attend_join<64>), jgrid, dim3(256), 0, st, a);
     else if (c.head_dim == 128) hipLaunchKernelGGL((k_kv_attend_join<128>), jgrid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_kv_attend_join<256>), jgrid, dim3(256), 0, st, a);

@@ -406,7 +406,7 @@ int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_atte
   a.sc = kv_score(at);
   a.group = at.n_heads / c.n_heads;
   const RowsPlan p = rows_plan(at, b, c);
-  if (p.wgs >= (1ll << 31)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld work-groups", p.wgs);
+  if (p.wgs >= (1ll << 24)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld work-groups", p.wgs);
   a.tiles = int(p.tiles);
   a.whole = int(p.whole);
   a.split_tiles = int(p.split_tiles);

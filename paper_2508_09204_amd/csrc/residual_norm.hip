@@ -3,10 +3,6 @@
 
 namespace moqe {
 
-#ifndef NORM_ONE
-#define NORM_ONE 1024
-#endif
-
 struct NormArgs {
   const void* y; const void* r; void* r_out; uint16_t* out;
   const float *gate, *post_gain, *post_offset, *pre_gain, *pre_offset;
@@ -22,7 +18,7 @@ __device__ __forceinline__ uint32_t bf16_round(float x) {
 }
 
 // Eight values from feature f on, of a row or vector of d.  Rows that start anywhere (ODD: an odd d, stride or address) still take wide accesses, which need
-// no alignment beyond an element's; only the last piece of an odd d goes element by element. 
+// no alignment beyond an element's; only the last piece of an odd d goes element by element.
 template <bool BF16> struct Values {
   uint4 q[BF16 ? 1 : 2];
   static constexpr int SIZE = BF16 ? 2 : 4;
@@ -147,8 +143,9 @@ template <int NV, bool ODD, bool YBF, bool RBF>
 __global__ __launch_bounds__(1024) void k_residual_norm(NormArgs a) {
   __shared__ float part[4 * 16];
   const int th = a.row_threads, d = a.d, lane = th == 64 ? threadIdx.x & 63 : threadIdx.x;
-  const int row = th == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-  if (row >= a.M) return;
+  const uint32_t wg = blockIdx.y * gridDim.x + blockIdx.x, in_order = th == 64 ? wg * 4 + (threadIdx.x >> 6) : wg;
+  if (in_order >= uint32_t(a.M)) return;
+  const int row = static_cast<int>(in_order);
   float u[NV][8], t[NV][8];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -194,7 +191,9 @@ namespace {
 template <int NV, bool ODD>
 void launch_types(const NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
   const bool wave_rows = a.row_threads == 64;
-  const dim3 grid(wave_rows ? (a.M + 3) / 4 : a.M), block(wave_rows ? 256 : a.row_threads);
+  // a launch has fewer than 2^32 threads along x
+  const uint32_t wgs = wave_rows ? (uint32_t(a.M) + 3) / 4 : uint32_t(a.M), gx = wgs < (1u << 20) ? wgs : 1u << 20;
+  const dim3 grid(gx, (wgs + gx - 1) / gx), block(wave_rows ? 256 : a.row_threads);
   if (ybf && rbf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, true, true>), grid, block, 0, st, a);
   else if (ybf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, true, false>), grid, block, 0, st, a);
   else if (rbf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, false, true>), grid, block, 0, st, a);
@@ -203,7 +202,7 @@ void launch_types(const NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
 template <bool ODD>
 void launch_pieces(NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
   const int pieces = (a.d + 7) / 8;
-  const int nv = pieces <= NORM_ONE ? 1 : pieces <= 2048 ? 2 : 4;
+  const int nv = pieces <= 1024 ? 1 : pieces <= 2048 ? 2 : 4;
   a.row_threads = ((pieces + nv - 1) / nv + 63) / 64 * 64;
   if (nv == 1) launch_types<1, ODD>(a, ybf, rbf, st);
   else if (nv == 2) launch_types<2, ODD>(a, ybf, rbf, st);

@@ -221,3 +221,9 @@ def test_scale_exponents(probe):
 
 def test_steps_cover_what_rows_see(probe):
     assert probe("steps").startswith("0 bad of ")
+
+
+def test_sizes_that_the_launches_do_not_hold_are_refused(mq):
+    assert _attend(mq, batch={"S": 1 << 16, "T": 1, "M": 1 << 16, "table_width": 1 << 13}) == 0
+    assert _attend(mq, batch={"S": 1 << 16, "T": 1, "M": 1 << 16, "table_width": 1 << 14}) == -2        # 2^36 places for tokens
+    assert _append(mq, batch={"S": 1 << 16, "T": 1, "M": 1 << 16, "table_width": 1 << 14}) == -2
