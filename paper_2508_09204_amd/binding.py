@@ -486,6 +486,11 @@ def moqe_label_pass(blk: Block, x: torch.Tensor, targets: torch.Tensor, S: int, 
                                _ptr(workspace), workspace.numel(), _stream()))
 
 
+def moqe_workspace_bytes_routed(blk: Block, S: int, T: int) -> int:
+    b = blk.c()
+    return lib.moqe_workspace_bytes_routed(C.byref(b), S, T)
+
+
 def moqe_forward_routed(blk: Block, expert_idx: torch.Tensor, x: torch.Tensor, S: int, T: int, y: torch.Tensor,
                         aux: Optional[Aux] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """The block on experts chosen by the caller (e.g. by moqe_route_nlp or moqe_route_cv)."""
