@@ -12,18 +12,19 @@ struct FewArgs {
   int group, cols;              // query heads to a key head; columns (rows x group) of a sequence and key head at most
   int target, min_steps;        // chunks wanted in all, steps of 32 tokens that a chunk has at least
   KvParts parts;                // [chunk][key head][column]; NULL: one chunk a sequence
+  int2* of_seq;                 // first chunk and chunks of every sequence, for the launch that joins them
 };
 
-// How the sequences' steps are cut into chunks: all chunks but a sequence's last have C steps.  Every wave works it out by itself.
+// How the sequences' steps are cut into chunks, equal ones within a sequence.  Every wave works it out by itself.
 struct FewPlan {
-  int s, chunk, first, chunks, steps;      // sequence, chunk in it, number of its first chunk, its chunks, steps of a chunk
+  int s, first, chunks, j, j_end;          // sequence, number of its first chunk, its chunks, steps of this one
 };
 __device__ __forceinline__ KvSteps few_steps(const FewArgs& a, int s, KvSeq* q) {
   *q = kv_seq(a.b, s, a.c.bt_log2);
   return kv_steps(q->len, q->n > 0 ? q->len : 0, q->first(), a.sc.window, a.sc.prefix ? a.sc.prefix[s] : 0);
 }
-// The sequence that chunk number `w` falls into (by_chunk), or the chunks of sequence `w`.  False: there is no such chunk.
-__device__ __forceinline__ bool few_plan(const FewArgs& a, int w, bool by_chunk, FewPlan* p) {
+// The sequence that chunk number `w` falls into.  False: there is no such chunk.
+__device__ __forceinline__ bool few_plan(const FewArgs& a, int w, FewPlan* p) {
   const int lane = threadIdx.x & 63, S = a.b.S;
   int total = 0;
   for (int base = 0; base < S; base += 64) {
@@ -32,26 +33,28 @@ __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, bool by_chunk,
   }
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
-  p->steps = max(a.min_steps, (total + a.target - 1) / a.target);
+  const int steps = max(a.min_steps, (total + a.target - 1) / a.target);
   int before = 0;
   for (int base = 0; base < S; base += 64) {
     KvSeq q;
-    const int s = base + lane;
-    const int n = s < S ? max(1, (few_steps(a, s, &q).count + p->steps - 1) / p->steps) : 0;
+    const int s = base + lane, count = s < S ? few_steps(a, s, &q).count : 0;
+    const int n = s < S ? max(1, (count + steps - 1) / steps) : 0;
     int upto = n;                                   // inclusive sum over the lanes
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const int o = __shfl_up(upto, d);
       if (lane >= d) upto += o;
     }
-    const bool here = by_chunk ? w < before + upto : s == w;
-    const unsigned long long hit = __ballot(here);
+    const unsigned long long hit = __ballot(w < before + upto);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       p->s = base + l;
-      p->chunks = __shfl(n, l);
-      p->first = before + __shfl(upto, l) - p->chunks;
-      p->chunk = w - p->first;
+      p->chunks = __builtin_amdgcn_readlane(n, l);
+      p->first = __builtin_amdgcn_readfirstlane(before) + __builtin_amdgcn_readlane(upto, l) - p->chunks;
+      const int c = w - p->first, all = __builtin_amdgcn_readlane(count, l);
+      const int each = all / p->chunks, more = all - each * p->chunks;        // the first chunks have one step more
+      p->j = __builtin_amdgcn_readfirstlane(c * each + min(c, more));
+      p->j_end = __builtin_amdgcn_readfirstlane(p->j + each + (c < more ? 1 : 0));
       return true;
     }
     before += __shfl(upto, 63);
@@ -62,9 +65,10 @@ __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, bool by_chunk,
 // One work-group takes a chunk of a sequence's tokens for one key head; each of its W waves takes every W-th step of 32 tokens.  A wave reads its step's codes
 // straight into matrix-core operands, 16 bytes a lane, and asks for the next step's keys as soon as this one's have gone through their product, for its values
 // likewise.  It keeps its own running maximum and sum for the NC * 16 columns (row i, query head g: column i * group + g); the waves' results are joined in LDS.
-template <int DH, int NC, int W, int EXTRA>
-__global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_attend_few(FewArgs a) {
-  constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64, VL = DH / 32;
+constexpr int FEW_W = 8;
+template <int DH, int NC, int EXTRA>
+__global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_attend_few(FewArgs a) {
+  constexpr int W = FEW_W, KS = DH / 32, DT = DH / 16, KL = DH / 64, VL = DH / 32;
   constexpr int PAD = DH + 4;
   __shared__ float obuf[4][16][PAD];
   __shared__ float2 ml[W][NC * 16];
@@ -72,9 +76,9 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
   const int h = blockIdx.x % a.c.heads, w = blockIdx.x / a.c.heads;
   FewPlan pl;
   if (a.parts.o) {
-    if (!few_plan(a, w, true, &pl)) return;
+    if (!few_plan(a, w, &pl)) return;
   } else {
-    pl = FewPlan{w, 0, w, 1, 1 << 30};
+    pl = FewPlan{w, w, 1, 0, 1 << 30};
   }
   KvSeq q;
   const KvSteps ks = few_steps(a, pl.s, &q);
@@ -82,7 +86,7 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
   if (rows == 0) return;
   const int pre = a.sc.prefix ? min(a.sc.prefix[pl.s], q.len) : 0, window = a.sc.window, last_pos = first_pos + rows - 1;
   const KvRange all_see = kv_all_see(first_pos, last_pos, pre, window);
-  const int j_begin = pl.chunk * pl.steps + wave, j_end = min(ks.count, pl.chunk < 1 ? pl.steps : pl.steps * (pl.chunk + 1));
+  const int j_begin = pl.j + wave, j_end = min(ks.count, pl.j_end);
   const float scale2 = a.sc.scale2;
 
   // 64 steps of this wave at a time: lane i looks up step j0 + W i: block (-1: absent, nothing is seen) and scales
@@ -235,6 +239,7 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
     load_values(j + W, next);
   }
 
+  if (a.parts.o && w == pl.first && h == 0 && tid == 0) a.of_seq[pl.s] = make_int2(pl.first, pl.chunks);      // not earlier: loads after a store are not scalar
   // the waves' results: common maximum, then sums in a fixed order: wave v + 4 joins wave v, then four waves in a row
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -250,20 +255,16 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
     for (int v = 1; v < W; ++v) mt = fmaxf(mt, ml[v][c * 16 + r].x);
     const float f = exp2f(m[c] - mt);
     if (c > 0) __syncthreads();              // the columns before have been read
-    if (W == 8) {
-      if (wave >= 4) {
+    if (wave >= 4) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *reinterpret_cast<kv_f32x4*>(&obuf[wave & 3][r][d * 16 + kq * 4]) = o[c][d] * f;
-      }
-      __syncthreads();
+      for (int d = 0; d < DT; ++d) *reinterpret_cast<kv_f32x4*>(&obuf[wave & 3][r][d * 16 + kq * 4]) = o[c][d] * f;
     }
+    __syncthreads();
     if (wave < 4) {                          // a lane reads and writes its own places
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         kv_f32x4* at = reinterpret_cast<kv_f32x4*>(&obuf[wave][r][d * 16 + kq * 4]);
-        kv_f32x4 v = o[c][d] * f;
-        if (W == 8) v += *at;
-        *at = v;
+        *at += o[c][d] * f;
       }
     }
     __syncthreads();
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_att
 }
 
 // Joins the chunks: a work-group for each column of a sequence and key head.  DH / 4 lanes hold a row; the 1024 / DH such groups of lanes take every so many-th
-// chunk, and their sums are added in order.
+// chunk, and their sums are added in order.  The first chunk of each group is asked for along with the maxima.
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv_attend_join(FewArgs a) {
   constexpr int L = DH / 4, GROUPS = 256 / L;
@@ -331,24 +332,28 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(FewArgs a) {
   __shared__ float lsum[GROUPS];
   const int group = threadIdx.x / L, lane = threadIdx.x % L;
   const int h = blockIdx.x % a.c.heads, s = blockIdx.x / a.c.heads / a.cols, col = blockIdx.x / a.c.heads % a.cols;
-  FewPlan pl;
-  if (!few_plan(a, s, false, &pl) || pl.chunks == 1) return;
-  const int chunks = pl.chunks;
-  const long long step = static_cast<long long>(a.c.heads) * a.cols, at = pl.first * step + static_cast<long long>(h) * a.cols + col;
+  const int2 of_seq = a.of_seq[s];
   const KvSeq q = kv_seq(a.b, s, a.c.bt_log2);
-  const int i = col / a.group, g = col - i * a.group;
-  if (i >= min(q.n, a.b.T)) return;
+  const int chunks = of_seq.y, i = col / a.group, g = col - i * a.group;
+  if (chunks <= 1 || i >= min(q.n, a.b.T)) return;
+  const long long step = static_cast<long long>(a.c.heads) * a.cols, at = of_seq.x * step + static_cast<long long>(h) * a.cols + col;
+  float2 x = make_float2(-3e38f, 0.f);
+  float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto load = [&](int c) {
+    x = a.parts.ml[at + c * step];
+    p = *reinterpret_cast<const float4*>(a.parts.o + (at + c * step) * DH + lane * 4);
+  };
+  if (group < chunks) load(group);
   float m = -3e38f;
   for (int c = threadIdx.x & 63; c < chunks; c += 64) m = fmaxf(m, a.parts.ml[at + c * step].x);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  float l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float f = exp2f(x.x - m), l = x.y * f;
+  float4 o = make_float4(f * p.x, f * p.y, f * p.z, f * p.w);
 #pragma unroll 8
-  for (int c = group; c < chunks; c += GROUPS) {
-    const float2 x = a.parts.ml[at + c * step];
-    const float4 p = *reinterpret_cast<const float4*>(a.parts.o + (at + c * step) * DH + lane * 4);
-    const float f = exp2f(x.x - m);
+  for (int c = group + GROUPS; c < chunks; c += GROUPS) {
+    load(c);
+    f = exp2f(x.x - m);
     l += x.y * f;
     o.x += f * p.x; o.y += f * p.y; o.z += f * p.z; o.w += f * p.w;
   }
@@ -358,8 +363,8 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(FewArgs a) {
   if (group > 0) return;
 #pragma unroll
   for (int v = 1; v < GROUPS; ++v) {
-    const float4 p = sums[v][lane];
-    o.x += p.x; o.y += p.y; o.z += p.z; o.w += p.w;
+    const float4 y = sums[v][lane];
+    o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
     l += lsum[v];
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -368,18 +373,25 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(FewArgs a) {
 }
 
 namespace {
-constexpr int FEW_TARGET_WGS = 1024, FEW_MIN_STEPS = 32;
-long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c) {          // chunks at most; 0: one a sequence
-  const long long most = static_cast<long long>(b.table_width) * c.block_tokens / 32;
-  if (most <= FEW_MIN_STEPS) return 0;
-  const int target = FEW_TARGET_WGS / c.n_heads > 0 ? FEW_TARGET_WGS / c.n_heads : 1;
-  return target + static_cast<long long>(b.S);
+// Chunks wanted of a key head: as many work-groups as run at once (two a CU; one where the head is wide or there are more than 16 columns), or the smallest multiple of that
+// with one for each sequence, less the half chunk that each sequence adds by rounding up.  Chunks of fewer than 32 steps, four a wave, are mostly the time of their first loads.
+// One round / 1024 / 2048 work-groups wanted: 2 sequences of 131000 tokens 98 / 103 / 120 us, 64 of up to 8000 57 / 58 / 65.
+constexpr int FEW_MIN_STEPS = 32;
+int few_target(const moqe_kv_batch& b, const moqe_kv_cache& c, int cols) {
+  const int at_once = cols <= 16 && c.head_dim <= 128 ? 512 : 256;
+  const long long round = at_once / c.n_heads > 0 ? at_once / c.n_heads : 1, rounds = (b.S + round - 1) / round;
+  return static_cast<int>(rounds * round - b.S / 2);
+}
+long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c, int cols) {          // chunks at most; 0: one a sequence
+  if (static_cast<long long>(b.table_width) * c.block_tokens / 32 <= FEW_MIN_STEPS) return 0;
+  return few_target(b, c, cols) + static_cast<long long>(b.S);
 }
 }  // namespace
 
 size_t kv_attend_few_ws_bytes(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c) {
-  const size_t rows = size_t(few_chunks(b, c)) * c.n_heads * (size_t(b.T) * (at.n_heads / c.n_heads));
-  return align256(rows * 8) + align256(rows * c.head_dim * 4);
+  const int cols = b.T * (at.n_heads / c.n_heads);
+  const size_t rows = size_t(few_chunks(b, c, cols)) * c.n_heads * cols;
+  return align256(rows * 8) + align256(rows * c.head_dim * 4) + align256(rows ? size_t(b.S) * 8 : 0);
 }
 
 int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c,
@@ -391,33 +403,33 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   a.sc = kv_score(at);
   a.group = at.n_heads / c.n_heads;
   a.cols = b.T * a.group;
-  a.target = FEW_TARGET_WGS / c.n_heads > 0 ? FEW_TARGET_WGS / c.n_heads : 1;
+  a.target = few_target(b, c, a.cols);
   a.min_steps = FEW_MIN_STEPS;
-  const long long chunks = few_chunks(b, c);
-  if (chunks) a.parts = kv_parts(ws, size_t(chunks) * c.n_heads * a.cols);
+  const long long chunks = few_chunks(b, c, a.cols);
+  if (chunks) {
+    const size_t rows = size_t(chunks) * c.n_heads * a.cols;
+    a.parts = kv_parts(ws, rows);
+    a.of_seq = reinterpret_cast<int2*>(static_cast<uint8_t*>(ws) + align256(rows * 8) + align256(rows * c.head_dim * 4));
+  }
   const long long wgs = (chunks ? chunks : b.S) * c.n_heads;
   const long long join_wgs = chunks ? static_cast<long long>(b.S) * c.n_heads * a.cols : 0;
   if (wgs >= (1ll << 23) || join_wgs >= (1ll << 24)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld and %lld work-groups", wgs, join_wgs);
   ProfileScope ps(MOQE_PK_OTHER, st);
   const dim3 grid(static_cast<unsigned>(wgs));
-  const int nc = a.cols <= 16 ? 1 : a.cols <= 32 ? 2 : 4;
   const int extra = kv_extra(at);
-  auto launch = [&](auto dh, auto cols, auto waves) {
-    constexpr int DH = decltype(dh)::value, NC = decltype(cols)::value, W = decltype(waves)::value;
-    const dim3 block(W * 64);
-    if (extra == KV_PLAIN) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, KV_PLAIN>), grid, block, 0, st, a);
-    else if (extra == KV_CAP) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, KV_CAP>), grid, block, 0, st, a);
-    else if (extra == KV_BIAS) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, KV_BIAS>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, W, KV_CAP | KV_BIAS>), grid, block, 0, st, a);
+  auto launch = [&](auto dh, auto cols) {
+    constexpr int DH = decltype(dh)::value, NC = decltype(cols)::value;
+    const dim3 block(FEW_W * 64);
+    if (extra == KV_PLAIN) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_PLAIN>), grid, block, 0, st, a);
+    else if (extra == KV_CAP) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_CAP>), grid, block, 0, st, a);
+    else if (extra == KV_BIAS) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_BIAS>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_CAP | KV_BIAS>), grid, block, 0, st, a);
   };
   auto launch_cols = [&](auto dh) {
-    const std::integral_constant<int, 4> four;
-    const std::integral_constant<int, 8> eight;
-    if (nc == 1) launch(dh, std::integral_constant<int, 1>(), eight);
     if constexpr (decltype(dh)::value < 256) {
-      if (nc == 2) launch(dh, std::integral_constant<int, 2>(), eight);
-      if (nc == 4) launch(dh, four, four);
+      if (a.cols > 16) return launch(dh, std::integral_constant<int, 2>());
     }
+    launch(dh, std::integral_constant<int, 1>());
   };
   if (c.head_dim == 64) launch_cols(std::integral_constant<int, 64>());
   else if (c.head_dim == 128) launch_cols(std::integral_constant<int, 128>());
