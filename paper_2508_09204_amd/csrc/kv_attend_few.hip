@@ -89,6 +89,26 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
   const int j_begin = pl.j + wave, j_end = min(ks.count, pl.j_end);
   const float scale2 = a.sc.scale2;
 
+  kv_bf16x8 qf[NC][KS];
+  KvSight sight[NC];
+  int pos[NC];
+  float slope[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int col = c * 16 + r, i = col / a.group, g = col - i * a.group;
+    const bool in = i < rows;
+    pos[c] = first_pos + i;
+    sight[c] = kv_sight(pos[c], q.len, window);
+    if (EXTRA & KV_BIAS) slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
+    const uint16_t* src = a.q + (q.row0 + i) * a.q_stride + static_cast<long long>(h * a.group + g) * DH + kq * 8;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (in) v = *reinterpret_cast<const uint4*>(src + k * 32);
+      qf[c][k] = __builtin_bit_cast(kv_bf16x8, v);
+    }
+  }
+
   // 64 steps of this wave at a time: lane i looks up step j0 + W i: block (-1: absent, nothing is seen) and scales
   const long long block_bytes = static_cast<long long>(DH) << a.c.bt_log2;
   const int* table = a.b.table + static_cast<long long>(pl.s) * a.b.width;
@@ -121,28 +141,6 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
 #pragma unroll
     for (int x = 0; x < VL; ++x) vc[x] = *reinterpret_cast<const uint4*>(p + x * 1024);
   };
-  look_up(j_begin);
-
-  kv_bf16x8 qf[NC][KS];
-  KvSight sight[NC];
-  int pos[NC];
-  float slope[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int col = c * 16 + r, i = col / a.group, g = col - i * a.group;
-    const bool in = i < rows;
-    pos[c] = first_pos + i;
-    sight[c] = kv_sight(pos[c], q.len, window);
-    if (EXTRA & KV_BIAS) slope[c] = in && a.sc.slopes ? a.sc.slopes[h * a.group + g] * KV_LOG2E : 0.f;
-    const uint16_t* src = a.q + (q.row0 + i) * a.q_stride + static_cast<long long>(h * a.group + g) * DH + kq * 8;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (in) v = *reinterpret_cast<const uint4*>(src + k * 32);
-      qf[c][k] = __builtin_bit_cast(kv_bf16x8, v);
-    }
-  }
-
   kv_f32x4 o[NC][DT];
   float m[NC], l[NC];
 #pragma unroll
@@ -154,12 +152,13 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
   }
 
   bool nan = false;
-  __builtin_amdgcn_s_waitcnt(0);         // the queries have come: else the loop would wait for all loads under way before its first product, every time
+  look_up(j_begin);
   {
     const int bid = max(__builtin_amdgcn_readlane(id, 0), 0);
     load_keys(j_begin, bid);
     load_values(j_begin, bid);
   }
+  kv_wait_loads<2 * KL + VL>();          // the queries and scales have come: else the loop would wait for all loads under way before its first product, every time
   int i = 0;                             // the step's place among those looked up
   for (int j = j_begin; j < j_end; j += W) {
     const int bid = __builtin_amdgcn_readlane(id, i);

@@ -77,6 +77,10 @@ __device__ __forceinline__ float kv_add8(kv_bf16x8 w, float sum) {
   return sum;
 }
 
+// Waits until no more than the N youngest loads are under way.
+template <int N>
+__device__ __forceinline__ void kv_wait_loads() { __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70); }
+
 // What turns q . k into the score's base-2 exponent, and who sees what.
 struct KvScore {
   const float* slopes; const int32_t* prefix;
