@@ -459,7 +459,8 @@ size_t moqe_kv_codes_bytes(const moqe_kv_cache* cache);
  *   block_table : device int32 [S, table_width]: block of tokens j * block_tokens ..  An entry outside [0, n_blocks) stands for an absent block
  *                 (given back, or not needed by this call): nothing is written there, and its tokens are not seen.
  *   kv_len      : device int32 [S]; values are taken into [0, table_width * block_tokens]
- *   cu_rows     : device int32 [S+1] or NULL (then M = S*T); values are taken into [0, M], and rows past the first T of a sequence are not computed */
+ *   cu_rows     : device int32 [S+1] or NULL (then M = S*T); values are taken into [0, M], and rows past the first T of a sequence are not computed
+ * At most 2^30 tokens a sequence, 2^35 in all tables of a call, 2^24 rows a sequence, 2^30 rows. */
 typedef struct moqe_kv_batch {
   const int32_t *block_table, *kv_len, *cu_rows;
   int32_t S, T, M, table_width;
