@@ -346,17 +346,31 @@ __global__ __launch_bounds__(256) void k_kv_rows_join(RowsArgs a) {
   const int col = rt.tile * COLS + c % COLS, row = col / a.group, head = rt.h * a.group + col - row * a.group;
   if (row >= min(q.n, a.b.T)) return;
   const long long step = static_cast<long long>(a.split_tiles) * 8 * COLS;
-  float m = -3e38f;
-  for (int p = 0; p < a.splits; ++p) m = fmaxf(m, a.parts.ml[c + p * step].x);
-  float l = 0.f;
+  float m = -3e38f, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int p = 0; p < a.splits; ++p) {
-    const float2 x = a.parts.ml[c + p * step];
-    const float4 v = *reinterpret_cast<const float4*>(a.parts.o + (c + p * step) * DH + lane * 4);
-    const float f = exp2f(x.x - m);
-    l += x.y * f;
-    o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+  for (int p0 = 0; p0 < a.splits; p0 += 4) {           // four parts under way; past the last one the last again, not counted
+    float2 x[4];
+    float4 v[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const long long at = c + min(p0 + p, a.splits - 1) * step;
+      x[p] = a.parts.ml[at];
+      v[p] = *reinterpret_cast<const float4*>(a.parts.o + at * DH + lane * 4);
+    }
+    float mn = m;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) mn = fmaxf(mn, x[p].x);
+    const float old = exp2f(m - mn);
+    m = mn;
+    l *= old;
+    o.x *= old; o.y *= old; o.z *= old; o.w *= old;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      if (p0 + p >= a.splits) break;
+      const float f = exp2f(x[p].x - m);
+      l += x[p].y * f;
+      o.x += f * v[p].x; o.y += f * v[p].y; o.z += f * v[p].z; o.w += f * v[p].w;
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   uint16_t* dst = a.out + (q.row0 + row) * a.out_stride + static_cast<long long>(head) * DH + lane * 4;
