@@ -536,3 +536,21 @@ def test_append_turns_infinities():
             assert float(d.k_scale[0, 0]) == cache.k_scale[0, 0]
             assert np.array_equal(np.isnan(got), np.isnan(want)) and np.isnan(want).sum() == 2 and (np.abs(want) == 448).sum() >= 6
             assert (got == want)[~np.isnan(want)].mean() > 0.98 and np.array_equal(np.abs(got) == 448, np.abs(want) == 448)
+
+
+def test_attention_of_many_sequences_in_chunks():
+    """More sequences than a wave has lanes, of 1 to 40 chunks, some without rows and one without tokens."""
+    n = 70
+    lens = [1 + (s * 977) % 2600 for s in range(n)]
+    lens[5], lens[66] = 0, 41000
+    _check_attention([0 if s % 9 == 4 else 1 for s in range(n)], lens, 2, 1, 64, 32, seed=610)
+
+
+@pytest.mark.parametrize("rows,lens,heads,kv,dh,bt,masks", [
+    ([8, 3], [3000, 3], 4, 1, 128, 64, {}), ([5], [5000], 6, 1, 64, 128, dict(window=2100, prefix=[700])), ([4, 1, 2], [2500, 1100, 40], 4, 1, 256, 32, dict(cap=8.0)),
+    ([8, 8], [2049, 1056], 4, 1, 128, 32, dict(slopes=True)), ([32], [4100], 1, 1, 128, 64, dict(absent=[(0, 0), (0, 30), (0, 64)])),
+    ([33], [4100], 1, 1, 128, 64, {}), ([17], [1500], 1, 1, 256, 64, {}),
+])
+def test_attention_few_rows_in_chunks(rows, lens, heads, kv, dh, bt, masks):
+    """Up to 32 columns (16 where heads are 256 wide), and one more, on contexts that are cut into chunks."""
+    _check_attention(rows, lens, heads, kv, dh, bt, seed=620, **masks)
