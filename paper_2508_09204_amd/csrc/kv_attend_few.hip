@@ -1,6 +1,7 @@
 // Attention over the 8-bit cache for few rows (decode steps, short continuations): bound by reading the cache once.
 #include "kv_device.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace moqe {
@@ -383,7 +384,16 @@ int few_target(const moqe_kv_batch& b, const moqe_kv_cache& c, int cols) {
   const long long round = at_once / c.n_heads > 0 ? at_once / c.n_heads : 1, rounds = (b.S + round - 1) / round;
   return static_cast<int>(rounds * round - b.S / 2);
 }
-long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c, int cols) {          // chunks at most; 0: one a sequence
+// One chunk a sequence where none can have more than 64 steps, by the table or by the window: eight steps a wave take no longer than half of them and the join.  One / two chunks:
+// one sequence of 2000 tokens 8.4 / 10.8 us, 64 of 1400 17 / 26, 96 of 1900 54 / 62; of 3000 (94 steps) 15.1 / 12.7.
+constexpr int FEW_ONE_CHUNK = 64;
+bool few_one_chunk(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c) {
+  long long most = static_cast<long long>(b.table_width) * c.block_tokens / 32;
+  if (at.window > 0 && !at.prefix) most = std::min(most, (static_cast<long long>(at.window) + b.T + 30) / 32 + 1);
+  return most <= FEW_ONE_CHUNK;
+}
+// Chunks at most that the workspace holds parts of; 0 where a table has no more than 32 steps (from there on the workspace does not depend on how a call is divided).
+long long few_chunks(const moqe_kv_batch& b, const moqe_kv_cache& c, int cols) {
   if (static_cast<long long>(b.table_width) * c.block_tokens / 32 <= FEW_MIN_STEPS) return 0;
   return few_target(b, c, cols) + static_cast<long long>(b.S);
 }
@@ -406,7 +416,7 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   a.cols = b.T * a.group;
   a.target = few_target(b, c, a.cols);
   a.min_steps = FEW_MIN_STEPS;
-  const long long chunks = few_chunks(b, c, a.cols);
+  const long long chunks = few_one_chunk(at, b, c) ? 0 : few_chunks(b, c, a.cols);
   if (chunks) {
     const size_t rows = size_t(chunks) * c.n_heads * a.cols;
     a.parts = kv_parts(ws, rows);
