@@ -417,7 +417,7 @@ int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_atte
   a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
   a.b = kv_batch_args(b);
   a.c = kv_cache_args(c);
-  a.sc = kv_score(at);
+  a.sc = kv_score(at, b, c);
   a.group = at.n_heads / c.n_heads;
   const RowsPlan p = rows_plan(at, b, c);
   if (p.wgs >= (1ll << 24)) return set_error(MOQE_E_SHAPE, "moqe_kv_attention: %lld work-groups", p.wgs);

@@ -32,6 +32,10 @@ MOQE_HD int kv_scale_exponent(uint32_t bits) {
   return e < -120 ? -120 : e > 120 ? 120 : e;
 }
 
+// The window that kernels work with.  One as long as a sequence can be (`tokens`, 2^30 at most) hides nothing: none then.  So the first position of a call's rows (-2^24 at least)
+// less a window stays in 32 bits, here and below.
+inline int kv_window(int window, long long tokens) { return window > 0 && window < tokens ? window : 0; }
+
 // Steps of 32 tokens that the rows at positions first_pos .. of a sequence with len tokens go through: steps of the prefix, then steps from the window's
 // first token on.  Step number j of `count` is tokens 32 * step(j) ...
 struct KvSteps {
@@ -52,5 +56,23 @@ MOQE_HD KvSteps kv_steps(int len, int seen, int first_pos, int window, int prefi
   k.count = all - k.skip;
   return k;
 }
+
+// What a row at position p sees: tokens below `pre` and `span` tokens from `lo` on.
+struct KvSight {
+  int lo;
+  uint32_t span;
+  MOQE_HD bool sees(int t, int pre) const { return uint32_t(t - lo) < span || t < pre; }
+};
+MOQE_HD KvSight kv_sight(int p, int len, int window) {
+  const int hi = len < p + 1 ? len : p + 1, from = window > 0 ? p - window + 1 : 0, lo = from > 0 ? from : 0;
+  return KvSight{lo, uint32_t(hi > lo ? hi - lo : 0)};
+}
+// First tokens t0 of 32-token steps that rows at positions p0 .. p1 see all of, or may see any of.
+struct KvRange {
+  int lo, hi, pre;
+  MOQE_HD bool has(int t0) const { return (t0 >= lo && t0 < hi) || t0 < pre; }
+};
+MOQE_HD KvRange kv_all_see(int p0, int p1, int pre, int window) { return KvRange{window > 0 ? p1 - window + 1 : 0, p0 - 30, pre - 31}; }
+MOQE_HD KvRange kv_some_see(int p0, int p1, int pre, int window) { return KvRange{window > 0 ? p0 - window - 30 : 0, p1 + 1, pre}; }
 
 }  // namespace moqe

@@ -89,9 +89,10 @@ struct KvScore {
   int window;
 };
 constexpr float KV_LOG2E = 1.4426950408889634f;
-inline KvScore kv_score(const moqe_attention& a) {
+inline KvScore kv_score(const moqe_attention& a, const moqe_kv_batch& b, const moqe_kv_cache& c) {
   const bool capped = a.cap > 0.f;
-  return KvScore{a.slopes, a.prefix, a.scale * KV_LOG2E, capped ? a.cap * KV_LOG2E : 0.f, capped ? 2.f * KV_LOG2E * a.scale / a.cap : 0.f, a.window};
+  return KvScore{a.slopes, a.prefix, a.scale * KV_LOG2E, capped ? a.cap * KV_LOG2E : 0.f, capped ? 2.f * KV_LOG2E * a.scale / a.cap : 0.f,
+                 kv_window(a.window, static_cast<long long>(b.table_width) * c.block_tokens)};
 }
 // What a score needs beyond its scale: KV_CAP, KV_BIAS (by distance; also where the scale is not positive, since the kernels take the largest product for the largest score).
 enum : int { KV_PLAIN = 0, KV_CAP = 1, KV_BIAS = 2 };
@@ -107,24 +108,6 @@ __device__ __forceinline__ float kv_extra_score(const KvScore& sc, float d, floa
   if constexpr ((EXTRA & KV_BIAS) != 0) v = fmaf(-slope, fabsf(distance), v);
   return v;
 }
-
-// What a row at position p sees: tokens below `pre` and `span` tokens from `lo` on.
-struct KvSight {
-  int lo;
-  uint32_t span;
-  __device__ __forceinline__ bool sees(int t, int pre) const { return uint32_t(t - lo) < span || t < pre; }
-};
-__device__ __forceinline__ KvSight kv_sight(int p, int len, int window) {
-  const int hi = min(len, p + 1), lo = window > 0 ? max(p - window + 1, 0) : 0;
-  return KvSight{lo, uint32_t(max(hi - lo, 0))};
-}
-// First tokens t0 of 32-token steps that rows at positions p0 .. p1 see all of, or may see any of.
-struct KvRange {
-  int lo, hi, pre;
-  __device__ __forceinline__ bool has(int t0) const { return (t0 >= lo && t0 < hi) || t0 < pre; }
-};
-__device__ __forceinline__ KvRange kv_all_see(int p0, int p1, int pre, int window) { return KvRange{window > 0 ? p1 - window + 1 : 0, p0 - 30, pre - 31}; }
-__device__ __forceinline__ KvRange kv_some_see(int p0, int p1, int pre, int window) { return KvRange{window > 0 ? p0 - window - 30 : 0, p1 + 1, pre}; }
 
 // Bytes of NaN among four codes, as 1 in their lowest bits.
 __device__ __forceinline__ uint32_t kv_nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7; }
