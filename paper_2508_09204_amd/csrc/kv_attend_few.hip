@@ -87,7 +87,7 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
   const KvSteps ks = few_steps(a, pl.s, &q);
   const int rows = min(q.n, a.b.T), first_pos = q.first();
   if (rows == 0) return;
-  const int pre = a.sc.prefix ? min(a.sc.prefix[pl.s], q.len) : 0, window = a.sc.window, last_pos = first_pos + rows - 1;
+  const int pre = a.sc.prefix ? kv_prefix(a.sc.prefix[pl.s], q.len) : 0, window = a.sc.window, last_pos = first_pos + rows - 1;
   const KvRange all_see = kv_all_see(first_pos, last_pos, pre, window);
   const int j_begin = pl.j + wave, j_end = min(ks.count, pl.j_end);
   const float scale2 = a.sc.scale2;

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_ro
   if (i_first >= rows) return;
   const int i_last = min((tile * COLS + COLS - 1) / a.group, rows - 1);
   const int p_first = first_pos + i_first, p_last = first_pos + i_last;
-  const int pre = a.sc.prefix ? min(a.sc.prefix[s], q.len) : 0, window = a.sc.window;
+  const int pre = a.sc.prefix ? kv_prefix(a.sc.prefix[s], q.len) : 0, window = a.sc.window;
   const int seen = min(q.len, max(max(p_last + 1, pre), 0));                   // tokens from here on are seen by no row of the work-group
   const KvSteps ks = kv_steps(q.len, seen, p_first, window, pre);
   const float scale2 = a.sc.scale2;

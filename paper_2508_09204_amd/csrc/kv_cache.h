@@ -36,6 +36,9 @@ MOQE_HD int kv_scale_exponent(uint32_t bits) {
 // less a window stays in 32 bits, here and below.
 inline int kv_window(int window, long long tokens) { return window > 0 && window < tokens ? window : 0; }
 
+// Tokens that every row sees: a device value, taken into its range.
+MOQE_HD int kv_prefix(int prefix, int len) { return prefix < 0 ? 0 : prefix < len ? prefix : len; }
+
 // Steps of 32 tokens that the rows at positions first_pos .. of a sequence with len tokens go through: steps of the prefix, then steps from the window's
 // first token on.  Step number j of `count` is tokens 32 * step(j) ...
 struct KvSteps {
@@ -48,8 +51,7 @@ MOQE_HD KvSteps kv_steps(int len, int seen, int first_pos, int window, int prefi
   int lo = window > 0 ? first_pos + 1 - window : 0;
   lo = lo < 0 ? 0 : lo;
   const int from = lo / 32 < all ? lo / 32 : all;
-  prefix = prefix < len ? prefix : len;
-  int pre = prefix > 0 ? (prefix + 31) / 32 : 0;
+  int pre = (kv_prefix(prefix, len) + 31) / 32;
   pre = pre < all ? pre : all;
   k.pre = pre < from ? pre : from;
   k.skip = from - k.pre;

@@ -24,7 +24,7 @@ int main(int argc, char** argv) {
   for (int len = 0; len <= tokens && len <= 200; len += 9) for (int first = -40; first <= len; first += 3) for (int rows = 1; rows <= 45; rows += 11) {
     if (first + rows > len) continue;                       // rows are the last tokens
     const int last = first + rows - 1, window = kv_window(int(asked), tokens);
-    PREFIX
+    const int pre = kv_prefix(int(prefix), len);
     int seen = last + 1 > pre ? last + 1 : pre;
     seen = seen < 0 ? 0 : seen > len ? len : seen;
     const KvSteps k = kv_steps(len, seen, first, window, pre);
@@ -58,7 +58,7 @@ int main(int argc, char** argv) {
 def probe(tmp_path_factory):
     d = tmp_path_factory.mktemp("bounds")
     src, exe = d / "probe.cpp", d / "probe"
-    src.write_text(PROBE.replace("PREFIX", "const int pre = int(prefix < len ? prefix : len);"))
+    src.write_text(PROBE)
     subprocess.run(["g++", "-O1", "-std=c++17", "-fwrapv", "-I", os.path.join(ROOT, "paper_2508_09204_amd", "csrc"), "-o", str(exe), str(src)], check=True)
 
     def run(*a):
@@ -73,3 +73,9 @@ def probe(tmp_path_factory):
 def test_windows_of_any_size(probe, window, tokens):
     assert probe(window, 0, tokens) == 0
     assert probe(window, 40, tokens) == 0
+
+
+@pytest.mark.parametrize("prefix", [-2 ** 31, -2 ** 31 + 30, -2 ** 31 + 31, -1, 0, 1, 31, 32, 100, 2 ** 30, 2 ** 31 - 1])
+@pytest.mark.parametrize("window", [0, 50])
+def test_prefixes_of_any_size(probe, prefix, window):
+    assert probe(window, prefix, 192) == 0

@@ -13,3 +13,11 @@ def test_windows_that_hide_nothing(window, rows, lens):
     got = tg._check_attention(rows, lens, 4, 2, 64, 32, window=window, seed=800)
     none = tg._check_attention(rows, lens, 4, 2, 64, 32, window=0, seed=800)
     assert (got == none).all()
+
+
+@pytest.mark.parametrize("rows,lens", [([130, 40], [130, 200]), ([2, 1], [40, 300])])
+def test_prefixes_at_the_ends_of_their_range(rows, lens):
+    """A prefix below 0 is none, one past the last token is all of them."""
+    for window in (0, 20):
+        for prefix in (-2 ** 31, -2 ** 31 + 20, -1, 2 ** 31 - 1):
+            tg._check_attention(rows, lens, 4, 2, 64, 32, window=window, prefix=[prefix] * 2, seed=801)
