@@ -51,6 +51,14 @@ __device__ __forceinline__ void angle(const AppendArgs& a, int j, int p, float* 
   *cs = n == 1 || n == 2 ? -u : u;
   *sn = n >= 2 ? -v : v;
 }
+// Which of a slot's pieces the rotation takes: with neighbouring pairs each by itself, in the half layout both or none.  rot is a multiple of 16, so a piece is in or out as a whole.
+struct SlotTurns { bool first, second; };
+__device__ __forceinline__ SlotTurns slot_turns(const AppendArgs& a, int da, int db) {
+  if (a.inter) return SlotTurns{da < a.rot, db < a.rot};
+  const bool both = da < a.rot / 2;
+  return SlotTurns{both, both};
+}
+
 template <int P>
 __device__ __forceinline__ void slot_angles(const AppendArgs& a, int da, int db, int p, float* cs, float* sn) {
 #pragma unroll
@@ -72,20 +80,22 @@ __device__ __forceinline__ float turned(float e, float f, float cs, float sn) {
   const float x = r - fmaf(f, sn, -w);
   return x == x ? x : r;                         // an infinite f leaves NaN
 }
+// Pieces that the rotation leaves out have cos 1 and sin 0, and a partner of 0: an infinity or NaN times that sin would be NaN.
 template <int P, bool EXACT>
-__device__ __forceinline__ void turn(bool inter, const float* cs, const float* sn, float* x) {
+__device__ __forceinline__ void turn(bool inter, const SlotTurns& on, const float* cs, const float* sn, float* x) {
 #pragma unroll
   for (int i = 0; i < P; ++i) {
+    const bool turns = i < P / 2 ? on.first : on.second;
     const int s = i, t = P + i;                                       // half layout
     const int u = i / (P / 2) * P + 2 * (i % (P / 2));                // neighbours
     if (inter) {
       const float e = x[u], f = x[u + 1];
-      x[u] = turned<EXACT>(e, f, cs[i], sn[i]);
-      x[u + 1] = turned<EXACT>(f, e, cs[i], -sn[i]);
+      x[u] = turned<EXACT>(e, turns ? f : 0.f, cs[i], sn[i]);
+      x[u + 1] = turned<EXACT>(f, turns ? e : 0.f, cs[i], -sn[i]);
     } else {
       const float e = x[s], f = x[t];
-      x[s] = turned<EXACT>(e, f, cs[i], sn[i]);
-      x[t] = turned<EXACT>(f, e, cs[i], -sn[i]);
+      x[s] = turned<EXACT>(e, turns ? f : 0.f, cs[i], sn[i]);
+      x[t] = turned<EXACT>(f, turns ? e : 0.f, cs[i], -sn[i]);
     }
   }
 }
@@ -233,6 +243,7 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const BlockToke
   const int slots = (b.hi - b.lo) * SL, tid = threadIdx.x, th = blockDim.x;
   int da, db;
   slot_dims<DH, BF16>(a, tid % SL, &da, &db);
+  const SlotTurns on = slot_turns(a, da, db);
   uint4 pa[NS], pb[NS];
   auto load = [&](int head) {
 #pragma unroll
@@ -265,7 +276,7 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const BlockToke
         piece_values<BF16>(pa[n], x[n]);
         piece_values<BF16>(pb[n], x[n] + P);
         if (a.k_gain) head_norm<DH, BF16, true>(a.k_gain, a.eps, da, db, x[n]);        // a head vector's slots are all in or all out
-        if (a.rot > 0) turn<P, true>(a.inter, cs[n], sn[n], x[n]);
+        if (a.rot > 0) turn<P, true>(a.inter, on, cs[n], sn[n], x[n]);
         largest(x[n], &top, &infinite);
       }
     }
@@ -412,6 +423,7 @@ __global__ __launch_bounds__(TH, TH > 512 ? 1 : BF16 ? 4 : 3) void k_kv_append(A
   if (i >= min(q.n, a.b.T)) return;
   int da, db;
   slot_dims<DH, BF16>(a, tid % SL, &da, &db);
+  const SlotTurns on = slot_turns(a, da, db);
   const long long row = static_cast<long long>(q.row0 + i) * a.qkv_stride, to = (q.row0 + i) * a.q_stride;
   const int h_end = min(a.heads, (split + 1) * a.split_heads);
   constexpr int B = 4;                           // heads in flight
@@ -437,7 +449,7 @@ __global__ __launch_bounds__(TH, TH > 512 ? 1 : BF16 ? 4 : 3) void k_kv_append(A
       piece_values<BF16>(pa[n], x);
       piece_values<BF16>(pb[n], x + P);
       if (a.q_gain) head_norm<DH, BF16, false>(a.q_gain, a.eps, da, db, x);
-      if (a.rot > 0) turn<P, false>(a.inter, cs, sn, x);
+      if (a.rot > 0) turn<P, false>(a.inter, on, cs, sn, x);
       uint16_t* oa = a.q + to + h * DH + da;
       uint16_t* ob = a.q + to + h * DH + db;
       if constexpr (BF16) {

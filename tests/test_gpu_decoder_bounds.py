@@ -1,6 +1,10 @@
 """Arguments at the ends of their ranges, on the GPU against the 64-bit oracle.  Tolerances as in test_gpu_decoder.py."""
+import numpy as np
 import pytest
+import torch
 
+from oracle import decoder_oracle as do
+from paper_2508_09204_amd import binding as mq
 from tests import test_gpu_decoder as tg
 
 pytestmark = pytest.mark.gpu
@@ -21,3 +25,39 @@ def test_prefixes_at_the_ends_of_their_range(rows, lens):
     for window in (0, 20):
         for prefix in (-2 ** 31, -2 ** 31 + 20, -1, 2 ** 31 - 1):
             tg._check_attention(rows, lens, 4, 2, 64, 32, window=window, prefix=[prefix] * 2, seed=801)
+
+
+@pytest.mark.parametrize("dh,rot", [(64, 16), (64, 32), (128, 64), (256, 16), (64, 0)])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+def test_rotation_leaves_the_other_dims_alone(dh, rot, inter, t):
+    """Infinities and NaN in every dim in turn, past the rotation among them: a turned pair spoils itself, what is not turned keeps its value, queries and keys alike.
+    Keys that are not turned have the code of the value itself; the turned ones that are finite may have a neighbour's."""
+    bt, rows = 32, 32
+    rng = np.random.default_rng(dh + rot)
+    host = rng.normal(size=(rows, 3 * dh))
+    for i in range(rows):
+        host[i, i * 7 % dh] = host[i, dh + i * 5 % dh] = (np.inf, -np.inf, np.nan)[i % 3]
+    for i in range(12):                                      # a row each for the dims around the rotation's end
+        host[i, :2 * dh] = rng.normal(size=2 * dh)
+        host[i, (rot - 2 + i) % dh] = host[i, dh + (rot - 2 + i) % dh] = (np.inf, np.nan)[i % 2]
+    x = torch.from_numpy(host).to(tg.DEV, t)
+    f = 100.0 ** (-2.0 * np.arange(rot // 2) / max(1, rot))
+    i32 = dict(dtype=torch.int32, device=tg.DEV)
+    cache, batch = do.Cache(1, 1, bt, dh), mq.KvBatch(torch.zeros((1, 1), **i32), torch.full((1,), rows, **i32), 1, rows, rows)
+    d, q = tg._on_device(cache), torch.empty((rows, dh), dtype=torch.bfloat16, device=tg.DEV)
+    mq.moqe_kv_append(x, 1, mq.Rope(tg.dev(f) if rot else None, rot, inter, 1.125), batch, d, q)
+    tg.sync()
+    with np.errstate(invalid="ignore"):
+        want = do.kv_append(tg.f64(x), 1, cache, np.zeros((1, 1), int), do.sequences(1, rows, rows, [rows], 1, bt), rows, f, rot, inter, 1.125).reshape(rows, dh)
+    got = tg.f64(q)
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    size = np.abs(np.where(np.isfinite(host), host, 0.0)).max()
+    assert (np.abs(got - want)[fine] <= 2.0 ** -8 * np.abs(want)[fine] + 2.0 ** -19 * 2.5 * size).all()
+    at = cache.at["k"][:rows]
+    code, right = d.k.cpu().numpy()[0, 0][at], cache.k[0, 0][at]
+    gv, wv = do.e4m3_value(code), do.e4m3_value(right)
+    same = (code == right) | (np.isnan(gv) & np.isnan(wv)) | ((gv == 0) & (wv == 0))
+    assert float(d.k_scale[0, 0]) == cache.k_scale[0, 0] and np.array_equal(np.isnan(gv), np.isnan(wv))
+    assert same[:, rot:].all() and (np.abs(code.astype(int) - right.astype(int))[~same] == 1).all() and (~same).mean() < 2e-3
