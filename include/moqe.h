@@ -489,7 +489,7 @@ int32_t moqe_kv_append(const void* qkv, int32_t qkv_type, int64_t qkv_stride, in
                        const moqe_kv_batch* batch, const moqe_kv_cache* cache, void* q_out, int64_t q_stride, void* stream);
 
 /* Attention of a call's rows over the cache (after moqe_kv_append: over themselves too).  Query head h reads key head h / (n_heads / cache->n_heads):
- *   a = scale * q . k_t;   cap > 0: a = cap * tanh(a / cap);   slopes: a -= slopes[h] * |p - t|
+ *   a = scale * q . k_t;   cap > 0: a = cap * tanh(a / cap) (an infinite cap is none);   slopes: a -= slopes[h] * |p - t|
  *   out = sum_t softmax(a)_t v_t over the tokens t that the row at position p sees:
  *         t < kv_len, its block present, and (t < prefix, or t <= p and (window <= 0 or p - t < window))
  * A row that sees nothing gives zeros; what lies in places that a row does not see has no influence on it, NaN included.

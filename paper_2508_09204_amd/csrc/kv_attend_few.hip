@@ -434,7 +434,8 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
     if (extra == KV_PLAIN) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_PLAIN>), grid, block, 0, st, a);
     else if (extra == KV_CAP) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_CAP>), grid, block, 0, st, a);
     else if (extra == KV_BIAS) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_BIAS>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_CAP | KV_BIAS>), grid, block, 0, st, a);
+    else if (extra == (KV_CAP | KV_BIAS)) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_CAP | KV_BIAS>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_FAR_CAP>), grid, block, 0, st, a);
   };
   auto launch_cols = [&](auto dh) {
     if constexpr (decltype(dh)::value < 256) {

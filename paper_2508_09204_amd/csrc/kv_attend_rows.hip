@@ -433,14 +433,15 @@ int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_atte
   ProfileScope ps(MOQE_PK_OTHER, st);
   auto launch = [&](auto dh, auto ex) {
     constexpr int DH = decltype(dh)::value, EX = decltype(ex)::value;
-    if (DH == 256) rc = ensure_dynamic_lds(LDSK_ATTEND_ROWS + EX, reinterpret_cast<const void*>(k_kv_attend_rows<DH, EX>), lds, "moqe_kv_attention");
+    if (DH == 256) rc = ensure_dynamic_lds(LDSK_ATTEND_ROWS + (EX == KV_FAR_CAP ? 4 : EX), reinterpret_cast<const void*>(k_kv_attend_rows<DH, EX>), lds, "moqe_kv_attention");
     if (!rc) hipLaunchKernelGGL((k_kv_attend_rows<DH, EX>), grid, block, lds, st, a);
   };
   auto launch_dh = [&](auto dh) {
     if (extra == KV_PLAIN) launch(dh, std::integral_constant<int, KV_PLAIN>());
     else if (extra == KV_CAP) launch(dh, std::integral_constant<int, KV_CAP>());
     else if (extra == KV_BIAS) launch(dh, std::integral_constant<int, KV_BIAS>());
-    else launch(dh, std::integral_constant<int, KV_CAP | KV_BIAS>());
+    else if (extra == (KV_CAP | KV_BIAS)) launch(dh, std::integral_constant<int, KV_CAP | KV_BIAS>());
+    else launch(dh, std::integral_constant<int, KV_FAR_CAP>());
   };
   if (c.head_dim == 64) launch_dh(std::integral_constant<int, 64>());
   else if (c.head_dim == 128) launch_dh(std::integral_constant<int, 128>());

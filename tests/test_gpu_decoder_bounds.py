@@ -54,10 +54,19 @@ def test_rotation_leaves_the_other_dims_alone(dh, rot, inter, t):
     fine = np.isfinite(want)
     assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
     size = np.abs(np.where(np.isfinite(host), host, 0.0)).max()
-    assert (np.abs(got - want)[fine] <= 2.0 ** -8 * np.abs(want)[fine] + 2.0 ** -19 * 2.5 * size).all()
+    assert (np.abs(got[fine] - want[fine]) <= 2.0 ** -8 * np.abs(want[fine]) + 2.0 ** -19 * 2.5 * size).all()
     at = cache.at["k"][:rows]
     code, right = d.k.cpu().numpy()[0, 0][at], cache.k[0, 0][at]
     gv, wv = do.e4m3_value(code), do.e4m3_value(right)
     same = (code == right) | (np.isnan(gv) & np.isnan(wv)) | ((gv == 0) & (wv == 0))
     assert float(d.k_scale[0, 0]) == cache.k_scale[0, 0] and np.array_equal(np.isnan(gv), np.isnan(wv))
     assert same[:, rot:].all() and (np.abs(code.astype(int) - right.astype(int))[~same] == 1).all() and (~same).mean() < 2e-3
+
+
+@pytest.mark.parametrize("cap", [1e-3, 0.5, 30.0, 1e3, 1e4, 1e6, 1e12, 3e38, 1e300])
+@pytest.mark.parametrize("rows,dh", [([1, 1], 128), ([9, 4], 64), ([70, 40], 128), ([40, 70], 256)])
+def test_caps_of_any_size(cap, rows, dh):
+    """Scores far below the cap are the scores, those far above are the cap; past the largest fp32 (1e300) it is infinite, so none."""
+    for q_by in (0.2, 3.0):
+        tg._check_attention(rows, [90, 200], 4, 2, dh, 32, cap=cap, q_by=q_by, seed=802)
+    tg._check_attention(rows, [90, 200], 4, 2, dh, 32, cap=cap, slopes=True, seed=803)
