@@ -594,6 +594,13 @@ def _type_of(t: torch.Tensor, what: str) -> int:
     raise TypeError(f"{what} must be float32 or bfloat16, not {t.dtype}")
 
 
+def _int32(value: int, what: str) -> int:
+    """ctypes would cut a wider integer to its lowest 32 bits."""
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{what} = {value} does not fit in 32 bits")
+    return int(value)
+
+
 def _vector(t: Optional[torch.Tensor], n: int, what: str, dtype=torch.float32) -> Optional[int]:
     """Address of a contiguous tensor of n values that the library reads as `dtype`."""
     if t is None:
@@ -638,7 +645,7 @@ class ResidualNormCall:
                  scale: float = 1.0, post: Optional[Norm] = None, pre: Optional[Norm] = None):
         M, d = residual.shape
         s = _ResidualStep()
-        s.M, s.d, s.gate_rows, s.scale = M, d, gate_rows, scale
+        s.M, s.d, s.gate_rows, s.scale = _int32(M, "M"), _int32(d, "d"), _int32(gate_rows, "gate_rows"), scale
         s.residual_type = _type_of(residual, "residual")
         s.residual, s.residual_stride = _rows(residual, M, d, "residual")
         if y is not None:
@@ -685,7 +692,8 @@ class KvCache:
 
     def c(self) -> _KvCache:
         n_blocks, n_heads = self.k_scale.shape
-        c = _KvCache(None, None, None, None, n_blocks, self.block_tokens, n_heads, self.head_dim)
+        c = _KvCache(None, None, None, None, _int32(n_blocks, "n_blocks"), _int32(self.block_tokens, "block_tokens"), _int32(n_heads, "n_heads"),
+                     _int32(self.head_dim, "head_dim"))
         codes = n_blocks * n_heads * self.block_tokens * self.head_dim
         c.k, c.v = _vector(self.k, codes, "k", torch.uint8), _vector(self.v, codes, "v", torch.uint8)
         c.k_scale, c.v_scale = (_vector(t, n_blocks * n_heads, "scales") for t in (self.k_scale, self.v_scale))
@@ -710,7 +718,8 @@ class KvBatch:
     def c(self) -> _KvBatch:
         width = self.block_table.shape[1]
         return _KvBatch(_vector(self.block_table, self.S * width, "block_table", torch.int32), _vector(self.kv_len, self.S, "kv_len", torch.int32),
-                        _vector(self.cu_rows, self.S + 1, "cu_rows", torch.int32), self.S, self.T, self.M, width)
+                        _vector(self.cu_rows, self.S + 1, "cu_rows", torch.int32), *(_int32(v, n) for v, n in ((self.S, "S"), (self.T, "T"), (self.M, "M"),
+                                                                                                               (width, "table_width"))))
 
 
 @dataclass
@@ -726,7 +735,7 @@ class Rope:
 
     def c(self, head_dim: int) -> _Rope:
         return _Rope(_vector(self.inv_freq, self.rot_dim // 2, "inv_freq", torch.float64), _vector(self.q_gain, head_dim, "q_gain"),
-                     _vector(self.k_gain, head_dim, "k_gain"), self.eps, self.mscale, self.rot_dim, int(self.interleaved))
+                     _vector(self.k_gain, head_dim, "k_gain"), self.eps, self.mscale, _int32(self.rot_dim, "rot_dim"), int(self.interleaved))
 
 
 @dataclass
@@ -741,7 +750,7 @@ class Attention:
 
     def c(self, S: int) -> _Attention:
         return _Attention(_vector(self.slopes, self.n_heads, "slopes"), _vector(self.prefix, S, "prefix", torch.int32), self.scale, self.cap,
-                          self.n_heads, self.window)
+                          _int32(self.n_heads, "n_heads"), _int32(self.window, "window"))
 
 
 class KvAppendCall:
@@ -752,7 +761,7 @@ class KvAppendCall:
         self._keep = (qkv, rope, batch, cache, q_out)
         qp, qs = _rows(qkv, batch.M, (n_heads + 2 * cache.k_scale.shape[1]) * cache.head_dim, "qkv")
         op, os_ = _rows(q_out, batch.M, n_heads * cache.head_dim, "q_out", torch.bfloat16)
-        self._args = (qp, _type_of(qkv, "qkv"), qs, n_heads, *(C.byref(x) for x in self._c), op, os_)
+        self._args = (qp, _type_of(qkv, "qkv"), qs, _int32(n_heads, "n_heads"), *(C.byref(x) for x in self._c), op, os_)
 
     def __call__(self, stream: Optional[int] = None) -> None:
         rc = lib.moqe_kv_append(*self._args, _stream() if stream is None else stream)

@@ -1,0 +1,39 @@
+"""What the binding of the decoder layer's operators does with its arguments before the library sees them (no GPU; dry-run mode where a call is made)."""
+import pytest
+import torch
+
+BF, I32 = torch.bfloat16, torch.int32
+
+
+@pytest.fixture(scope="module")
+def mq():
+    from paper_2508_09204_amd import binding
+    binding.moqe_set_dry_run(True)
+    yield binding
+    binding.moqe_set_dry_run(False)
+
+
+def z(*s, t=torch.float32):
+    return torch.zeros(s, dtype=t)
+
+
+@pytest.mark.parametrize("wide", [2 ** 32 + 5, 2 ** 31, -2 ** 31 - 1])
+def test_integers_that_do_not_fit_are_refused(mq, wide):
+    cache = mq.KvCache.empty(3, 2, 32, 64, "cpu")
+    batch = mq.KvBatch(z(2, 4, t=I32), z(2, t=I32), 2, 1, 2)
+    q, out = z(2, 256, t=BF), z(2, 256, t=BF)
+    with pytest.raises(ValueError, match="window"):
+        mq.KvAttentionCall(q, mq.Attention(4, 0.1, window=wide), batch, cache, out)
+    with pytest.raises(ValueError, match="window"):
+        mq.moqe_kv_attention_workspace_bytes(mq.Attention(4, 0.1, window=wide), batch, cache)
+    with pytest.raises(ValueError, match="n_heads"):
+        mq.KvAttentionCall(q, mq.Attention(wide, 0.1), batch, cache, out)
+    with pytest.raises(ValueError, match="T = "):
+        mq.KvBatch(z(2, 4, t=I32), z(2, t=I32), 2, wide, 2).c()
+    with pytest.raises(ValueError, match="M = "):
+        mq.KvBatch(z(2, 4, t=I32), z(2, t=I32), 2, 1, wide).c()
+    with pytest.raises(ValueError, match="rot_dim"):
+        mq.Rope(None, wide).c(64)
+    with pytest.raises(ValueError, match="gate_rows"):
+        mq.ResidualNormCall(z(2, 8), z(2, 8), z(2, 8, t=BF), gate_rows=wide)
+    assert mq.Attention(4, 0.1, window=2 ** 31 - 1).c(2).window == 2 ** 31 - 1
