@@ -614,7 +614,7 @@ def _rows(t: torch.Tensor, M: int, width: int, what: str, dtype=None):
     """Address and row stride of M rows of `width` values; trailing dimensions of a row have to be dense."""
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    if t.dim() < 2 or t.shape[0] != M or t[0:1].numel() != width:
+    if t.dim() < 2 or t.shape[0] != M or t.shape[1:].numel() != width:
         raise ValueError(f"{what} must have {M} rows of {width} values, got {tuple(t.shape)}")
     n = 1
     for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):

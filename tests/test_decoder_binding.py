@@ -37,3 +37,16 @@ def test_integers_that_do_not_fit_are_refused(mq, wide):
     with pytest.raises(ValueError, match="gate_rows"):
         mq.ResidualNormCall(z(2, 8), z(2, 8), z(2, 8, t=BF), gate_rows=wide)
     assert mq.Attention(4, 0.1, window=2 ** 31 - 1).c(2).window == 2 ** 31 - 1
+
+
+def test_calls_without_rows_do_nothing(mq):
+    """No rows, or no sequences: accepted, as the library accepts them."""
+    cache = mq.KvCache.empty(3, 2, 32, 64, "cpu")
+    for S in (0, 2):
+        batch = mq.KvBatch(z(S, 4, t=I32), z(S, t=I32), S, 1, 0, z(S + 1, t=I32))
+        mq.moqe_kv_append(z(0, 512, t=BF), 4, mq.Rope(z(32, t=torch.float64), 64), batch, cache, z(0, 256, t=BF))
+        mq.moqe_kv_attention(z(0, 256, t=BF), mq.Attention(4, 0.1), batch, cache, z(0, 4, 64, t=BF))
+    for gate in (None, z(0, 8)):
+        mq.moqe_residual_norm(z(0, 8), z(0, 8), z(0, 8, t=BF), z(0, 8), gate, 3 if gate is not None else 0, pre=mq.Norm("rms", 1e-5, z(8)))
+    with pytest.raises(ValueError):
+        mq.moqe_kv_attention(z(0, 128, t=BF), mq.Attention(4, 0.1), batch, cache, z(0, 256, t=BF))      # rows of another width
