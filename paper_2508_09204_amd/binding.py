@@ -611,7 +611,7 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str, dtype=torch.float32) -
 
 
 def _rows(t: torch.Tensor, M: int, width: int, what: str, dtype=None):
-    """Address and row stride of M rows of `width` values; trailing dimensions of a row have to be dense."""
+    """Address and row stride of M rows of `width` values; trailing dimensions of a row have to be dense.  A single row (or none) has no stride of its own."""
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
     if t.dim() < 2 or t.shape[0] != M or t.shape[1:].numel() != width:
@@ -621,7 +621,7 @@ def _rows(t: torch.Tensor, M: int, width: int, what: str, dtype=None):
         if size > 1 and stride != n:
             raise ValueError(f"the values of a row of {what} must be dense")
         n *= size
-    return t.data_ptr(), t.stride(0) if M > 1 else max(t.stride(0), width)
+    return t.data_ptr(), t.stride(0) if M > 1 else width
 
 
 @dataclass

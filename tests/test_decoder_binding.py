@@ -50,3 +50,20 @@ def test_calls_without_rows_do_nothing(mq):
         mq.moqe_residual_norm(z(0, 8), z(0, 8), z(0, 8, t=BF), z(0, 8), gate, 3 if gate is not None else 0, pre=mq.Norm("rms", 1e-5, z(8)))
     with pytest.raises(ValueError):
         mq.moqe_kv_attention(z(0, 128, t=BF), mq.Attention(4, 0.1), batch, cache, z(0, 256, t=BF))      # rows of another width
+
+
+def aligned(nbytes):
+    t = torch.zeros(nbytes + 256, dtype=torch.uint8)
+    at = -t.data_ptr() % 256
+    return t[at:at + nbytes]
+
+
+def test_a_single_row_of_a_wider_buffer(mq):
+    """One row has no stride that could be misaligned, whatever the buffer it lies in."""
+    cache = mq.KvCache.empty(3, 2, 32, 64, "cpu")
+    batch = mq.KvBatch(z(1, 4, t=I32), z(1, t=I32), 1, 1, 1)
+    row = lambda n: aligned(2 * 5 * (n + 3)).view(BF).view(5, n + 3)[:1, :n]  # noqa: E731
+    mq.moqe_kv_append(row(512), 4, mq.Rope(z(32, t=torch.float64), 64), batch, cache, row(256))
+    mq.moqe_kv_attention(row(256), mq.Attention(4, 0.1), batch, cache, row(256))
+    r = row(256)
+    mq.moqe_residual_norm(None, r, row(256), r)
