@@ -336,7 +336,12 @@ def moqe_version() -> str:
     return lib.moqe_version().decode()
 
 
+_dry_run = False
+
+
 def moqe_set_dry_run(on: bool) -> None:
+    global _dry_run
+    _dry_run = bool(on)
     lib.moqe_set_dry_run(int(on))
 
 
@@ -624,6 +629,20 @@ def _rows(t: torch.Tensor, M: int, width: int, what: str, dtype=None):
     return t.data_ptr(), t.stride(0) if M > 1 else width
 
 
+class _DeviceCall:
+    """A call whose tensors the kernels read and write: all on one device.  Host memory passes the checks of a dry run only."""
+
+    def _hold(self, *tensors) -> None:
+        devices = {t.device for t in tensors if t is not None}
+        if len(devices) > 1:
+            raise ValueError(f"tensors on different devices: {', '.join(sorted(map(str, devices)))}")
+        self._host = any(d.type != "cuda" for d in devices)
+
+    def _on_device(self) -> None:
+        if self._host and not _dry_run:
+            raise ValueError("the library reads and writes device memory, these tensors are not on the GPU")
+
+
 @dataclass
 class Norm:
     """kind "rms" or "layer"; gain and offset fp32 [d] or None."""
@@ -636,7 +655,7 @@ class Norm:
         return _Norm(_vector(self.gain, d, "gain"), _vector(self.offset, d, "offset"), NORM_KINDS[self.kind], self.eps)
 
 
-class ResidualNormCall:
+class ResidualNormCall(_DeviceCall):
     """moqe_residual_norm with its arguments marshalled once; calling it only enqueues the work.
     y [M, d] fp32 or bf16 or None, residual [M, d] fp32 or bf16, out bf16 [M, d] or None, residual_out like residual (may be it) or None."""
 
@@ -659,10 +678,12 @@ class ResidualNormCall:
         s.post = post.c(d) if post is not None else _Norm()
         s.pre = pre.c(d) if pre is not None else _Norm()
         self._keep = (y, residual, out, residual_out, gate, post, pre)
+        self._hold(y, residual, out, residual_out, gate, *(v for n in (post, pre) if n is not None for v in (n.gain, n.offset)))
         self._step = s
         self._arg = C.byref(s)
 
     def __call__(self, stream: Optional[int] = None) -> None:
+        self._on_device()
         rc = lib.moqe_residual_norm(self._arg, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
@@ -690,6 +711,9 @@ class KvCache:
         scales = [torch.empty((n_blocks, n_heads), dtype=torch.float32, device=device) for _ in range(2)]
         return cls(*codes, *scales, block_tokens, head_dim)
 
+    def tensors(self):
+        return self.k, self.v, self.k_scale, self.v_scale
+
     def c(self) -> _KvCache:
         n_blocks, n_heads = self.k_scale.shape
         c = _KvCache(None, None, None, None, _int32(n_blocks, "n_blocks"), _int32(self.block_tokens, "block_tokens"), _int32(n_heads, "n_heads"),
@@ -714,6 +738,9 @@ class KvBatch:
     T: int
     M: int
     cu_rows: Optional[torch.Tensor] = None
+
+    def tensors(self):
+        return self.block_table, self.kv_len, self.cu_rows
 
     def c(self) -> _KvBatch:
         width = self.block_table.shape[1]
@@ -753,17 +780,19 @@ class Attention:
                           _int32(self.n_heads, "n_heads"), _int32(self.window, "window"))
 
 
-class KvAppendCall:
+class KvAppendCall(_DeviceCall):
     """moqe_kv_append with its arguments marshalled once.  qkv [M, (n_heads + 2 kv heads) * head_dim] fp32 or bf16, q_out bf16 [M, n_heads * head_dim]."""
 
     def __init__(self, qkv: torch.Tensor, n_heads: int, rope: Rope, batch: KvBatch, cache: KvCache, q_out: torch.Tensor):
         self._c = (rope.c(cache.head_dim), batch.c(), cache.c())
         self._keep = (qkv, rope, batch, cache, q_out)
+        self._hold(qkv, q_out, rope.inv_freq, rope.q_gain, rope.k_gain, *batch.tensors(), *cache.tensors())
         qp, qs = _rows(qkv, batch.M, (n_heads + 2 * cache.k_scale.shape[1]) * cache.head_dim, "qkv")
         op, os_ = _rows(q_out, batch.M, n_heads * cache.head_dim, "q_out", torch.bfloat16)
         self._args = (qp, _type_of(qkv, "qkv"), qs, _int32(n_heads, "n_heads"), *(C.byref(x) for x in self._c), op, os_)
 
     def __call__(self, stream: Optional[int] = None) -> None:
+        self._on_device()
         rc = lib.moqe_kv_append(*self._args, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
@@ -778,7 +807,7 @@ def moqe_kv_attention_workspace_bytes(attn: Attention, batch: KvBatch, cache: Kv
     return lib.moqe_kv_attention_workspace_bytes(C.byref(a), C.byref(b), C.byref(c))
 
 
-class KvAttentionCall:
+class KvAttentionCall(_DeviceCall):
     """moqe_kv_attention with its arguments marshalled once and a workspace of its own.  q, out bf16 [M, n_heads * head_dim]."""
 
     def __init__(self, q: torch.Tensor, attn: Attention, batch: KvBatch, cache: KvCache, out: torch.Tensor,
@@ -789,11 +818,13 @@ class KvAttentionCall:
             workspace = _workspace(lib.moqe_kv_attention_workspace_bytes(*refs), q.device)
         self.workspace = workspace
         self._keep = (q, attn, batch, cache, out)
+        self._hold(q, out, workspace, attn.slopes, attn.prefix, *batch.tensors(), *cache.tensors())
         qp, qs = _rows(q, batch.M, attn.n_heads * cache.head_dim, "q", torch.bfloat16)
         op, os_ = _rows(out, batch.M, attn.n_heads * cache.head_dim, "out", torch.bfloat16)
         self._args = (qp, qs, *refs, op, os_, _ptr(workspace), workspace.numel())
 
     def __call__(self, stream: Optional[int] = None) -> None:
+        self._on_device()
         rc = lib.moqe_kv_attention(*self._args, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)

@@ -67,3 +67,41 @@ def test_a_single_row_of_a_wider_buffer(mq):
     mq.moqe_kv_attention(row(256), mq.Attention(4, 0.1), batch, cache, row(256))
     r = row(256)
     mq.moqe_residual_norm(None, r, row(256), r)
+
+
+def _calls(mq, at):
+    """One call of each kind, the argument named `at` on another device than the others."""
+    def d(name, t):
+        return t.to("meta") if name == at else t
+    cache = mq.KvCache(d("k", z(3, 2, 2048, t=torch.uint8)), z(3, 2, 2048, t=torch.uint8), z(3, 2), d("v_scale", z(3, 2)), 32, 64)
+    batch = mq.KvBatch(d("table", z(2, 4, t=I32)), d("kv_len", z(2, t=I32)), 2, 1, 2, d("cu", z(3, t=I32)))
+    rope = mq.Rope(d("inv_freq", z(32, t=torch.float64)), 64, q_gain=d("gain", z(64)))
+    attn = mq.Attention(4, 0.1, slopes=d("slopes", z(4)), prefix=d("prefix", z(2, t=I32)))
+    return [lambda: mq.KvAppendCall(d("qkv", z(2, 512)), 4, rope, batch, cache, d("q", z(2, 256, t=BF))),
+            lambda: mq.KvAttentionCall(d("q", z(2, 256, t=BF)), attn, batch, cache, z(2, 256, t=BF), d("ws", aligned(1 << 20))),
+            lambda: mq.ResidualNormCall(d("y", z(2, 8)), z(2, 8), z(2, 8, t=BF), gate=d("gate", z(8)), pre=mq.Norm("layer", 1e-5, z(8), d("offset", z(8))))]
+
+
+@pytest.mark.parametrize("at,which", [(n, [0, 1]) for n in ("k", "v_scale", "table", "kv_len", "cu", "q")] + [(n, [0]) for n in ("inv_freq", "gain", "qkv")] +
+                         [(n, [1]) for n in ("slopes", "prefix", "ws")] + [(n, [2]) for n in ("y", "gate", "offset")])
+def test_tensors_on_different_devices_are_refused(mq, at, which):
+    for i, make in enumerate(_calls(mq, at)):
+        if i in which:
+            with pytest.raises(ValueError, match="devices"):
+                make()
+        else:
+            make()
+
+
+def test_host_memory_is_for_dry_runs_only(mq):
+    """Outside a dry run an address on the host would go to a kernel."""
+    calls = [make() for make in _calls(mq, None)]
+    for call in calls:
+        call()
+    mq.moqe_set_dry_run(False)
+    try:
+        for call in calls:
+            with pytest.raises(ValueError, match="device memory"):
+                call()
+    finally:
+        mq.moqe_set_dry_run(True)
