@@ -20,9 +20,11 @@ struct FewArgs {
 struct FewPlan {
   int s, first, chunks, j, j_end;          // sequence, number of its first chunk, its chunks, steps of this one
 };
-__device__ __forceinline__ KvSteps few_steps(const FewArgs& a, int s, KvSeq* q) {
+__device__ __forceinline__ KvSteps few_steps(const FewArgs& a, int s, KvSeq* q, int* seen) {
   *q = kv_seq(a.b, s, a.c.bt_log2);
-  return kv_steps(q->len, q->n > 0 ? q->len : 0, q->first(), a.sc.window, a.sc.prefix ? a.sc.prefix[s] : 0);
+  const int pre = a.sc.prefix ? kv_prefix(a.sc.prefix[s], q->len) : 0, rows = min(q->n, a.b.T);
+  *seen = rows > 0 ? min(q->len, max(q->first() + rows, pre)) : 0;             // tokens from here on are seen by no row: nothing of them may be read into a sum
+  return kv_steps(q->len, max(*seen, 0), q->first(), a.sc.window, pre);
 }
 // The sequence that chunk number `w` falls into.  False: there is no such chunk.
 __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, FewPlan* p) {
@@ -30,7 +32,8 @@ __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, FewPlan* p) {
   int total = 0;
   for (int base = 0; base < S; base += 64) {
     KvSeq q;
-    total += base + lane < S ? few_steps(a, base + lane, &q).count : 0;
+    int seen;
+    total += base + lane < S ? few_steps(a, base + lane, &q, &seen).count : 0;
   }
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
@@ -38,7 +41,8 @@ __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, FewPlan* p) {
   int before = 0;
   for (int base = 0; base < S; base += 64) {
     KvSeq q;
-    const int s = base + lane, count = s < S ? few_steps(a, s, &q).count : 0;
+    int seen;
+    const int s = base + lane, count = s < S ? few_steps(a, s, &q, &seen).count : 0;
     const int n = s < S ? max(1, (count + steps - 1) / steps) : 0;
     int upto = n;                                   // inclusive sum over the lanes
 #pragma unroll
@@ -84,7 +88,8 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
     pl = FewPlan{w, w, 1, 0, 1 << 30};
   }
   KvSeq q;
-  const KvSteps ks = few_steps(a, pl.s, &q);
+  int seen;
+  const KvSteps ks = few_steps(a, pl.s, &q, &seen);
   const int rows = min(q.n, a.b.T), first_pos = q.first();
   if (rows == 0) return;
   const int pre = a.sc.prefix ? kv_prefix(a.sc.prefix[pl.s], q.len) : 0, window = a.sc.window, last_pos = first_pos + rows - 1;
@@ -225,7 +230,7 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
     if (!full) {                         // values that are NaN must not reach rows that do not see them: 0 * NaN would
 #pragma unroll
       for (int x = 0; x < VL; ++x) {
-        vc[x] = kv_before(vc[x], t0 + 4 * kq, q.len);
+        vc[x] = kv_before(vc[x], t0 + 4 * kq, seen);
         nan |= __ballot(kv_nan_bytes(vc[x]) != 0) != 0;
         vc[x] = kv_without_nan(vc[x]);
       }

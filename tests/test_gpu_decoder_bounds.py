@@ -70,3 +70,32 @@ def test_caps_of_any_size(cap, rows, dh):
     for q_by in (0.2, 3.0):
         tg._check_attention(rows, [90, 200], 4, 2, dh, 32, cap=cap, q_by=q_by, seed=802)
     tg._check_attention(rows, [90, 200], 4, 2, dh, 32, cap=cap, slopes=True, seed=803)
+
+
+@pytest.mark.parametrize("T,heads,dh", [(1, 4, 64), (4, 4, 128), (8, 8, 64), (3, 4, 256), (40, 4, 64)])
+@pytest.mark.parametrize("prefix", [None, 20])
+def test_rows_past_the_call_s_own_and_their_tokens(T, heads, dh, prefix):
+    """Sequences with more rows than the call computes: the tokens of the others, never stored, have no influence, whatever their blocks hold."""
+    rng = np.random.default_rng(T)
+    bt, H, rows, lens = 32, 2, [T + 150, 1, T + 40], [700, 90, T + 40]
+    table, n_blocks = tg._lay_out(rng, lens, bt)
+    cache = tg._random_cache(rng, n_blocks, H, bt, dh)
+    for s, (n, L) in enumerate(zip(rows, lens)):
+        stored = L - n + min(n, T)
+        for b in range(-(-stored // bt), -(-L // bt)):
+            for which in ("k", "v"):
+                cache.codes(which)[table[s, b]] = 0x7f if b % 2 else 0x55
+                cache.scales(which)[table[s, b]] = (np.nan, np.inf)[s % 2]
+    cu = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    M = int(cu[-1])
+    seqs = do.sequences(len(rows), T, M, lens, table.shape[1], bt, cu)
+    batch = mq.KvBatch(tg.dev(table), tg.dev(np.array(lens, dtype=np.int32)), len(rows), T, M, tg.dev(cu))
+    q = tg.dev(rng.normal(size=(M, heads * dh)), torch.bfloat16)
+    out = torch.full_like(q, 7.0)
+    pre = None if prefix is None else np.full(len(rows), prefix, dtype=np.int32)
+    mq.moqe_kv_attention(q, mq.Attention(heads, dh ** -0.5, prefix=None if pre is None else tg.dev(pre)), batch, tg._on_device(cache), out)
+    tg.sync()
+    want, size = do.kv_attention(tg.f64(q), heads, cache, table, seqs, T, dh ** -0.5, prefix=pre)
+    want, size, got = want.reshape(M, -1), size.reshape(M, -1), tg.f64(out)
+    done = ~np.isnan(want)
+    assert done.any() and (np.abs(got[done] - want[done]) <= tg._attention_tol(want, size)[done]).all() and (got[~done] == 7.0).all()
