@@ -72,8 +72,11 @@ __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, FewPlan* p) {
 // likewise.  It keeps its own running maximum and sum for the NC * 16 columns (row i, query head g: column i * group + g); the waves' results are joined in LDS.
 // Bound by reading the cache: 2 sequences of 131000 tokens, 8 key heads of 128 (537 MB), 98 us, 5.5 TB/s; 64 of up to 8000, 4 key heads (251 MB), 56 us with the join; short ones by
 // the trips to memory that wait for one another (lengths, block table, codes): one token on 63 tokens 4.8 us.
+// PAIR, up to eight columns: the other eight hold the same queries, hence the same scores, and take what the rounding of the weights to bf16 left, as weights of their own.  One
+// product does for both, and the error against 64 bits is that of the rounded result alone (one token on 600: 0.0021 -> 0.0017 of the outputs' size in the mean square).  For 9 to 32
+// columns that would take a second product, 2 to 7 % of the time: their weights are rounded to bf16, as in the kernel for many rows.
 constexpr int FEW_W = 8;
-template <int DH, int NC, int EXTRA>
+template <int DH, int NC, bool PAIR, int EXTRA>
 __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv_attend_few(FewArgs a) {
   constexpr int W = FEW_W, KS = DH / 32, DT = DH / 16, KL = DH / 64, VL = DH / 32;
   constexpr int PAD = DH + 4;
@@ -103,7 +106,7 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
   float slope[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const int col = c * 16 + r, i = col / a.group, g = col - i * a.group;
+    const int col = PAIR ? r & 7 : c * 16 + r, i = col / a.group, g = col - i * a.group;
     const bool in = i < rows;
     pos[c] = first_pos + i;
     sight[c] = kv_sight(pos[c], q.len, window);
@@ -159,6 +162,7 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
     for (int d = 0; d < DT; ++d) o[c][d] = kv_f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  const float less = PAIR && r >= 8 ? -1.f : 0.f;
   bool nan = false;
   look_up(j_begin);
   {
@@ -223,8 +227,10 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          pf[c][4 * t + x] = static_cast<__bf16>(__builtin_amdgcn_exp2f(EXTRA ? s[t][c][x] - m[c] : fmaf(s[t][c][x], scale2, -m[c])));
+        for (int x = 0; x < 4; ++x) {
+          const float weight = __builtin_amdgcn_exp2f(EXTRA ? s[t][c][x] - m[c] : fmaf(s[t][c][x], scale2, -m[c]));
+          pf[c][4 * t + x] = static_cast<__bf16>(PAIR ? fmaf(less, static_cast<float>(static_cast<__bf16>(weight)), weight) : weight);
+        }
       l[c] = kv_add8(pf[c], l[c]);
     }
     if (!full) {                         // values that are NaN must not reach rows that do not see them: 0 * NaN would
@@ -252,6 +258,7 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
   for (int c = 0; c < NC; ++c) {
     l[c] += __shfl_xor(l[c], 16);
     l[c] += __shfl_xor(l[c], 32);
+    if (PAIR) l[c] += __shfl_xor(l[c], 8);
     if (kq == 0) ml[wave][c * 16 + r] = make_float2(m[c], l[c]);
   }
   __syncthreads();
@@ -286,6 +293,11 @@ __global__ __launch_bounds__(FEW_W * 64, NC == 1 && DH <= 128 ? 4 : 1) void k_kv
       float y[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) y[e] = ((obuf[0][oc][d0 + e] + obuf[1][oc][d0 + e]) + obuf[2][oc][d0 + e]) + obuf[3][oc][d0 + e];
+      if (PAIR) {                              // row < rows: oc is below 8
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          y[e] += ((obuf[0][oc + 8][d0 + e] + obuf[1][oc + 8][d0 + e]) + obuf[2][oc + 8][d0 + e]) + obuf[3][oc + 8][d0 + e];
+      }
       if (pl.chunks == 1) {
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
         uint16_t* dst = a.out + (q.row0 + row) * a.out_stride + static_cast<long long>(h * a.group + g) * DH + d0;
@@ -433,20 +445,22 @@ int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_atten
   ProfileScope ps(MOQE_PK_OTHER, st);
   const dim3 grid(static_cast<unsigned>(wgs));
   const int extra = kv_extra(at);
-  auto launch = [&](auto dh, auto cols) {
+  auto launch = [&](auto dh, auto cols, auto pair) {
     constexpr int DH = decltype(dh)::value, NC = decltype(cols)::value;
+    constexpr bool PAIR = decltype(pair)::value;
     const dim3 block(FEW_W * 64);
-    if (extra == KV_PLAIN) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_PLAIN>), grid, block, 0, st, a);
-    else if (extra == KV_CAP) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_CAP>), grid, block, 0, st, a);
-    else if (extra == KV_BIAS) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_BIAS>), grid, block, 0, st, a);
-    else if (extra == (KV_CAP | KV_BIAS)) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_CAP | KV_BIAS>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, KV_FAR_CAP>), grid, block, 0, st, a);
+    if (extra == KV_PLAIN) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, PAIR, KV_PLAIN>), grid, block, 0, st, a);
+    else if (extra == KV_CAP) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, PAIR, KV_CAP>), grid, block, 0, st, a);
+    else if (extra == KV_BIAS) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, PAIR, KV_BIAS>), grid, block, 0, st, a);
+    else if (extra == (KV_CAP | KV_BIAS)) hipLaunchKernelGGL((k_kv_attend_few<DH, NC, PAIR, KV_CAP | KV_BIAS>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv_attend_few<DH, NC, PAIR, KV_FAR_CAP>), grid, block, 0, st, a);
   };
   auto launch_cols = [&](auto dh) {
     if constexpr (decltype(dh)::value < 256) {
-      if (a.cols > 16) return launch(dh, std::integral_constant<int, 2>());
+      if (a.cols > 16) return launch(dh, std::integral_constant<int, 2>(), std::false_type());
     }
-    launch(dh, std::integral_constant<int, 1>());
+    if (a.cols > 8) launch(dh, std::integral_constant<int, 1>(), std::false_type());
+    else launch(dh, std::integral_constant<int, 1>(), std::true_type());
   };
   if (c.head_dim == 64) launch_cols(std::integral_constant<int, 64>());
   else if (c.head_dim == 128) launch_cols(std::integral_constant<int, 128>());
