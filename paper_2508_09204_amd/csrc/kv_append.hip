@@ -270,12 +270,16 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const BlockToke
     float x[NS][2 * P];
     float top = 0.f;
     bool infinite = false;
+    // The gains are read again for every head: held through the loop, which they would be if the address were known to stay, they are the registers that spill (16 x 256 rows in bf16
+    // with heads of 256, blocks of 128: 296 us and 1044 bytes of scratch a lane, so 58 and none).
+    const float* gain = a.k_gain;
+    asm("" : "+s"(gain));
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
       if (n * th + tid < slots) {
         piece_values<BF16>(pa[n], x[n]);
         piece_values<BF16>(pb[n], x[n] + P);
-        if (a.k_gain) head_norm<DH, BF16, true>(a.k_gain, a.eps, da, db, x[n]);        // a head vector's slots are all in or all out
+        if (gain) head_norm<DH, BF16, true>(gain, a.eps, da, db, x[n]);        // a head vector's slots are all in or all out
         if (a.rot > 0) turn<P, true>(a.inter, on, cs[n], sn[n], x[n]);
         largest(x[n], &top, &infinite);
       }
