@@ -495,10 +495,17 @@ int32_t moqe_kv_append(const void* qkv, int32_t qkv_type, int64_t qkv_stride, in
  * A row that sees nothing gives zeros; what lies in places that a row does not see has no influence on it, NaN included.
  *   q, out : bf16 rows of n_heads * head_dim, 16-byte aligned, row strides multiples of 8 elements
  *   slopes : device float [n_heads] or NULL (linear biases by distance);  prefix: device int32 [S] or NULL (tokens that every row of the sequence sees)
- * Arithmetic: keys and values are exact in bf16; products on bf16 matrix cores with fp32 accumulation; scores, softmax and sums in fp32; the weights
- * exp(a - max) are rounded to bf16 before their product with the values (as are q and out: 2^-8 of a value at most, errors that average out over the tokens).
- * Sums run in an order that depends on sizes only (deterministic).  Few rows: the tokens are divided over work-groups by their number on the
- * device, and a second launch joins the parts; workspace as the query says, 256-byte aligned. */
+ *   window : one of at least table_width * block_tokens hides nothing;  prefix: values below 0 are 0, those past kv_len all of its tokens
+ * Arithmetic: keys and values are exact in bf16; products on bf16 matrix cores with fp32 accumulation; scores, softmax and sums in fp32.  Up to eight columns (T rows times
+ * query heads of a key head) the weights exp(a - max) go into their product with the values in two bf16 pieces, and the result's rounding to bf16 is what is left of the error; with more
+ * columns they are rounded to bf16, 2^-8 of a weight at most, errors that average out over the tokens (0.0020 of the outputs' size in the mean square, where 0.0017 is the result's rounding).
+ * The same call gives the same bits.  A sequence's bits may differ beside other sequences or with a wider table: how its tokens are divided over work-groups depends on S, T, the head counts
+ * and table_width, and where columns are few (up to 32, 16 with heads of 256) on all lengths of the call too.  Divided tokens are joined in a second launch, from the workspace that
+ * the query asks for, 256-byte aligned.
+ * T decides for all sequences of a call which kernel they take.  Single rows beside a prompt in one call go through their whole context in one work-group each: 63 on up to 8000 tokens
+ * beside 512 rows, 28 heads on 4 of 128, 315 us, in a call of their own before the prompt's 74 together; one on 131000 beside 512, 32 heads on 8, 1376 and 77.  So decode rows and prompts
+ * belong into two calls.
+ * Refused besides: launches of 2^32 threads (of few columns 2^23 pairs of a sequence and key head, or 2^24 of a sequence, query head and row of T; of many 2^31 of a row and query head). */
 typedef struct moqe_attention {
   const float* slopes; const int32_t* prefix;
   float scale, cap;

@@ -400,7 +400,7 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, const BlockTo
 // Work-groups of the keys (one for each block a sequence can touch and group of heads), of the values (one for each block and head), then of the queries (a row tile
 // and some heads each).  At most TH threads: 1024 for blocks of 128 tokens of 256 dims, whose work-groups have to do with 128 registers.
 // Bound by memory: 16 prompts of 512 tokens with 32 heads of 128 (336 MB) 75 us,
-// rows of mixed lengths in fp32 with 28 (475 MB) 103 us, where a copy of as many bytes takes 68 and 96.
+// rows of mixed lengths in fp32 with 28 (475 MB) 104 us, where a copy of as many bytes takes 68 and 96.
 template <int DH, bool BF16, int TH>
 __global__ __launch_bounds__(TH, TH > 512 ? 1 : BF16 ? 4 : 3) void k_kv_append(AppendArgs a) {
   extern __shared__ __align__(16) uint32_t lds[];
@@ -480,7 +480,7 @@ int32_t launch_kv_append(const void* qkv, bool bf16, long long qkv_stride, int h
   int th = 64;                                   // a thread of the cache part takes 32 values of a head's block
   while (th * 32 < tokens * dh) th *= 2;
   // keys: a work-group goes through several heads, whose angles are the same, where that still leaves two work-groups to a CU (16 prompts of 512 tokens, 32 heads: one head a
-  // work-group 103 us, eight 74, as with work-groups for all CUs twice)
+  // work-group 103 us, eight 75, as with work-groups for all CUs twice)
   a.seq_blocks = (b.T + bt - 2) / bt + 1;
   const long long blocks = static_cast<long long>(b.S) * a.seq_blocks;
   const long long fewest = (511 + blocks) / blocks;

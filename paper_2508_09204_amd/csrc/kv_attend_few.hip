@@ -73,7 +73,7 @@ __device__ __forceinline__ bool few_plan(const FewArgs& a, int w, FewPlan* p) {
 // Bound by reading the cache: 2 sequences of 131000 tokens, 8 key heads of 128 (537 MB), 98 us, 5.5 TB/s; 64 of up to 8000, 4 key heads (251 MB), 56 us with the join; short ones by
 // the trips to memory that wait for one another (lengths, block table, codes): one token on 63 tokens 4.8 us.
 // PAIR, up to eight columns: the other eight hold the same queries, hence the same scores, and take what the rounding of the weights to bf16 left, as weights of their own.  One
-// product does for both, and the error against 64 bits is that of the rounded result alone (one token on 600: 0.0021 -> 0.0017 of the outputs' size in the mean square).  For 9 to 32
+// product does for both, and the error against 64 bits is that of the rounded result alone (one token on 600: 0.0021 -> 0.0017 of the outputs' size in the mean square, 6.9 -> 7.0 us).  For 9 to 32
 // columns that would take a second product, 2 to 7 % of the time: their weights are rounded to bf16, as in the kernel for many rows.
 constexpr int FEW_W = 8;
 template <int DH, int NC, bool PAIR, int EXTRA>

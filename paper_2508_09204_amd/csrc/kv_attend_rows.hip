@@ -268,6 +268,8 @@ __global__ __launch_bounds__(ROWS_W * 64, DH == 256 ? 1 : 2) void k_kv_attend_ro
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] *= f;
       }
+      // Weights rounded to bf16: a second product with what the rounding leaves takes the mean error from 0.0020 to 0.0016 of the outputs and costs 1.14 to 1.43 times the time
+      // (2 x 2048 rows on 16384 tokens 904 -> 1227 us), since this kernel is bound by the matrix cores and their issue.
       kv_bf16x8 pf[2][2];
 #pragma unroll
       for (int e = 0; e < 2; ++e)

@@ -5,7 +5,8 @@
          -> output projection -> residual and norm -> SILU_MLP block -> residual and norm of the next layer
 
 with the grouped products of the library, moqe_residual_norm, moqe_kv_append and moqe_kv_attention.  A `Step` holds the buffers and marshalled calls for
-S sequences of T new rows each (a prompt, or one token each); a step of one token can be captured into a graph, since lengths live on the device.
+S sequences of T new rows each (a prompt, or one token each); a step of one token can be captured into a graph, since lengths live on the device.  All sequences of a `Sequences` are
+equally long; ragged rows, prefixes, biases by distance, gates and norms behind a block are arguments of the calls themselves (binding.KvBatch, Attention, ResidualNormCall).
 
     python -m paper_2508_09204_amd.decoder --prompt 512 --tokens 64
 
