@@ -499,6 +499,7 @@ int32_t moqe_kv_append(const void* qkv, int32_t qkv_type, int64_t qkv_stride, in
  * Arithmetic: keys and values are exact in bf16; products on bf16 matrix cores with fp32 accumulation; scores, softmax and sums in fp32.  Up to eight columns (T rows times
  * query heads of a key head) the weights exp(a - max) go into their product with the values in two bf16 pieces, and the result's rounding to bf16 is what is left of the error; with more
  * columns they are rounded to bf16, 2^-8 of a weight at most, errors that average out over the tokens (0.0020 of the outputs' size in the mean square, where 0.0017 is the result's rounding).
+ * Scores stay below 2^30 in size (there fp32 has steps of 64 and more, and past it a row may become NaN).
  * The same call gives the same bits.  A sequence's bits may differ beside other sequences or with a wider table: how its tokens are divided over work-groups depends on S, T, the head counts
  * and table_width, and where columns are few (up to 32, 16 with heads of 256) on all lengths of the call too.  Divided tokens are joined in a second launch, from the workspace that
  * the query asks for, 256-byte aligned.

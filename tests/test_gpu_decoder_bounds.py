@@ -99,3 +99,63 @@ def test_rows_past_the_call_s_own_and_their_tokens(T, heads, dh, prefix):
     want, size, got = want.reshape(M, -1), size.reshape(M, -1), tg.f64(out)
     done = ~np.isnan(want)
     assert done.any() and (np.abs(got[done] - want[done]) <= tg._attention_tol(want, size)[done]).all() and (got[~done] == 7.0).all()
+
+
+def _attend(q, heads, kv, dh, bt, rows, lens, scale, slopes=None, seed=810, prefix=None):
+    """Outputs and the oracle's, with the sums over |v|."""
+    rng = np.random.default_rng(seed)
+    table, n_blocks = tg._lay_out(rng, lens, bt)
+    cache = tg._random_cache(rng, n_blocks, kv, bt, dh)
+    tg._poison(cache, table, lens)
+    batch, seqs, T = tg._batch(table, lens, rows)
+    x = tg.dev(q, torch.bfloat16)
+    out = torch.full_like(x, 7.0)
+    mq.moqe_kv_attention(x, mq.Attention(heads, scale, slopes=None if slopes is None else tg.dev(slopes, torch.float32)), batch, tg._on_device(cache), out)
+    tg.sync()
+    with np.errstate(invalid="ignore", over="ignore"):
+        want, size = do.kv_attention(tg.f64(x), heads, cache, table, seqs, T, scale, slopes=slopes)
+    return tg.f64(out), want.reshape(batch.M, -1), size.reshape(batch.M, -1)
+
+
+FORMS = [([1, 1], 4, 2), ([4, 3], 8, 2), ([9, 4], 4, 2), ([70, 40], 4, 2)]
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.125, 1e-30, 1e6])
+@pytest.mark.parametrize("rows,heads,kv", FORMS)
+def test_scales_of_any_sign_and_size(rows, heads, kv, scale):
+    """Scale 0 is the mean of what a row sees, a negative one prefers the smallest products, a large one leaves the largest alone (here by a score of thousands)."""
+    q = np.random.default_rng(5).normal(size=(sum(rows), heads * 64))
+    got, want, size = _attend(q, heads, kv, 64, 32, rows, [90, 200], scale)
+    assert (np.abs(got - want) <= tg._attention_tol(want, size)).all()
+
+
+@pytest.mark.parametrize("by", [-0.25, 40.0])
+@pytest.mark.parametrize("rows,heads,kv", FORMS)
+def test_slopes_of_any_sign_and_size(rows, heads, kv, by):
+    """Negative slopes prefer far tokens, large ones leave a row its own token alone."""
+    q = np.random.default_rng(6).normal(size=(sum(rows), heads * 64))
+    got, want, size = _attend(q, heads, kv, 64, 32, rows, [90, 200], 0.125, slopes=by * (1 + np.arange(heads)))
+    assert (np.abs(got - want) <= tg._attention_tol(want, size)).all()
+
+
+@pytest.mark.parametrize("rows,heads,kv", [([3, 3], 2, 1), ([4, 4], 4, 1), ([8, 8], 4, 1), ([70, 40], 4, 2)])
+def test_rows_of_nan_and_infinities_keep_apart(rows, heads, kv):
+    q = np.random.default_rng(7).normal(size=(sum(rows), heads * 64))
+    q[1, 5], q[rows[0], 64 + 3], q[-1, 0] = np.nan, np.inf, -np.inf
+    got, want, size = _attend(q, heads, kv, 64, 32, rows, [90, 200], 0.125)
+    fine = np.ones(got.shape, bool)
+    for r, h in ((1, 0), (rows[0], 1), (len(q) - 1, 0)):
+        fine[r, h * 64:(h + 1) * 64] = False
+    assert np.isnan(got[1, :64]).all() and (np.abs(got - want)[fine] <= tg._attention_tol(want, size)[fine]).all()
+
+
+@pytest.mark.parametrize("rows,heads,kv,lens", [([1, 1], 150, 1, [300, 40]), ([3, 2], 150, 1, [90, 700]), ([1] * 3, 96, 96, [40, 1, 90]), ([1, 2], 640, 640, [33, 40])])
+def test_many_heads(rows, heads, kv, lens):
+    """More query heads to a key head than a tile has columns, and more key heads than work-groups run at once."""
+    tg._check_attention(rows, lens, heads, kv, 64, 32, seed=820)
+
+
+def test_six_hundred_sequences():
+    n = 600
+    tg._check_attention([1] * n, [1 + (s * 131) % 300 + (2300 if s % 97 == 5 else 0) for s in range(n)], 2, 1, 64, 32, seed=821)
+    tg._check_attention([1 + s % 3 * 20 for s in range(n)], [61 + (s * 131) % 90 for s in range(n)], 1, 1, 64, 32, seed=822)
