@@ -159,3 +159,41 @@ def test_six_hundred_sequences():
     n = 600
     tg._check_attention([1] * n, [1 + (s * 131) % 300 + (2300 if s % 97 == 5 else 0) for s in range(n)], 2, 1, 64, 32, seed=821)
     tg._check_attention([1 + s % 3 * 20 for s in range(n)], [61 + (s * 131) % 90 for s in range(n)], 1, 1, 64, 32, seed=822)
+
+
+def test_norms_of_four_million_rows():
+    """More work-groups than a launch takes along x, and elements past 2^31: every row against torch's fp32, half a bf16 step and 2^-18 of the row's largest value."""
+    M, d = (1 << 22) + 9, 520
+    r = torch.randn((M, d), generator=torch.Generator(device=tg.DEV).manual_seed(3), device=tg.DEV, dtype=torch.bfloat16)
+    out = torch.empty_like(r)
+    mq.moqe_residual_norm(None, r, out, pre=mq.Norm("rms", 1e-5))
+    for lo in range(0, M, 1 << 19):
+        x = r[lo:lo + (1 << 19)].float()
+        want = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-5)
+        assert ((out[lo:lo + (1 << 19)].float() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18 * want.abs().amax(-1, keepdim=True)).all()
+
+
+def test_rows_past_two_to_the_31_elements():
+    """140000 sequences of one token: the last rows of a call are those of a call of their own, and attention over one token is its value."""
+    S, heads, dh, bt, few = 140000, 62, 256, 32, 500
+    gen = torch.Generator(device=tg.DEV).manual_seed(4)
+    qkv = torch.randn((S, (heads + 2) * dh), generator=gen, device=tg.DEV, dtype=torch.bfloat16)
+    assert qkv.numel() > 2 ** 31
+    rope = mq.Rope(tg.dev(100.0 ** (-2.0 * np.arange(128) / 256)), 256)
+    i32 = dict(dtype=torch.int32, device=tg.DEV)
+
+    def run(x):
+        n = len(x)
+        cache = mq.KvCache.empty(n, 1, bt, dh, tg.DEV)
+        batch = mq.KvBatch(torch.arange(n, **i32).view(n, 1), torch.ones(n, **i32), n, 1, n)
+        q, out = (torch.empty((n, heads * dh), dtype=torch.bfloat16, device=tg.DEV) for _ in range(2))
+        mq.moqe_kv_append(x, heads, rope, batch, cache, q)
+        mq.moqe_kv_attention(q, mq.Attention(heads, 1 / 16), batch, cache, out)
+        tg.sync()
+        return q, out, cache
+    q, out, cache = run(qkv)
+    q2, out2, cache2 = run(qkv[-few:])
+    assert torch.equal(q[-few:], q2) and torch.equal(out[-few:], out2) and torch.equal(cache.v_scale[-few:], cache2.v_scale)
+    at = torch.from_numpy(do.value_at(np.zeros(dh, dtype=np.int64), np.arange(dh), dh)).to(tg.DEV)
+    v = cache.v[-few:, 0][:, at].view(torch.float8_e4m3fn).float() * cache.v_scale[-few:]
+    assert torch.equal(out2.view(few, heads, dh).float(), v[:, None].expand(few, heads, dh))
