@@ -17,7 +17,8 @@
  * statistics of Section 3.3 (moqe_label_pass, moqe_balance_stats); samples of different lengths
  * (moqe_*_ragged); on-demand residency of the experts' weights (moqe_cache_*, Section 4.4).  What a decoder layer of
  * an expert does around its products: norms with the residual (moqe_residual_norm), rotary positions and a paged key/value
- * cache in 8 bits (moqe_kv_append), attention over that cache (moqe_kv_attention).
+ * cache in 8 bits (moqe_kv_append), attention over that cache (moqe_kv_attention).  Rows and matrices in 8-bit floating point
+ * (moqe_residual_norm_f8, moqe_f8_*), and tokens from logits (moqe_sample).
  *
  * Conventions (all entry points).
  *  - Return value: 0 on success, a negative MOQE_E_* code on failure.  Every argument
@@ -31,7 +32,7 @@
  *    An activation matrix (rows x features, bf16) and a packed weight matrix must each stay below 4 GiB
  *    (the kernels address them with 32-bit byte offsets; larger ones are refused with MOQE_E_SHAPE).  Descriptor structs
  *    (moqe_qmat, moqe_router, moqe_nlp_router, moqe_cv_router, moqe_block, moqe_aux, moqe_norm, moqe_residual_step,
- *    moqe_kv_cache, moqe_kv_batch, moqe_rope, moqe_attention) and arrays of them are HOST memory,
+ *    moqe_kv_cache, moqe_kv_batch, moqe_rope, moqe_attention, moqe_f8_rows, moqe_f8_mat, moqe_f8_result, moqe_sampling) and arrays of them are HOST memory,
  *    read during the call only.  Scratch memory is a caller-provided device workspace
  *    whose size comes from the matching *_workspace_bytes query; it must be 256-byte
  *    aligned and may be reused between calls on the same stream.
@@ -516,6 +517,64 @@ size_t  moqe_kv_attention_workspace_bytes(const moqe_attention* attn, const moqe
 int32_t moqe_kv_attention(const void* q, int64_t q_stride, const moqe_attention* attn, const moqe_kv_batch* batch,
                           const moqe_kv_cache* cache, void* out, int64_t out_stride,
                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- 8-bit floating point --------------------------------------------------------------- */
+
+/* Rows in 8 bits: e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; largest 448, no infinities) in blocks of 128 features, each block with a power-of-two scale 2^e,
+ * -120 <= e <= 120, stored as the byte 127 + e.  An element is 2^e * code.  A row of d features has B = ceil(d / 128) blocks; codes past d in its last block are zeros.
+ *   codes  : device, 16-byte aligned, row i at byte i * code_stride (a multiple of 16, at least 128 B)
+ *   scales : device, 4-byte aligned, row i at byte i * scale_stride (a multiple of 4, at least B); bytes past B are neither written nor used
+ * Quantizing a block of fp32 values: e is the smallest with max |x| <= 448 * 2^e over its finite values (-120 if they are all zero), codes are x / 2^e to nearest
+ * (ties to even); infinities become the largest code of their sign, NaN stays. */
+typedef struct moqe_f8_rows { uint8_t *codes, *scales; int64_t code_stride, scale_stride; } moqe_f8_rows;
+
+/* moqe_residual_norm with its result in 8 bits: out8 = quantized pre(t) (from fp32).  step->out may be given too (bf16) or NULL.  Without y, pre and residual_out it is the
+ * quantizer of rows, activations and weights alike. */
+int32_t moqe_residual_norm_f8(const moqe_residual_step* step, const moqe_f8_rows* out8, void* stream);
+
+/* Matrices in 8 bits, laid out for the matrix cores.  A plain one is [n, k]; a gated pair is two of them, gate and up, for products silu(g) * u of n features.  n and k are any sizes
+ * of at least 1; packed matrices stay below 4 GiB.
+ * moqe_f8_pack: w (and up of a pair, NULL: plain): n rows of k features as above -> packed, device, 256-byte aligned, moqe_f8_packed_bytes(n, k, gated) bytes (0: refused).
+ * moqe_f8_unpack: the way back. */
+typedef struct moqe_f8_mat { const void* packed; int32_t n, k, gated; } moqe_f8_mat;
+size_t  moqe_f8_packed_bytes(int32_t n, int32_t k, int32_t gated);
+int32_t moqe_f8_pack(const moqe_f8_rows* w, const moqe_f8_rows* up, int32_t n, int32_t k, void* packed, size_t bytes, void* stream);
+int32_t moqe_f8_unpack(const moqe_f8_mat* mat, const moqe_f8_rows* w, const moqe_f8_rows* up, void* stream);
+
+/* Products of 8-bit rows and matrices:  y_row = a_row * W_e^T, or silu(a_row G_e^T) * (a_row U_e^T) for gated pairs, with the buckets of moqe_grouped_qgemm:
+ *   a       : S * T rows of k features in 8 bits, in the caller's order when perm is given (gathered on load), else in bucket order
+ *   offsets : device int32 [K + 1] in samples (values are taken into [0, S]), or NULL: K is 1 and all rows are its bucket;  perm: device int32 [S] or NULL (samples outside
+ *             [0, S) are passed over).  Rows in no bucket are left as they were.
+ *   experts : host array of K matrices of equal n, k and kind
+ *   y       : result rows of n features: MOQE_TYPE_F32 or MOQE_TYPE_BF16 (data, stride in elements, at least n, aligned to its type), or, of gated pairs, MOQE_TYPE_F8 (rows8,
+ *             quantized from fp32; n <= 32768).  y and a must not overlap.
+ *   flags   : MOQE_SCATTER_OUTPUT, MOQE_INPUT_IN_BUCKET_ORDER as in moqe_grouped_qgemm
+ * Arithmetic: products of codes are exact, scales are exact powers of two inside the matrix cores' products, sums are fp32; the same call gives the same bits.
+ * a stays below 4 GiB (S * T * code_stride).  NaN in a row of a makes NaN of that row, NaN in a row of a matrix of that feature. */
+#define MOQE_TYPE_F8     2
+typedef struct moqe_f8_result { void* data; int64_t stride; int32_t type; moqe_f8_rows rows8; } moqe_f8_result;
+size_t  moqe_f8_gemm_workspace_bytes(const moqe_f8_mat* experts, int32_t K, int32_t S, int32_t T, int32_t y_type);
+int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_t* perm, int32_t S, int32_t T, const moqe_f8_mat* experts, int32_t K,
+                     const moqe_f8_result* y, int32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- tokens ------------------------------------------------------------------------------ */
+
+/* One token of each row of logits [S, V], from a uniform number of its own.  Of row s, with l = logits, m = max l and, each NULL for all rows or device [S],
+ *   temperature : float; x_i = (l_i - m) / temperature, w_i = exp(x_i).  NULL: 1.  Values that are not above 0 take the largest logit.
+ *   top_k       : int32; the k largest logits are kept, all if k < 1
+ *   top_p       : float; of those, in descending order, the shortest run whose weight reaches top_p of theirs (at least one); all if not below 1
+ *   min_p       : float; of those, the ones with w_i >= min_p (taken as 1 if larger); all if not above 0
+ * Equal logits are ordered by index, the lowest first.  With W the weight of what is kept, tokens[s] is the first kept index, in ascending order, whose running weight
+ * exceeds u[s] * W, and logprobs[s] = log(w_token / W).
+ *   logits   : MOQE_TYPE_F32 or MOQE_TYPE_BF16, aligned to the type, row s at element s * stride (at least V);  V <= 2^20
+ *   u        : device float [S] (taken into [0, 1]; NaN is 0);  tokens: device int32 [S];  logprobs: device float [S] or NULL
+ * Minus infinity and NaN are never taken; a row without anything else gives token -1 and log probability minus infinity.  Infinite logits share all of the weight.
+ * Weights are in 64 bits, summed as integers of 2^-42 of the largest (results do not depend on any order); smaller ones count as nothing.
+ * Workspace as the query says, 256-byte aligned.  S == 0 is a no-op. */
+typedef struct moqe_sampling { const float* temperature; const int32_t* top_k; const float *top_p, *min_p; } moqe_sampling;
+size_t  moqe_sample_workspace_bytes(int32_t S, int32_t V);
+int32_t moqe_sample(const void* logits, int32_t type, int64_t stride, int32_t S, int32_t V, const moqe_sampling* how, const float* u,
+                    int32_t* tokens, float* logprobs, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- timing ------------------------------------------------------------------------- */
 

@@ -108,6 +108,22 @@ class _Attention(C.Structure):
                 ("window", C.c_int32)]
 
 
+class _F8Rows(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("code_stride", C.c_int64), ("scale_stride", C.c_int64)]
+
+
+class _F8Mat(C.Structure):
+    _fields_ = [("packed", C.c_void_p), ("n", C.c_int32), ("k", C.c_int32), ("gated", C.c_int32)]
+
+
+class _F8Result(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32), ("rows8", _F8Rows)]
+
+
+class _Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2508_09204_amd.build` "
@@ -154,6 +170,14 @@ def _load() -> C.CDLL:
         "moqe_kv_attention_workspace_bytes": (sz, [C.POINTER(_Attention), C.POINTER(_KvBatch), C.POINTER(_KvCache)]),
         "moqe_kv_attention": (i32, [vp, C.c_int64, C.POINTER(_Attention), C.POINTER(_KvBatch), C.POINTER(_KvCache), vp, C.c_int64,
                                     vp, sz, vp]),
+        "moqe_residual_norm_f8": (i32, [C.POINTER(_ResidualStep), C.POINTER(_F8Rows), vp]),
+        "moqe_f8_packed_bytes": (sz, [i32, i32, i32]),
+        "moqe_f8_pack": (i32, [C.POINTER(_F8Rows), C.POINTER(_F8Rows), i32, i32, vp, sz, vp]),
+        "moqe_f8_unpack": (i32, [C.POINTER(_F8Mat), C.POINTER(_F8Rows), C.POINTER(_F8Rows), vp]),
+        "moqe_f8_gemm_workspace_bytes": (sz, [C.POINTER(_F8Mat), i32, i32, i32, i32]),
+        "moqe_f8_gemm": (i32, [C.POINTER(_F8Rows), vp, vp, i32, i32, C.POINTER(_F8Mat), i32, C.POINTER(_F8Result), i32, vp, sz, vp]),
+        "moqe_sample_workspace_bytes": (sz, [i32, i32]),
+        "moqe_sample": (i32, [vp, i32, C.c_int64, i32, i32, C.POINTER(_Sampling), vp, vp, vp, vp, sz, vp]),
         "moqe_profile_enable": (i32, [i32]),
         "moqe_profile_read": (i32, [i32, C.POINTER(i32), C.POINTER(C.c_double)]),
     }
@@ -175,7 +199,8 @@ EXPORTED = ["moqe_version", "moqe_last_error_string", "moqe_set_dry_run", "moqe_
             "moqe_unpack_qmat", "moqe_grouped_qgemm_workspace_bytes", "moqe_grouped_qgemm",
             "moqe_workspace_bytes", "moqe_forward", "moqe_forward_static", "moqe_workspace_bytes_routed", "moqe_forward_routed", "moqe_label_pass_workspace_bytes", "moqe_label_pass", "moqe_cache_create", "moqe_cache_destroy", "moqe_cache_acquire",
             "moqe_cache_stats", "moqe_residual_norm", "moqe_kv_codes_bytes", "moqe_kv_append", "moqe_kv_attention_workspace_bytes",
-            "moqe_kv_attention", "moqe_profile_enable", "moqe_profile_read"]
+            "moqe_kv_attention", "moqe_residual_norm_f8", "moqe_f8_packed_bytes", "moqe_f8_pack", "moqe_f8_unpack", "moqe_f8_gemm_workspace_bytes", "moqe_f8_gemm",
+            "moqe_sample_workspace_bytes", "moqe_sample", "moqe_profile_enable", "moqe_profile_read"]
 
 
 def _check(rc: int) -> None:
@@ -662,6 +687,9 @@ class ResidualNormCall(_DeviceCall):
     def __init__(self, y: Optional[torch.Tensor], residual: torch.Tensor, out: Optional[torch.Tensor],
                  residual_out: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
                  scale: float = 1.0, post: Optional[Norm] = None, pre: Optional[Norm] = None):
+        self._marshal(y, residual, out, residual_out, gate, gate_rows, scale, post, pre)
+
+    def _marshal(self, y, residual, out, residual_out, gate, gate_rows, scale, post, pre, *others) -> None:
         M, d = residual.shape
         s = _ResidualStep()
         s.M, s.d, s.gate_rows, s.scale = _int32(M, "M"), _int32(d, "d"), _int32(gate_rows, "gate_rows"), scale
@@ -677,8 +705,8 @@ class ResidualNormCall(_DeviceCall):
         s.gate = _vector(gate, d * (-(-M // gate_rows) if gate_rows > 0 else 1), "gate")
         s.post = post.c(d) if post is not None else _Norm()
         s.pre = pre.c(d) if pre is not None else _Norm()
-        self._keep = (y, residual, out, residual_out, gate, post, pre)
-        self._hold(y, residual, out, residual_out, gate, *(v for n in (post, pre) if n is not None for v in (n.gain, n.offset)))
+        self._keep = (y, residual, out, residual_out, gate, post, pre, *others)
+        self._hold(y, residual, out, residual_out, gate, *others, *(v for n in (post, pre) if n is not None for v in (n.gain, n.offset)))
         self._step = s
         self._arg = C.byref(s)
 
@@ -833,3 +861,222 @@ class KvAttentionCall(_DeviceCall):
 def moqe_kv_attention(q: torch.Tensor, attn: Attention, batch: KvBatch, cache: KvCache, out: torch.Tensor,
                       workspace: Optional[torch.Tensor] = None) -> None:
     KvAttentionCall(q, attn, batch, cache, out, workspace)()
+
+
+# --------------------------------------------------------------------------------------
+# 8-bit floating point, tokens
+# --------------------------------------------------------------------------------------
+TYPE_F8 = 2
+F8_BLOCK = 128
+
+
+@dataclass
+class F8Rows:
+    """M rows of d features in 8 bits: codes uint8 [M, >= 128 * blocks], scales uint8 [M, >= blocks] (127 + the power of two), each with dense rows.
+    Codes past d in the last block are zeros, as moqe_residual_norm_f8 and moqe_f8_gemm leave them."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    M: int
+    d: int
+
+    @property
+    def blocks(self) -> int:
+        return -(-self.d // F8_BLOCK)
+
+    @classmethod
+    def empty(cls, M: int, d: int, device) -> "F8Rows":
+        blocks = -(-d // F8_BLOCK)
+        return cls(torch.empty((M, blocks * F8_BLOCK), dtype=torch.uint8, device=device),
+                   torch.empty((M, (blocks + 3) // 4 * 4), dtype=torch.uint8, device=device), M, d)
+
+    def float(self) -> torch.Tensor:
+        """The values, fp32 [M, d]."""
+        b = self.blocks
+        x = self.codes[:, : b * F8_BLOCK].view(torch.float8_e4m3fn).float().view(self.M, b, F8_BLOCK)
+        return (x * torch.exp2(self.scales[:, :b].float() - 127)[:, :, None]).reshape(self.M, -1)[:, : self.d]
+
+    def tensors(self):
+        return self.codes, self.scales
+
+    def c(self, what: str = "rows") -> _F8Rows:
+        got = []
+        for name, t, least in (("codes", self.codes, self.blocks * F8_BLOCK), ("scales", self.scales, self.blocks)):
+            if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != self.M or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError(f"{name} of {what} must be {self.M} dense rows of at least {least} bytes, got {tuple(t.shape)} of {t.dtype}")
+            unit = 16 if name == "codes" else 4
+            got.append((t.data_ptr(), t.stride(0) if self.M > 1 else -(-t.shape[1] // unit) * unit))
+        _int32(self.M, "M"), _int32(self.d, "d")
+        return _F8Rows(got[0][0], got[1][0], got[0][1], got[1][1])
+
+
+class ResidualNormF8Call(ResidualNormCall):
+    """moqe_residual_norm_f8 with its arguments marshalled once: as ResidualNormCall, with the result in `rows` (8 bits), and in out (bf16) too if given."""
+
+    def __init__(self, y: Optional[torch.Tensor], residual: torch.Tensor, rows: F8Rows, out: Optional[torch.Tensor] = None,
+                 residual_out: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
+                 scale: float = 1.0, post: Optional[Norm] = None, pre: Optional[Norm] = None):
+        if (rows.M, rows.d) != tuple(residual.shape):
+            raise ValueError(f"rows are {rows.M} of {rows.d} features, residual is {tuple(residual.shape)}")
+        self._rows_c = rows.c()
+        self._marshal(y, residual, out, residual_out, gate, gate_rows, scale, post, pre, *rows.tensors())
+
+    def __call__(self, stream: Optional[int] = None) -> None:
+        self._on_device()
+        rc = lib.moqe_residual_norm_f8(self._arg, C.byref(self._rows_c), _stream() if stream is None else stream)
+        if rc != 0:
+            _check(rc)
+
+
+def moqe_residual_norm_f8(y: Optional[torch.Tensor], residual: torch.Tensor, rows: F8Rows, out: Optional[torch.Tensor] = None,
+                          residual_out: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
+                          scale: float = 1.0, post: Optional[Norm] = None, pre: Optional[Norm] = None) -> None:
+    ResidualNormF8Call(y, residual, rows, out, residual_out, gate, gate_rows, scale, post, pre)()
+
+
+def moqe_f8_packed_bytes(n: int, k: int, gated: bool = False) -> int:
+    return lib.moqe_f8_packed_bytes(_int32(n, "n"), _int32(k, "k"), int(gated))
+
+
+class _F8Layout(_DeviceCall):
+    def __init__(self, *tensors):
+        self._hold(*tensors)
+        self._on_device()
+
+
+@dataclass
+class F8Mat:
+    """A matrix [n, k] in 8 bits, packed by moqe_f8_pack, or a gated pair of them."""
+    packed: torch.Tensor
+    n: int
+    k: int
+    gated: bool = False
+
+    @classmethod
+    def pack(cls, w: F8Rows, up: Optional[F8Rows] = None) -> "F8Mat":
+        """From rows; with `up`, the pair of gate w and up."""
+        nbytes = moqe_f8_packed_bytes(w.M, w.d, up is not None)
+        if nbytes == 0:
+            raise ValueError(f"no packed layout for a matrix of {w.M} x {w.d}")
+        mat = cls(torch.empty(nbytes, dtype=torch.uint8, device=w.codes.device), w.M, w.d, up is not None)
+        moqe_f8_pack(w, up, mat.packed)
+        return mat
+
+    def c(self) -> _F8Mat:
+        need = moqe_f8_packed_bytes(self.n, self.k, self.gated)
+        if need == 0 or self.packed.dtype != torch.uint8 or self.packed.numel() < need or not self.packed.is_contiguous():
+            raise ValueError(f"a packed matrix of {self.n} x {self.k} needs {need} contiguous bytes")
+        return _F8Mat(self.packed.data_ptr(), _int32(self.n, "n"), _int32(self.k, "k"), int(self.gated))
+
+
+def _f8_pair(w: F8Rows, up: Optional[F8Rows]):
+    if up is not None and (up.M, up.d) != (w.M, w.d):
+        raise ValueError(f"gate is {w.M} x {w.d}, up {up.M} x {up.d}")
+    return w.c("w"), up.c("up") if up is not None else None
+
+
+def moqe_f8_pack(w: F8Rows, up: Optional[F8Rows], packed: torch.Tensor) -> None:
+    wc, uc = _f8_pair(w, up)
+    _F8Layout(*w.tensors(), packed, *(up.tensors() if up is not None else ()))
+    _check(lib.moqe_f8_pack(C.byref(wc), C.byref(uc) if uc is not None else None, _int32(w.M, "n"), _int32(w.d, "k"), _ptr(packed), packed.numel(), _stream()))
+
+
+def moqe_f8_unpack(mat: F8Mat, w: F8Rows, up: Optional[F8Rows] = None) -> None:
+    if (w.M, w.d) != (mat.n, mat.k):
+        raise ValueError(f"rows are {w.M} x {w.d}, the matrix is {mat.n} x {mat.k}")
+    wc, uc = _f8_pair(w, up)
+    m = mat.c()
+    _F8Layout(mat.packed, *w.tensors(), *(up.tensors() if up is not None else ()))
+    _check(lib.moqe_f8_unpack(C.byref(m), C.byref(wc), C.byref(uc) if uc is not None else None, _stream()))
+
+
+def _f8_experts(experts: Sequence[F8Mat]):
+    return (_F8Mat * len(experts))(*(m.c() for m in experts))
+
+
+def _f8_type(y) -> int:
+    return TYPE_F8 if isinstance(y, F8Rows) else _type_of(y, "y")
+
+
+def moqe_f8_gemm_workspace_bytes(experts: Sequence[F8Mat], S: int, T: int, y_type: int) -> int:
+    return lib.moqe_f8_gemm_workspace_bytes(_f8_experts(experts), len(experts), _int32(S, "S"), _int32(T, "T"), y_type)
+
+
+class F8GemmCall(_DeviceCall):
+    """moqe_f8_gemm with its arguments marshalled once and a workspace of its own.  a: S * T rows in 8 bits; y: fp32 or bf16 [S * T, n], or F8Rows (gated pairs).
+    Without offsets there is one matrix, for all rows (S: as many as a has, T 1, if not given)."""
+
+    def __init__(self, a: F8Rows, experts: Sequence[F8Mat], y, offsets: Optional[torch.Tensor] = None, perm: Optional[torch.Tensor] = None,
+                 S: Optional[int] = None, T: int = 1, scatter: bool = False, in_bucket_order: bool = False, workspace: Optional[torch.Tensor] = None):
+        S = a.M // T if S is None else S
+        if S * T != a.M or a.d != experts[0].k:
+            raise ValueError(f"a is {a.M} rows of {a.d} features, the call is of {S} * {T} of {experts[0].k}")
+        K, n = len(experts), experts[0].n
+        if offsets is None and perm is not None:
+            raise ValueError("perm comes with offsets")
+        self._mats = _f8_experts(experts)
+        self._a = a.c("a")
+        r = _F8Result(type=_f8_type(y))
+        if isinstance(y, F8Rows):
+            if (y.M, y.d) != (a.M, n):
+                raise ValueError(f"the result has {y.M} rows of {y.d} features, not {a.M} of {n}")
+            r.rows8 = y.c("y")
+            out = y.tensors()
+        else:
+            r.data, r.stride = _rows(y, a.M, n, "y")
+            out = (y,)
+        self._result = r
+        if workspace is None:
+            workspace = _workspace(lib.moqe_f8_gemm_workspace_bytes(self._mats, K, _int32(S, "S"), _int32(T, "T"), r.type), a.codes.device)
+        self.workspace = workspace
+        self._keep = (a, experts, y, offsets, perm)
+        self._hold(*a.tensors(), *out, offsets, perm, workspace, *(m.packed for m in experts))
+        self._args = (C.byref(self._a), _vector(offsets, K + 1, "offsets", torch.int32), _vector(perm, S, "perm", torch.int32), _int32(S, "S"), _int32(T, "T"), self._mats, K,
+                      C.byref(r), (SCATTER_OUTPUT if scatter else 0) | (INPUT_IN_BUCKET_ORDER if in_bucket_order else 0), _ptr(workspace), workspace.numel())
+
+    def __call__(self, stream: Optional[int] = None) -> None:
+        self._on_device()
+        rc = lib.moqe_f8_gemm(*self._args, _stream() if stream is None else stream)
+        if rc != 0:
+            _check(rc)
+
+
+def moqe_f8_gemm(a: F8Rows, experts: Sequence[F8Mat], y, offsets: Optional[torch.Tensor] = None, perm: Optional[torch.Tensor] = None,
+                 S: Optional[int] = None, T: int = 1, scatter: bool = False, in_bucket_order: bool = False, workspace: Optional[torch.Tensor] = None) -> None:
+    F8GemmCall(a, experts, y, offsets, perm, S, T, scatter, in_bucket_order, workspace)()
+
+
+def moqe_sample_workspace_bytes(S: int, V: int) -> int:
+    return lib.moqe_sample_workspace_bytes(_int32(S, "S"), _int32(V, "V"))
+
+
+class SampleCall(_DeviceCall):
+    """moqe_sample with its arguments marshalled once and a workspace of its own.  logits fp32 or bf16 [S, V]; u fp32 [S]; tokens int32 [S]; logprobs fp32 [S] or None;
+    temperature, top_p, min_p fp32 [S], top_k int32 [S], each None if all rows go without."""
+
+    def __init__(self, logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                 top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, logprobs: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None):
+        if logits.dim() != 2:
+            raise ValueError(f"logits must be [S, V], got {tuple(logits.shape)}")
+        S, V = logits.shape
+        p, stride = _rows(logits, S, V, "logits")
+        how = _Sampling(_vector(temperature, S, "temperature"), _vector(top_k, S, "top_k", torch.int32), _vector(top_p, S, "top_p"), _vector(min_p, S, "min_p"))
+        if workspace is None:
+            workspace = _workspace(lib.moqe_sample_workspace_bytes(_int32(S, "S"), _int32(V, "V")), logits.device)
+        self.workspace = workspace
+        self._keep = (logits, u, tokens, temperature, top_k, top_p, min_p, logprobs, how)
+        self._hold(logits, u, tokens, temperature, top_k, top_p, min_p, logprobs, workspace)
+        self._args = (p, _type_of(logits, "logits"), stride, _int32(S, "S"), _int32(V, "V"), C.byref(how), _vector(u, S, "u"), _vector(tokens, S, "tokens", torch.int32),
+                      _vector(logprobs, S, "logprobs"), _ptr(workspace), workspace.numel())
+
+    def __call__(self, stream: Optional[int] = None) -> None:
+        self._on_device()
+        rc = lib.moqe_sample(*self._args, _stream() if stream is None else stream)
+        if rc != 0:
+            _check(rc)
+
+
+def moqe_sample(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, logprobs: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None) -> None:
+    SampleCall(logits, u, tokens, temperature, top_k, top_p, min_p, logprobs, workspace)()

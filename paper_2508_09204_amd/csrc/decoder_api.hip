@@ -7,11 +7,11 @@ namespace {
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-int32_t check_norm(const moqe_norm& n, const char* which) {
-  if (n.kind < MOQE_NORM_NONE || n.kind > MOQE_NORM_LAYER) return set_error(MOQE_E_FORMAT, "moqe_residual_norm: %s norm of kind %d", which, n.kind);
-  if (n.kind != MOQE_NORM_NONE && !(n.eps >= 0.f)) return set_error(MOQE_E_SHAPE, "moqe_residual_norm: %s norm has a negative eps", which);
-  if (n.offset && n.kind != MOQE_NORM_LAYER) return set_error(MOQE_E_FORMAT, "moqe_residual_norm: %s norm: only layer norms have an offset", which);
-  if (!aligned(n.gain, 4) || !aligned(n.offset, 4)) return set_error(MOQE_E_SHAPE, "moqe_residual_norm: %s norm: misaligned vector", which);
+int32_t check_norm(const moqe_norm& n, const char* which, const char* who) {
+  if (n.kind < MOQE_NORM_NONE || n.kind > MOQE_NORM_LAYER) return set_error(MOQE_E_FORMAT, "%s: %s norm of kind %d", who, which, n.kind);
+  if (n.kind != MOQE_NORM_NONE && !(n.eps >= 0.f)) return set_error(MOQE_E_SHAPE, "%s: %s norm has a negative eps", who, which);
+  if (n.offset && n.kind != MOQE_NORM_LAYER) return set_error(MOQE_E_FORMAT, "%s: %s norm: only layer norms have an offset", who, which);
+  if (!aligned(n.gain, 4) || !aligned(n.offset, 4)) return set_error(MOQE_E_SHAPE, "%s: %s norm: misaligned vector", who, which);
   return MOQE_OK;
 }
 
@@ -69,6 +69,33 @@ int32_t check_attention(const moqe_attention* at, const moqe_kv_batch* b, const 
   return MOQE_OK;
 }
 
+// `out8`: results in 8 bits are wanted, so that there need not be others.  *empty: there are no rows.
+int32_t check_residual_step(const moqe_residual_step* s, bool out8, const char* who, bool* empty) {
+  *empty = false;
+  if (!s) return set_error(MOQE_E_NULL, "%s: step is NULL", who);
+  if (s->M < 0 || s->d < 1 || s->d > 32768) return set_error(MOQE_E_SHAPE, "%s: %d rows of %d features (1 .. 32768)", who, s->M, s->d);
+  if ((s->y_type != MOQE_TYPE_F32 && s->y_type != MOQE_TYPE_BF16) || (s->residual_type != MOQE_TYPE_F32 && s->residual_type != MOQE_TYPE_BF16))
+    return set_error(MOQE_E_FORMAT, "%s: y_type %d, residual_type %d", who, s->y_type, s->residual_type);
+  int32_t rc = check_norm(s->post, "post", who);
+  if (!rc) rc = check_norm(s->pre, "pre", who);
+  if (rc) return rc;
+  if (s->gate_rows < 0) return set_error(MOQE_E_SHAPE, "%s: gate_rows %d", who, s->gate_rows);
+  if (s->M == 0) {
+    *empty = true;
+    return MOQE_OK;
+  }
+  if (!s->residual) return set_error(MOQE_E_NULL, "%s: residual is NULL", who);
+  if (!s->residual_out && !s->out && !out8) return set_error(MOQE_E_NULL, "%s: residual_out and out are both NULL", who);
+  if (s->residual_stride < s->d || (s->y && s->y_stride < s->d) || (s->residual_out && s->residual_out_stride < s->d) || (s->out && s->out_stride < s->d))
+    return set_error(MOQE_E_SHAPE, "%s: a row stride is smaller than d = %d", who, s->d);
+  if (s->residual_out == s->residual && s->residual_out_stride != s->residual_stride)
+    return set_error(MOQE_E_SHAPE, "%s: residual_out is residual with another stride", who);
+  const size_t ysz = s->y_type == MOQE_TYPE_F32 ? 4 : 2, rsz = s->residual_type == MOQE_TYPE_F32 ? 4 : 2;
+  if (!aligned(s->y, ysz) || !aligned(s->residual, rsz) || !aligned(s->residual_out, rsz) || !aligned(s->out, 2) || !aligned(s->gate, 4))
+    return set_error(MOQE_E_SHAPE, "%s: a pointer is not aligned to its type", who);
+  return MOQE_OK;
+}
+
 }  // namespace
 }  // namespace moqe
 
@@ -77,27 +104,20 @@ using namespace moqe;
 extern "C" {
 
 int32_t moqe_residual_norm(const moqe_residual_step* s, void* stream) {
-  const char* who = "moqe_residual_norm";
-  if (!s) return set_error(MOQE_E_NULL, "%s: step is NULL", who);
-  if (s->M < 0 || s->d < 1 || s->d > 32768) return set_error(MOQE_E_SHAPE, "%s: %d rows of %d features (1 .. 32768)", who, s->M, s->d);
-  if ((s->y_type != MOQE_TYPE_F32 && s->y_type != MOQE_TYPE_BF16) || (s->residual_type != MOQE_TYPE_F32 && s->residual_type != MOQE_TYPE_BF16))
-    return set_error(MOQE_E_FORMAT, "%s: y_type %d, residual_type %d", who, s->y_type, s->residual_type);
-  int32_t rc = check_norm(s->post, "post");
-  if (!rc) rc = check_norm(s->pre, "pre");
-  if (rc) return rc;
-  if (s->gate_rows < 0) return set_error(MOQE_E_SHAPE, "%s: gate_rows %d", who, s->gate_rows);
-  if (s->M == 0) return MOQE_OK;
-  if (!s->residual) return set_error(MOQE_E_NULL, "%s: residual is NULL", who);
-  if (!s->residual_out && !s->out) return set_error(MOQE_E_NULL, "%s: residual_out and out are both NULL", who);
-  if (s->residual_stride < s->d || (s->y && s->y_stride < s->d) || (s->residual_out && s->residual_out_stride < s->d) || (s->out && s->out_stride < s->d))
-    return set_error(MOQE_E_SHAPE, "%s: a row stride is smaller than d = %d", who, s->d);
-  if (s->residual_out == s->residual && s->residual_out_stride != s->residual_stride)
-    return set_error(MOQE_E_SHAPE, "%s: residual_out is residual with another stride", who);
-  const size_t ysz = s->y_type == MOQE_TYPE_F32 ? 4 : 2, rsz = s->residual_type == MOQE_TYPE_F32 ? 4 : 2;
-  if (!aligned(s->y, ysz) || !aligned(s->residual, rsz) || !aligned(s->residual_out, rsz) || !aligned(s->out, 2) || !aligned(s->gate, 4))
-    return set_error(MOQE_E_SHAPE, "%s: a pointer is not aligned to its type", who);
-  if (dry_run()) return MOQE_OK;
-  return launch_residual_norm(*s, static_cast<hipStream_t>(stream));
+  bool empty;
+  const int32_t rc = check_residual_step(s, false, "moqe_residual_norm", &empty);
+  if (rc || empty || dry_run()) return rc;
+  return launch_residual_norm(*s, nullptr, static_cast<hipStream_t>(stream));
+}
+
+int32_t moqe_residual_norm_f8(const moqe_residual_step* s, const moqe_f8_rows* out8, void* stream) {
+  const char* who = "moqe_residual_norm_f8";
+  bool empty;
+  int32_t rc = check_residual_step(s, true, who, &empty);
+  if (rc || empty) return rc;
+  rc = check_f8_rows(out8, s->d, "out8", who);
+  if (rc || dry_run()) return rc;
+  return launch_residual_norm(*s, out8, static_cast<hipStream_t>(stream));
 }
 
 size_t moqe_kv_codes_bytes(const moqe_kv_cache* c) {

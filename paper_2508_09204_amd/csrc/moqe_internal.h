@@ -245,7 +245,7 @@ int32_t launch_act_quant(const void* x_bf16, int kdim, int T, const int32_t* off
                          int expert, int max_rows, int8_t* out, float* scales, hipStream_t st);
 
 // Around the products of a decoder layer (residual_norm.hip, kv_append.hip, kv_attend_few.hip, kv_attend_rows.hip): arguments already checked.
-int32_t launch_residual_norm(const moqe_residual_step& s, hipStream_t st);
+int32_t launch_residual_norm(const moqe_residual_step& s, const moqe_f8_rows* out8, hipStream_t st);       // out8 NULL: none
 int32_t launch_kv_append(const void* qkv, bool bf16, long long qkv_stride, int heads, const moqe_rope& r, const moqe_kv_batch& b,
                          const moqe_kv_cache& c, void* q_out, long long q_stride, hipStream_t st);
 int32_t launch_kv_attend_few(const void* q, long long q_stride, const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c,
@@ -254,5 +254,19 @@ size_t  kv_attend_few_ws_bytes(const moqe_attention& at, const moqe_kv_batch& b,
 int32_t launch_kv_attend_rows(const void* q, long long q_stride, const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c,
                               void* out, long long out_stride, void* ws, hipStream_t st);
 size_t  kv_attend_rows_ws_bytes(const moqe_attention& at, const moqe_kv_batch& b, const moqe_kv_cache& c);
+
+// Rows, matrices and products in 8-bit floating point (f8_pack.hip, f8_gemm.hip), tokens (sample.hip).
+struct F8Args;
+int32_t check_f8_rows(const moqe_f8_rows* r, int32_t d, const char* what, const char* who);
+int32_t launch_f8_pack(const moqe_f8_rows& w, const moqe_f8_rows* up, int n, int k, uint8_t* out, hipStream_t st);
+int32_t launch_f8_unpack(const moqe_f8_mat& m, const moqe_f8_rows& w, const moqe_f8_rows* up, hipStream_t st);
+int32_t launch_f8_gemm(const F8Args& a, bool gated, void* ws, hipStream_t st);
+int32_t launch_f8_tile(const F8Args& a, bool gated, bool exact, int shape, hipStream_t st);
+int32_t launch_f8_few(const F8Args& a, bool gated, bool exact, int mb, int wt, hipStream_t st);
+int32_t launch_f8_quantize(const F8Args& a, const float* h, hipStream_t st);
+size_t  f8_gemm_ws_bytes(long long M, int n, int k, int K, bool gated, bool out8);
+int32_t launch_sample(const void* logits, bool bf16, long long stride, int S, int V, const moqe_sampling& how, const float* u, int32_t* tokens, float* logprobs,
+                      void* ws, hipStream_t st);
+size_t  sample_ws_bytes(int S, int V);
 
 }  // namespace moqe

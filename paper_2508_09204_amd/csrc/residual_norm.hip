@@ -1,12 +1,14 @@
 // Norms before and after a block, fused with its gate and the residual: u = post(y), t = r + scale gate (.) u, r' = t, out = pre(t).
-#include "moqe_internal.h"
+#include "f8_device.h"
+
+#include <type_traits>
 
 namespace moqe {
 
 struct NormArgs {
-  const void* y; const void* r; void* r_out; uint16_t* out;
+  const void* y; const void* r; void* r_out; uint16_t* out; uint8_t *codes, *scales;
   const float *gate, *post_gain, *post_offset, *pre_gain, *pre_offset;
-  long long ys, rs, ros, os;
+  long long ys, rs, ros, os, cs, ss;
   int M, d, gate_rows, post, pre, row_threads;
   float scale, post_eps, pre_eps;
 };
@@ -139,7 +141,8 @@ __device__ __forceinline__ void normed(float (&t)[NV][8], int d, int th, int lan
 }
 
 // A row in the registers of a.row_threads threads, every input read once.  Rows of one wave need no barrier, and four share a work-group.
-template <int NV, bool ODD, bool YBF, bool RBF>
+// F8: the result as 8-bit rows, besides bf16 ones if those are wanted too.  A block of 128 features is a piece of 16 neighbouring lanes.
+template <int NV, bool ODD, bool YBF, bool RBF, bool F8>
 __global__ __launch_bounds__(1024) void k_residual_norm(NormArgs a) {
   __shared__ float part[4 * 16];
   const int th = a.row_threads, d = a.d, lane = th == 64 ? threadIdx.x & 63 : threadIdx.x;
@@ -178,12 +181,25 @@ __global__ __launch_bounds__(1024) void k_residual_norm(NormArgs a) {
       if (f < d) store_values<RBF, ODD>(a.r_out, row * a.ros, f, d, t[j]);
     }
   }
-  if (!a.out) return;
+  if (!F8 && !a.out) return;
   if (a.pre != MOQE_NORM_NONE) normed<NV, ODD>(t, d, th, lane, a.pre, a.pre_eps, a.pre_gain, a.pre_offset, part + 32);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int f = (j * th + lane) * 8;
-    if (f < d) store_values<true, ODD>(a.out, row * a.os, f, d, t[j]);
+    if ((!F8 || a.out) && f < d) store_values<true, ODD>(a.out, row * a.os, f, d, t[j]);
+  }
+  if constexpr (F8) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int f = (j * th + lane) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[j][i] = f + i < d ? t[j][i] : 0.f;
+      const int e = f8_exponent(f8_row_top(f8_top(t[j])));
+      if (f < f8_blocks(d) * F8_BLOCK) {
+        *reinterpret_cast<uint2*>(a.codes + row * a.cs + f) = f8_codes(t[j], e);
+        if ((threadIdx.x & 15) == 0) a.scales[row * a.ss + f / F8_BLOCK] = uint8_t(e + 127);
+      }
+    }
   }
 }
 
@@ -194,10 +210,15 @@ void launch_types(const NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
   // a launch has fewer than 2^32 threads along x
   const uint32_t wgs = wave_rows ? (uint32_t(a.M) + 3) / 4 : uint32_t(a.M), gx = wgs < (1u << 20) ? wgs : 1u << 20;
   const dim3 grid(gx, (wgs + gx - 1) / gx), block(wave_rows ? 256 : a.row_threads);
-  if (ybf && rbf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, true, true>), grid, block, 0, st, a);
-  else if (ybf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, true, false>), grid, block, 0, st, a);
-  else if (rbf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, false, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_residual_norm<NV, ODD, false, false>), grid, block, 0, st, a);
+  auto launch = [&](auto f8) {
+    constexpr bool F8 = decltype(f8)::value;
+    if (ybf && rbf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, true, true, F8>), grid, block, 0, st, a);
+    else if (ybf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, true, false, F8>), grid, block, 0, st, a);
+    else if (rbf) hipLaunchKernelGGL((k_residual_norm<NV, ODD, false, true, F8>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_residual_norm<NV, ODD, false, false, F8>), grid, block, 0, st, a);
+  };
+  if (a.codes) launch(std::true_type());
+  else launch(std::false_type());
 }
 template <bool ODD>
 void launch_pieces(NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
@@ -210,13 +231,14 @@ void launch_pieces(NormArgs& a, bool ybf, bool rbf, hipStream_t st) {
 }
 }  // namespace
 
-int32_t launch_residual_norm(const moqe_residual_step& s, hipStream_t st) {
+int32_t launch_residual_norm(const moqe_residual_step& s, const moqe_f8_rows* out8, hipStream_t st) {
   NormArgs a{};
   a.y = s.y; a.r = s.residual; a.r_out = s.residual_out; a.out = static_cast<uint16_t*>(s.out); a.gate = s.gate;
   a.post_gain = s.post.gain; a.post_offset = s.post.offset; a.pre_gain = s.pre.gain; a.pre_offset = s.pre.offset;
   a.ys = s.y_stride; a.rs = s.residual_stride; a.ros = s.residual_out_stride; a.os = s.out_stride;
   a.M = s.M; a.d = s.d; a.gate_rows = s.gate_rows; a.post = s.post.kind; a.pre = s.pre.kind;
   a.scale = s.scale; a.post_eps = s.post.eps; a.pre_eps = s.pre.eps;
+  if (out8) { a.codes = out8->codes; a.scales = out8->scales; a.cs = out8->code_stride; a.ss = out8->scale_stride; }
   // 16-byte accesses where every row and vector starts on 16 bytes
   uintptr_t at = 0;
   for (const void* p : {s.y, s.residual, static_cast<const void*>(s.residual_out), static_cast<const void*>(s.out), static_cast<const void*>(s.gate),

@@ -1,0 +1,382 @@
+"""Rows and products in 8-bit floating point on the GPU against the 64-bit oracle, at the sizes, strides and values where they can go wrong.
+
+Tolerances, from the roundings of each path (half a step: bf16 2^-8 of a value, fp32 2^-24, e4m3 2^-4 or half the smallest step):
+  codes     bit-equal where the value is exact in fp32; behind norms (fp32 sums of d terms: 2^-18 of the row's largest value, as for bf16 results) half a step of the
+            value plus that; a scale may be the neighbour's only where the block's largest value lies within 2^-18 of 448 * 2^e
+  products  codes and scales are exact, sums in fp32 in any order: k steps of 2^-24 of sum |a w| are the bound for sums one by one, of which 128 are added inside an
+            instruction; 2^-24 (blocks + 128) of sum |a w| covers both; bf16 results half a step more; silu 2^-20 of the result, and its inputs' error (|silu'| <= 1.1)
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decoder_oracle as do
+from oracle import f8_oracle as fo
+from paper_2508_09204_amd import binding as mq
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+    return t if dtype is None else t.to(dtype)
+
+
+def sync():
+    torch.cuda.synchronize()
+
+
+def empty_rows(M, d, pad=0):
+    """8-bit rows with `pad` * 16 spare bytes a row, all bytes 0xa5."""
+    blocks = -(-d // 128)
+    return mq.F8Rows(torch.full((M, blocks * 128 + pad * 16), 0xa5, dtype=torch.uint8, device=DEV),
+                     torch.full((M, (blocks + 3) // 4 * 4 + pad * 4), 0xa5, dtype=torch.uint8, device=DEV), M, d)
+
+
+def rows_of(x, pad=0):
+    """8-bit rows of x, quantized by the oracle, and what they stand for."""
+    codes, scales = fo.quantize_rows(x)
+    r = empty_rows(*x.shape, pad)
+    r.codes[:, : codes.shape[1]] = dev(codes)
+    r.scales[:, : scales.shape[1]] = dev(scales)
+    return r, fo.rows_value(codes, scales, x.shape[1])
+
+
+def check_rows(got, want, near):
+    """got: rows from the GPU; want: values in 64 bits; near [M, 1]: error of a value before its rounding."""
+    b = got.blocks
+    codes, scales = got.codes[:, : b * 128].cpu().numpy(), got.scales[:, :b].cpu().numpy()
+    M, d = want.shape
+    full = np.zeros((M, b * 128))
+    full[:, :d] = want
+    top = np.abs(full.reshape(M, b, 128)).max(2)
+    s = 2.0 ** (scales.astype(np.float64) - 127)
+    assert (top <= 448 * s + near).all() and ((top > 224 * s - near) | (scales == 7)).all()
+    v = do.e4m3_value(codes) * np.repeat(s, 128, 1)
+    step = np.repeat(s, 128, 1) * 2.0 ** -10
+    assert (np.abs(v - full) <= np.maximum(2.0 ** -4 * np.abs(full), step) + near * 1.07 + np.where(np.abs(full) > 448 * np.repeat(s, 128, 1), near, 0)).all()
+    assert not codes[:, d:].any()
+    assert (got.codes[:, b * 128:] == 0xa5).all() and (got.scales[:, (b + 3) // 4 * 4:] == 0xa5).all()      # spare bytes as they were
+
+
+# ------------------------------------------------------------------------------------------------------------------ rows
+@pytest.mark.parametrize("M,d", [(1, 1), (1, 128), (3, 7), (5, 129), (4, 255), (2, 2047), (9, 2056), (3, 4096), (2, 8200), (1, 16385), (1, 32768), (130, 96)])
+@pytest.mark.parametrize("t", [F32, BF])
+def test_quantizer_is_exact(M, d, t):
+    rng = np.random.default_rng(M * 7 + d)
+    x = dev((rng.normal(size=(M, d)) * np.exp2(rng.integers(-30, 30, size=(M, 1)))).astype(np.float32), t)
+    got = empty_rows(M, d, 1)
+    mq.moqe_residual_norm_f8(None, x, got)
+    sync()
+    codes, scales = fo.quantize_rows(f64(x))
+    b = got.blocks
+    assert np.array_equal(got.scales[:, :b].cpu().numpy(), scales) and np.array_equal(got.codes[:, : b * 128].cpu().numpy(), codes)
+    assert (got.codes[:, b * 128:] == 0xa5).all() and (got.scales[:, (b + 3) // 4 * 4:] == 0xa5).all()
+    assert np.array_equal(f64(got.float()), fo.rows_value(codes, scales, d))
+
+
+def test_quantizer_of_special_values():
+    x = torch.zeros((8, 384), device=DEV)
+    x[1, 130], x[1, 131], x[1, 132], x[1, 133] = float("inf"), float("-inf"), float("nan"), 3.0
+    x[2, :] = float("nan")
+    x[3, 5] = float("inf")
+    x[4, 7], x[4, 8] = 3e38, -3e38                              # past 448 * 2^120
+    x[5, 0], x[5, 1] = 1e-45, -1e-40                            # below every code
+    x[6, 0], x[6, 1], x[6, 128], x[6, 129] = 448.0, 1.0, 448.00003, 1.0
+    x[7, :128] = torch.arange(128, device=DEV) * 2.0 ** -9 - 0.1
+    got = empty_rows(8, 384)
+    mq.moqe_residual_norm_f8(None, x, got)
+    sync()
+    codes, scales = fo.quantize_rows(f64(x))
+    assert np.array_equal(got.scales[:, :3].cpu().numpy(), scales)
+    ours, nan = got.codes.cpu().numpy(), (codes & 0x7f) == 0x7f
+    assert np.array_equal(ours[~nan], codes[~nan]) and ((ours[nan] & 0x7f) == 0x7f).all()
+
+
+def _norm_case(M, d, y_t, r_t, post, pre, gate, pad=0, lead=0, both=False):
+    rng = np.random.default_rng(M * 7 + d + pad)
+    def rows(t):
+        buf = torch.zeros(lead + M * (d + pad), dtype=t, device=DEV)
+        v = buf[lead:].view(M, d + pad)[:, :d]
+        v.copy_(dev(rng.normal(size=(M, d)) + 0.5))
+        return v
+    y, r = rows(y_t) if y_t else None, rows(r_t)
+    res, out = rows(r_t), rows(BF) if both else None
+    g = None if not gate else dev(rng.normal(size=(-(-M // 3), d) if gate == "sample" else d).astype(np.float32))
+    vec = lambda on: dev(rng.normal(size=d).astype(np.float32)) if on else None
+    norms = {n: None if not k else mq.Norm(k, 1e-5, vec(n == "pre" or k == "rms"), vec(k == "layer")) for n, k in (("post", post), ("pre", pre))}
+    args = {n: None if v is None else (v.kind, 1e-5, None if v.gain is None else f64(v.gain), None if v.offset is None else f64(v.offset))
+            for n, v in norms.items()}
+    gate_rows = 3 if gate == "sample" else 0
+    want_t, want_o = do.residual_norm(None if y is None else f64(y), f64(r), None if g is None else f64(g), gate_rows, 0.75, args["post"], args["pre"])
+    got = empty_rows(M, d, 2)
+    mq.moqe_residual_norm_f8(y, r, got, out, res, g, gate_rows, 0.75, norms["post"], norms["pre"])
+    sync()
+    near = 2.0 ** -18 * np.abs(want_o).max(1, keepdims=True)
+    check_rows(got, want_o, near)
+    plain = torch.empty((M, d), dtype=BF, device=DEV)
+    res2 = torch.empty((M, d), dtype=r_t, device=DEV)
+    mq.moqe_residual_norm(y, r, plain, res2, g, gate_rows, 0.75, norms["post"], norms["pre"])
+    sync()
+    assert torch.equal(res2, res) and (out is None or torch.equal(plain, out))       # beside 8 bits the rest is what it is without
+
+
+@pytest.mark.parametrize("M,d", [(1, 1), (3, 7), (5, 8), (4, 255), (2, 2048), (3, 4096), (2, 5003), (2, 8200), (1, 32767), (1, 32768), (130, 96)])
+@pytest.mark.parametrize("pre", ["rms", "layer"])
+def test_norm_sizes(M, d, pre):
+    _norm_case(M, d, F32, BF, "", pre, "")
+    _norm_case(M, d, BF, F32, "layer" if pre == "rms" else "rms", pre, "sample", both=True)
+
+
+@pytest.mark.parametrize("y_t,r_t", [(F32, F32), (F32, BF), (BF, F32), (BF, BF), (None, F32)])
+def test_norm_types(y_t, r_t):
+    _norm_case(7, 200, y_t, r_t, "rms", "", "all")
+    _norm_case(7, 200, y_t, r_t, "", "rms", "", both=True)
+
+
+@pytest.mark.parametrize("pad,lead", [(8, 0), (1, 0), (5, 3), (0, 1), (0, 2)])
+def test_norm_strides_and_alignment(pad, lead):
+    for d in (64, 100, 5000):
+        _norm_case(6, d, BF, F32, "rms", "layer", "all", pad=pad, lead=lead)
+
+
+def test_norm_rows_keep_apart():
+    r = torch.ones((8, 300), device=DEV)
+    r[2, 7], r[4, 0], r[5] = float("inf"), float("nan"), 0.0
+    got = empty_rows(8, 300)
+    mq.moqe_residual_norm_f8(None, r, got, pre=mq.Norm("rms", 1e-6))
+    sync()
+    v = got.float()
+    fine = [0, 1, 3, 6, 7]
+    assert (v[fine] == 1.0).all() and (v[5] == 0.0).all() and v[4].isnan().all() and v[2, 7].isnan() and (v[2, :7] == 0.0).all()
+
+
+# ------------------------------------------------------------------------------------------------------------------ packing
+@pytest.mark.parametrize("n,k", [(1, 1), (16, 128), (17, 129), (40, 1000), (256, 640), (100, 15)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_pack_and_unpack(n, k, gated):
+    rng = np.random.default_rng(n + k)
+    w = [rows_of(rng.normal(size=(n, k)), 1)[0] for _ in range(2 if gated else 1)]
+    for r in w:
+        r.codes[:, k:] = 0x7f                                    # past the last column: not taken along
+    mat = mq.F8Mat.pack(*w)
+    back = [empty_rows(n, k) for _ in w]
+    mq.moqe_f8_unpack(mat, *back)
+    sync()
+    for a, b in zip(w, back):
+        assert torch.equal(a.codes[:, :k], b.codes[:, :k]) and not b.codes[:, k:].any() and torch.equal(a.scales[:, : a.blocks], b.scales[:, : b.blocks])
+
+
+# ------------------------------------------------------------------------------------------------------------------ products
+def buckets(rng, S, K, skew=None):
+    e = rng.integers(0, K, size=S) if skew is None else np.asarray(skew)
+    perm = np.argsort(e, kind="stable").astype(np.int32)
+    return e, dev(np.concatenate([[0], np.cumsum(np.bincount(e, minlength=K))]).astype(np.int32)), dev(perm)
+
+
+def check_product(y, a, w, up, t):
+    """y from the GPU (F8Rows or tensor), operands' values."""
+    k = a.shape[1]
+    rel = 2.0 ** -24 * (-(-k // 128) + 128)
+    want = fo.product(a, w, up)
+    size = np.abs(a) @ np.abs(w).T
+    if up is None:
+        tol = rel * size
+    else:
+        g, u = a @ w.T, a @ up.T
+        silu = g / (1 + np.exp(-g))
+        tol = 1.1 * rel * size * np.abs(u) + rel * (np.abs(a) @ np.abs(up).T) * np.abs(silu) + 2.0 ** -20 * np.abs(want) + 1e-37
+    if t == "f8":
+        check_rows(y, want, tol.max(1, keepdims=True))
+    else:
+        got = f64(y)
+        assert (np.abs(got - want) <= tol + (2.0 ** -8 * np.abs(want) if t == BF else 2.0 ** -24 * np.abs(want))).all(), np.abs(got - want).max()
+
+
+def result(M, n, t):
+    return empty_rows(M, n, 1) if t == "f8" else torch.full((M, n), float("nan"), dtype=t, device=DEV)
+
+
+SIZES = [(1, 16, 128), (1, 1, 1), (3, 50, 100), (16, 64, 256), (17, 300, 384), (33, 129, 1000), (64, 512, 640), (65, 257, 130), (130, 1000, 515), (200, 48, 2048), (257, 640, 1152),
+         (400, 272, 256)]
+
+
+@pytest.mark.parametrize("M,n,k", SIZES)
+@pytest.mark.parametrize("gated,t", [(False, F32), (False, BF), (True, F32), (True, BF), (True, "f8")])
+def test_dense_products(M, n, k, gated, t):
+    rng = np.random.default_rng(M + n + k)
+    a, av = rows_of(rng.normal(size=(M, k)) * np.exp2(rng.integers(-6, 6, size=(M, 1))), 1)
+    w = [rows_of(rng.normal(size=(n, k)) * k ** -0.5 * np.exp2(rng.integers(-3, 3, size=(n, 1)))) for _ in range(2 if gated else 1)]
+    y = result(M, n, t)
+    mq.moqe_f8_gemm(a, [mq.F8Mat.pack(*(r for r, _ in w))], y)
+    sync()
+    check_product(y, av, w[0][1], w[1][1] if gated else None, t)
+
+
+@pytest.mark.parametrize("S,T,K", [(1, 1, 2), (5, 1, 3), (40, 1, 4), (7, 9, 3), (12, 33, 2), (3, 130, 4), (300, 1, 16), (64, 5, 1)])
+@pytest.mark.parametrize("gated,t", [(False, F32), (False, BF), (True, "f8"), (True, BF)])
+@pytest.mark.parametrize("scatter", [False, True])
+def test_grouped_products(S, T, K, gated, t, scatter):
+    rng = np.random.default_rng(S * 3 + T + K)
+    n, k, M = 200, 300, S * T
+    e, offsets, perm = buckets(rng, S, K)
+    a, av = rows_of(rng.normal(size=(M, k)))
+    w = [[rows_of(rng.normal(size=(n, k)) * 0.1) for _ in range(2 if gated else 1)] for _ in range(K)]
+    mats = [mq.F8Mat.pack(*(r for r, _ in x)) for x in w]
+    y = result(M, n, t)
+    mq.moqe_f8_gemm(a, mats, y, offsets, perm, S, T, scatter=scatter)
+    sync()
+    order = perm.cpu().numpy()
+    for s in range(S):
+        slot = s if scatter else int(np.where(order == s)[0][0])
+        at = slice(slot * T, slot * T + T)
+        part = mq.F8Rows(y.codes[at], y.scales[at], T, n) if t == "f8" else y[at]
+        check_product(part, av[s * T : (s + 1) * T], w[e[s]][0][1], w[e[s]][1][1] if gated else None, t)
+
+
+def test_bucket_order_in_and_out():
+    rng = np.random.default_rng(3)
+    S, T, K, n, k = 20, 3, 3, 96, 256
+    e, offsets, perm = buckets(rng, S, K)
+    a, _ = rows_of(rng.normal(size=(S * T, k)))
+    mats = [mq.F8Mat.pack(rows_of(rng.normal(size=(n, k)))[0]) for _ in range(K)]
+    whole, inner, gathered = (result(S * T, n, F32) for _ in range(3))
+    mq.moqe_f8_gemm(a, mats, whole, offsets, perm, S, T, scatter=True)
+    mq.moqe_f8_gemm(a, mats, gathered, offsets, perm, S, T)
+    order = (perm.long()[:, None] * T + torch.arange(T, device=DEV)).flatten()
+    moved = mq.F8Rows(a.codes[order], a.scales[order], S * T, k)
+    mq.moqe_f8_gemm(moved, mats, inner, offsets, None, S, T)
+    back = result(S * T, n, F32)
+    mq.moqe_f8_gemm(moved, mats, back, offsets, perm, S, T, scatter=True, in_bucket_order=True)
+    sync()
+    assert torch.equal(whole, back) and torch.equal(gathered, inner) and torch.equal(inner, whole[order])
+
+
+@pytest.mark.parametrize("S,T", [(12, 1), (12, 40)])
+@pytest.mark.parametrize("t", [F32, "f8"])
+def test_rows_in_no_bucket_stay(S, T, t):
+    """Offsets that leave samples out, empty experts, and a perm entry that names no sample."""
+    rng = np.random.default_rng(4)
+    K, n, k = 4, 64, 128
+    a, av = rows_of(rng.normal(size=(S * T, k)))
+    w = [[rows_of(rng.normal(size=(n, k))) for _ in range(2)] for _ in range(K)]
+    mats = [mq.F8Mat.pack(*(r for r, _ in x)) for x in w]
+    offsets = dev(np.array([2, 2, 7, 7, 9], np.int32))
+    perm = torch.randperm(S, generator=torch.Generator().manual_seed(1)).to(torch.int32)
+    perm[4] = S + 3
+    y = empty_rows(S * T, n) if t == "f8" else torch.full((S * T, n), -7.0, device=DEV)
+    mq.moqe_f8_gemm(a, mats, y, offsets, perm.to(DEV), S, T, scatter=True)
+    sync()
+    done = {int(perm[i]): (1 if i < 7 else 3) for i in (2, 3, 5, 6, 7, 8)}
+    for s in range(S):
+        at = slice(s * T, (s + 1) * T)
+        if s in done:
+            part = mq.F8Rows(y.codes[at], y.scales[at], T, n) if t == "f8" else y[at]
+            check_product(part, av[at], w[done[s]][0][1], w[done[s]][1][1], t)
+        elif t == "f8":
+            assert (y.codes[at] == 0xa5).all() and (y.scales[at] == 0xa5).all()
+        else:
+            assert (y[at] == -7.0).all()
+
+
+@pytest.mark.parametrize("M", [5, 300])
+def test_result_strides_and_alignment(M):
+    rng = np.random.default_rng(6)
+    n, k = 70, 256
+    a, av = rows_of(rng.normal(size=(M, k)))
+    w, wv = rows_of(rng.normal(size=(n, k)))
+    mat = mq.F8Mat.pack(w)
+    for t in (F32, BF):
+        for stride, lead in ((72, 0), (71, 0), (70, 1), (80, 8)):
+            buf = torch.full((lead + M * stride + 8,), -3.0, dtype=t, device=DEV)
+            y = buf[lead : lead + M * stride].view(M, stride)[:, :n]
+            mq.moqe_f8_gemm(a, [mat], y)
+            sync()
+            check_product(y, av, wv, None, t)
+            rest = buf.clone()
+            rest[lead : lead + M * stride].view(M, stride)[:, :n] = -3.0
+            assert (rest == -3.0).all()
+
+
+@pytest.mark.parametrize("M", [4, 200])
+def test_nan_keeps_to_its_row_and_feature(M):
+    rng = np.random.default_rng(7)
+    n, k = 100, 384
+    a, _ = rows_of(rng.normal(size=(M, k)))
+    w, _ = rows_of(rng.normal(size=(n, k)))
+    want, got = result(M, n, F32), result(M, n, F32)
+    mq.moqe_f8_gemm(a, [mq.F8Mat.pack(w)], want)
+    a.codes[2, 200], w.codes[33, 380] = 0x7f, 0xff
+    mq.moqe_f8_gemm(a, [mq.F8Mat.pack(w)], got)
+    sync()
+    assert got[2].isnan().all() and got[:, 33].isnan().all()
+    keep = torch.ones((M, n), dtype=torch.bool, device=DEV)
+    keep[2], keep[:, 33] = False, False
+    assert torch.equal(got[keep], want[keep])
+
+
+def test_far_scales():
+    """Scales at both ends of their range: products of 2^100 and 2^-110, and of 2^-120 with 2^-20, which is below fp32."""
+    a, av = rows_of(np.full((3, 128), 300.0) * np.exp2([[100.0], [-120.0], [-3.0]]))
+    w, wv = rows_of(np.full((20, 128), 1.5) * np.exp2(np.where(np.arange(20) % 2, -110.0, -20.0))[:, None])
+    y = result(3, 20, F32)
+    mq.moqe_f8_gemm(a, [mq.F8Mat.pack(w)], y)
+    sync()
+    want = av @ wv.T
+    got = f64(y)
+    assert np.allclose(got[0], want[0], rtol=2.0 ** -20, atol=0) and np.allclose(got[2], want[2], rtol=2.0 ** -20, atol=0)
+    assert (np.abs(got[1]) <= np.abs(want[1]) * (1 + 2.0 ** -20)).all()
+
+
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_products_are_the_same_every_time_and_on_streams(M):
+    rng = np.random.default_rng(8)
+    n, k = 512, 1024
+    a, _ = rows_of(rng.normal(size=(M, k)))
+    mat = mq.F8Mat.pack(rows_of(rng.normal(size=(n, k)))[0], rows_of(rng.normal(size=(n, k)))[0])
+    first = result(M, n, "f8")
+    mq.moqe_f8_gemm(a, [mat], first)
+    sync()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        again = result(M, n, "f8")
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            mq.F8GemmCall(a, [mat], again)()
+        side.synchronize()
+        assert torch.equal(first.codes, again.codes) and torch.equal(first.scales[:, :4], again.scales[:, :4])
+
+
+def test_an_mlp_in_8_bits_captured():
+    """Norm, gate and up, down, as they follow one another; replays with other work between them give the eager bits."""
+    rng = np.random.default_rng(9)
+    M, d, f = 24, 512, 1280
+    x = dev(rng.normal(size=(M, d)).astype(np.float32))
+    quant = lambda n, k: rows_of(rng.normal(size=(n, k)) * k ** -0.5)
+    gate, up, down = quant(f, d), quant(f, d), quant(d, f)
+    h8, f8, y = empty_rows(M, d), empty_rows(M, f), torch.empty((M, d), device=DEV)
+    calls = [mq.ResidualNormF8Call(None, x, h8, pre=mq.Norm("rms", 1e-6)), mq.F8GemmCall(h8, [mq.F8Mat.pack(gate[0], up[0])], f8),
+             mq.F8GemmCall(f8, [mq.F8Mat.pack(down[0])], y)]
+    for c in calls:
+        c()
+    sync()
+    want = y.clone()
+    h = f64(h8.float())
+    check_product(f8, h, gate[1], up[1], "f8")
+    check_product(y, f64(f8.float()), down[1], None, F32)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for c in calls:
+            c()
+    for _ in range(3):
+        y.fill_(0.0)
+        torch.randn(1000, device=DEV).sum().item()
+        graph.replay()
+        sync()
+        assert torch.equal(y, want)
