@@ -149,7 +149,7 @@ size_t moqe_sample_workspace_bytes(int32_t S, int32_t V) {
 int32_t moqe_sample(const void* logits, int32_t type, int64_t stride, int32_t S, int32_t V, const moqe_sampling* how, const float* u, int32_t* tokens, float* logprobs,
                     void* workspace, size_t workspace_bytes, void* stream) {
   const char* who = "moqe_sample";
-  if (S < 0 || V < 1 || V > (1 << 20) || S > (1 << 20)) return set_error(MOQE_E_SHAPE, "%s: %d rows of %d logits (at most 2^20 of each)", who, S, V);
+  if (S < 0 || V < 1 || V > (1 << 20) || S > 65535) return set_error(MOQE_E_SHAPE, "%s: %d rows (at most 65535) of %d logits (at most 2^20)", who, S, V);
   if (type != MOQE_TYPE_F32 && type != MOQE_TYPE_BF16) return set_error(MOQE_E_FORMAT, "%s: logits of type %d", who, type);
   if (!how) return set_error(MOQE_E_NULL, "%s: how is NULL", who);
   if (!aligned(how->temperature, 4) || !aligned(how->top_k, 4) || !aligned(how->top_p, 4) || !aligned(how->min_p, 4))
