@@ -16,9 +16,9 @@
 
 namespace moqe {
 
-constexpr int SMP_CHUNK = 8192, SMP_NEIGHBOURS = 256, SMP_BLOCKS = SMP_CHUNK / SMP_NEIGHBOURS;
+constexpr int SMP_THREADS = 512, SMP_NEIGHBOURS = 256;
 constexpr int SMP_BINS = 192;                  // quarters of an octave below the largest; the last one: everything that weighs nothing (2^-47 and less)
-constexpr int SMP_LIST = 8192;                 // of a row: longer lists are read from the logits instead
+constexpr int SMP_LIST = 4096;                 // of a row: longer lists are read from the logits instead
 constexpr int SMP_ONE = 43;
 
 typedef unsigned long long smp_u64;
@@ -27,12 +27,11 @@ struct SampleArgs {
   const void* logits; long long stride;
   const float* temperature; const int32_t* top_k; const float *top_p, *min_p; const float* u;
   int32_t* tokens; float* logprobs;
-  int32_t S, V, chunks;
-  struct SampleChunk* chunk; struct SampleRow* row; smp_u64* kept; uint32_t* list;       // [S][chunks], [S], [S][chunks * SMP_BLOCKS], [S][SMP_LIST]
+  int32_t S, V, chunks, blocks;                // blocks: of SMP_NEIGHBOURS logits, as the chunks have them
+  struct SampleChunk* chunk; struct SampleRow* row; smp_u64* block; uint32_t* list;      // [S][chunks], [S], [S][blocks], [S][SMP_LIST]
 };
 struct SampleChunk {
   uint32_t top, top_at;                        // largest key and its first index; 0: nothing but minus infinity and NaN
-  smp_u64 block[SMP_BLOCKS];
   smp_u64 mass[SMP_BINS];
   uint32_t count[SMP_BINS];
 };
@@ -108,13 +107,13 @@ struct SmpScale {
   __device__ double units(uint32_t key) const { return below(key) + shift * (1.0 / 256); }              // log2 of its mass
 };
 
-// Sixteen logits of a thread as keys: four at each of four places, SMP_NEIGHBOURS to a wave and place.  Past the row's end: 0.
-template <bool BF16>
-__device__ __forceinline__ void smp_load(const SampleArgs& a, int s, int chunk, uint32_t (&key)[4][4]) {
+// A thread's logits as keys: four at each of P places, SMP_NEIGHBOURS to a wave and place.  Past the row's end: 0.
+template <bool BF16, int P>
+__device__ __forceinline__ void smp_load(const SampleArgs& a, int s, int chunk, uint32_t (&key)[P][4]) {
   const char* row = static_cast<const char*>(a.logits) + s * a.stride * (BF16 ? 2 : 4);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int i = chunk * SMP_CHUNK + j * 2048 + int(threadIdx.x) * 4;
+  for (int j = 0; j < P; ++j) {
+    const int i = (chunk * P + j) * (SMP_THREADS * 4) + int(threadIdx.x) * 4;
     float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if (i + 4 <= a.V) {                                         // wide loads need no alignment beyond an element's
       if constexpr (BF16) {
@@ -141,20 +140,25 @@ __device__ __forceinline__ uint32_t smp_one(const SampleArgs& a, int s, int i) {
   else return smp_key(static_cast<const float*>(a.logits)[s * a.stride + i]);
 }
 
-__device__ __forceinline__ smp_u64 smp_wave_sum(smp_u64 v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+// Sums and maxima over a wave by moves between lanes in registers: rows of 16, then across them.  Lanes that get nothing get 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t smp_move(uint32_t v) { return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, ROWS, 0xf, false)); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ smp_u64 smp_move(smp_u64 v) { return smp_u64(smp_move<CTRL, ROWS>(uint32_t(v >> 32))) << 32 | smp_move<CTRL, ROWS>(uint32_t(v)); }
+template <typename T, typename F>
+__device__ __forceinline__ T smp_upto(T v, F&& f) {
+  v = f(v, smp_move<0x111, 0xf>(v));           // row_shr:1, 2, 4, 8
+  v = f(v, smp_move<0x112, 0xf>(v));
+  v = f(v, smp_move<0x114, 0xf>(v));
+  v = f(v, smp_move<0x118, 0xf>(v));
+  v = f(v, smp_move<0x142, 0xa>(v));           // row_bcast:15, row_bcast:31
+  return f(v, smp_move<0x143, 0xc>(v));
 }
-__device__ __forceinline__ smp_u64 smp_wave_upto(smp_u64 v) {      // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const smp_u64 o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
-}
+__device__ __forceinline__ uint32_t smp_lane(uint32_t v, int lane) { return uint32_t(__builtin_amdgcn_readlane(int(v), lane)); }
+__device__ __forceinline__ smp_u64 smp_lane(smp_u64 v, int lane) { return smp_u64(smp_lane(uint32_t(v >> 32), lane)) << 32 | smp_lane(uint32_t(v), lane); }
+template <typename T> __device__ __forceinline__ T smp_wave_upto(T v) { return smp_upto(v, [](T a, T b) { return a + b; }); }       // inclusive
+template <typename T> __device__ __forceinline__ T smp_wave_sum(T v) { return smp_lane(smp_wave_upto(v), 63); }
+__device__ __forceinline__ uint32_t smp_wave_max(uint32_t v) { return smp_lane(smp_upto(v, [](uint32_t a, uint32_t b) { return max(a, b); }), 63); }
 
 // What is asked of a row.
 struct SmpAsk {
@@ -162,15 +166,15 @@ struct SmpAsk {
   int k;                             // 0: all
   bool greedy, filtered;
   __device__ SmpAsk(const SampleArgs& a, int s) {
-    T = a.temperature ? a.temperature[s] : 1.f;
+    // all four asked for at once
+    const float t = (a.temperature ? a.temperature : a.u)[s], q = (a.top_p ? a.top_p : a.u)[s], m = (a.min_p ? a.min_p : a.u)[s];
+    const int n = (a.top_k ? a.top_k : reinterpret_cast<const int32_t*>(a.u))[s];
+    T = a.temperature ? t : 1.f;
     greedy = !(T > 0.f);
-    k = a.top_k ? a.top_k[s] : 0;
-    if (k < 1 || k >= a.V) k = 0;
-    p = a.top_p ? a.top_p[s] : 1.f;
-    if (!(p < 1.f)) p = 1.f;
+    k = a.top_k && n >= 1 && n < a.V ? n : 0;
+    p = a.top_p && q < 1.f ? q : 1.f;
     if (!(p > 0.f)) p = 0.f;
-    least = a.min_p ? a.min_p[s] : 0.f;
-    least = least > 0.f ? fminf(least, 1.f) : 0.f;
+    least = a.min_p && m > 0.f ? fminf(m, 1.f) : 0.f;
     filtered = !greedy && (k > 0 || p < 1.f || least > 0.f);
   }
 };
@@ -179,182 +183,187 @@ struct SmpAsk {
 __device__ __forceinline__ uint32_t smp_row_top(const SampleArgs& a, int s) {
   uint32_t top = 0;
   for (int c = threadIdx.x & 63; c < a.chunks; c += 64) top = max(top, a.chunk[static_cast<size_t>(s) * a.chunks + c].top);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) top = max(top, uint32_t(__shfl_xor(int(top), d)));
-  return top;
+  return smp_wave_max(top);
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(512) void k_sample_chunks(SampleArgs a) {
+template <bool BF16, int P>
+__global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
   __shared__ double powers[256];
   __shared__ uint32_t tops[8], count[SMP_BINS];
-  __shared__ int at[8];
   __shared__ smp_u64 mass[SMP_BINS];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, s = blockIdx.y, chunk = blockIdx.x;
   SampleChunk& out = a.chunk[static_cast<size_t>(s) * a.chunks + chunk];
-  uint32_t key[4][4];
-  smp_load<BF16>(a, s, chunk, key);
+  uint32_t key[P][4];
+  smp_load<BF16, P>(a, s, chunk, key);
   if (tid < 256) powers[tid] = SMP_POWERS.v[tid];
   const SmpAsk ask(a, s);
-  for (int b = tid; b < SMP_BINS; b += 512) { count[b] = 0; mass[b] = 0; }
+  if (tid < SMP_BINS) { count[tid] = 0; mass[tid] = 0; }
   uint32_t top = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < P; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) top = max(top, key[j][e]);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) top = max(top, uint32_t(__shfl_xor(int(top), d)));
+  top = smp_wave_max(top);
   if (lane == 0) tops[wave] = top;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < 8; ++w) top = max(top, tops[w]);
   if (ask.greedy) {                            // the first index of the largest
-    int first = 1 << 30;
+    uint32_t first = ~0u;
 #pragma unroll
-    for (int j = 3; j >= 0; --j)
+    for (int j = P - 1; j >= 0; --j)
 #pragma unroll
       for (int e = 3; e >= 0; --e)
-        if (key[j][e] == top) first = chunk * SMP_CHUNK + j * 2048 + tid * 4 + e;
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) first = min(first, __shfl_xor(first, d));
-    if (lane == 0) at[wave] = first;
+        if (key[j][e] == top) first = uint32_t((chunk * P + j) * (SMP_THREADS * 4) + tid * 4 + e);
+    first = ~smp_wave_max(~first);
+    __syncthreads();
+    if (lane == 0) tops[wave] = first;
     __syncthreads();
     if (tid == 0) {
 #pragma unroll
-      for (int w = 0; w < 8; ++w) first = min(first, at[w]);
+      for (int w = 0; w < 8; ++w) first = min(first, tops[w]);
       out.top = top;
-      out.top_at = uint32_t(first);
+      out.top_at = first;
     }
     return;
   }
   if (tid == 0) out.top = top;
   if (top == 0) return;
-  const double per = SmpScale::per_logit(ask.T);
-  const SmpScale sc(per, top);
+  const SmpScale sc(SmpScale::per_logit(ask.T), top);
+  const bool bins = ask.k > 0 || ask.p < 1.f;
+  smp_u64* block = a.block + static_cast<size_t>(s) * a.blocks + chunk * (P * 8) + wave;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < P; ++j) {
     smp_u64 sum = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const smp_u64 m = sc.mass(key[j][e], powers);
+      const smp_u64 m = !ask.filtered || ask.p < 1.f ? sc.mass(key[j][e], powers) : 0;
       sum += m;
-      if (ask.filtered && key[j][e] != 0) {
+      if (bins && key[j][e] != 0) {
         const int b = sc.bin(key[j][e]);
         atomicAdd(&count[b], 1u);
-        if (m) atomicAdd(&mass[b], m);
+        if (ask.p < 1.f && m) atomicAdd(&mass[b], m);
       }
     }
-    sum = smp_wave_sum(sum);
-    if (lane == 0) out.block[j * 8 + wave] = sum;
+    if (!ask.filtered) {
+      sum = smp_wave_sum(sum);
+      if (lane == 0) block[j * 8] = sum;
+    }
   }
-  if (!ask.filtered) return;
+  if (!bins) return;
   __syncthreads();
-  for (int b = tid; b < SMP_BINS; b += 512) { out.count[b] = count[b]; out.mass[b] = mass[b]; }
+  if (tid < SMP_BINS) { out.count[tid] = count[tid]; out.mass[tid] = mass[tid]; }
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(512) void k_sample_cut(SampleArgs a) {
+constexpr int SMP_CHUNKS = 128;                  // of a row at most
+
+template <bool BF16, int P>
+__global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
+  constexpr int BLOCKS = P * 8;
   __shared__ double powers[256];
-  __shared__ smp_u64 mass[SMP_BINS];
-  __shared__ uint32_t count[SMP_BINS], before[SMP_BLOCKS];
+  __shared__ smp_u64 mass[2][SMP_BINS];
+  __shared__ uint32_t count[2][SMP_BINS], before[BLOCKS];
+  __shared__ int bins_down[SMP_CHUNKS], units_down[SMP_CHUNKS];
   __shared__ SampleRow cut;
   __shared__ uint32_t list_at;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, s = blockIdx.y, chunk = blockIdx.x;
   const SmpAsk ask(a, s);
   if (!ask.filtered) return;
   const SampleChunk* of_row = a.chunk + static_cast<size_t>(s) * a.chunks;
+  uint32_t key[P][4];
+  smp_load<BF16, P>(a, s, chunk, key);
+  if (tid >= 256) powers[tid - 256] = SMP_POWERS.v[tid - 256];
   const uint32_t top = smp_row_top(a, s);
   if (top == 0) return;
-  uint32_t key[4][4];
-  smp_load<BF16>(a, s, chunk, key);
-  if (tid >= 256) powers[tid - 256] = SMP_POWERS.v[tid - 256];
   const double per = SmpScale::per_logit(ask.T);
   const SmpScale sc(per, top);
-  // the row's bins
-  if (tid < SMP_BINS) {
-    smp_u64 m = 0;
-    uint32_t n = 0;
-    for (int c = 0; c < a.chunks; ++c) {
-      if (of_row[c].top == 0) continue;
-      const SmpScale cs(per, of_row[c].top);
-      const int db = sc.bin_shift(cs), da = sc.unit_shift(cs);
-      if (tid < SMP_BINS - 1) {
-        if (tid >= db) {
-          n += of_row[c].count[tid - db];
-          if (da < 64) m += of_row[c].mass[tid - db] >> da;
-        }
-      } else {
-        for (int b = max(0, SMP_BINS - 1 - db); b < SMP_BINS; ++b) n += of_row[c].count[b];
-      }
-    }
-    count[tid] = n;
-    mass[tid] = m;
+  const bool bins = ask.k > 0 || ask.p < 1.f;
+  if (tid < a.chunks) {
+    const uint32_t t = of_row[tid].top;
+    const SmpScale cs(per, t ? t : 1);
+    bins_down[tid] = t ? sc.bin_shift(cs) : SMP_BINS;
+    units_down[tid] = t ? sc.unit_shift(cs) : 64;
   }
   __syncthreads();
-  if (wave == 0) {                               // bins 3 lane .. 3 lane + 2: sums up to them, and the bins that the cuts fall into
-    smp_u64 n[3], m[3];
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      n[i] = count[lane * 3 + i] + (i ? n[i - 1] : 0);
-      m[i] = mass[lane * 3 + i] + (i ? m[i - 1] : 0);
-    }
-    const smp_u64 n0 = smp_wave_upto(n[2]) - n[2], m0 = smp_wave_upto(m[2]) - m[2];
-#pragma unroll
-    for (int i = 0; i < 3; ++i) { n[i] += n0; m[i] += m0; }
-    auto first = [&](auto&& reached) {           // first bin with reached(sums up to it), SMP_BINS - 1 if none
-      int mine = SMP_BINS - 1;
-#pragma unroll
-      for (int i = 2; i >= 0; --i)
-        if (reached(n[i], m[i])) mine = min(mine, lane * 3 + i);
-#pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) mine = min(mine, __shfl_xor(mine, d));
-      return mine;
-    };
-    auto at = [&](const smp_u64 (&v)[3], int bin) {        // sum over the bins before `bin`
-      if (bin <= 0) return smp_u64(0);
-      const int b = bin - 1, l = b / 3, i = b - l * 3;
-      const smp_u64 mine = i == 0 ? v[0] : i == 1 ? v[1] : v[2];
-      return static_cast<smp_u64>(__shfl(mine, l));
-    };
-    SampleRow r{};
-    const smp_u64 all = __shfl(m[2], 63);
-    r.k_bin = SMP_BINS;
-    smp_u64 least = all, most = all;             // weight that top-k leaves
-    if (ask.k > 0) {
-      r.k_bin = first([&](smp_u64 cn, smp_u64) { return cn >= static_cast<smp_u64>(ask.k); });
-      if (r.k_bin == SMP_BINS - 1) r.k_bin = SMP_BINS;     // what is beyond weighs nothing
-      else {
-        r.k_above = at(n, r.k_bin);
-        r.k_mass = least = at(m, r.k_bin);
-        most = at(m, r.k_bin + 1);
+  if (bins && tid < 2 * SMP_BINS) {              // the row's bins, half the chunks each; what lies past the last one weighs nothing and is not counted
+    const int half = tid / SMP_BINS, b = tid - half * SMP_BINS, end = (half + 1) * a.chunks / 2;
+    smp_u64 m = 0;
+    uint32_t n = 0;
+#pragma unroll 8
+    for (int c = half * a.chunks / 2; c < end; ++c) {
+      const int db = bins_down[c], da = units_down[c], from = b - db;
+      if (from >= 0) {
+        n += of_row[c].count[from];
+        if (da < 64) m += of_row[c].mass[from] >> da;
       }
     }
-    r.p_lo = SMP_BINS;
+    count[half][b] = n;
+    mass[half][b] = m;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    SampleRow r{};
+    r.k_bin = r.p_lo = SMP_BINS;
     r.p_hi = -1;
-    if (ask.p < 1.f) {
-      const double lo = double(ask.p) * double(least), hi = double(ask.p) * double(most);
-      r.p_lo = first([&](smp_u64, smp_u64 cm) { return double(cm) >= lo && cm > 0; });
-      r.p_hi = first([&](smp_u64, smp_u64 cm) { return double(cm) >= hi && cm > 0; });
-      if (r.k_bin < SMP_BINS) { r.p_lo = min(r.p_lo, r.k_bin); r.p_hi = min(r.p_hi, r.k_bin); }
-      r.p_mass = at(m, r.p_lo);
-    }
-    // elements of the cuts' bins: in the row, and in the chunks ahead of this one
-    uint32_t listed = 0;
-    for (int i = 0; i < 3; ++i) {
-      const int b = lane * 3 + i;
-      if (b == r.k_bin || (b >= r.p_lo && b <= r.p_hi)) listed += count[b];
-    }
     uint32_t ahead = 0;
-    for (int c = lane; c < chunk; c += 64) {
-      if (of_row[c].top == 0) continue;
-      const int db = sc.bin_shift(SmpScale(per, of_row[c].top));
-      for (int b = r.p_lo; b <= r.p_hi; ++b)
-        if (b != r.k_bin && b >= db) ahead += of_row[c].count[b - db];
-      if (r.k_bin < SMP_BINS && r.k_bin >= db) ahead += of_row[c].count[r.k_bin - db];
+    if (bins) {                                  // bins 3 lane .. 3 lane + 2: sums up to them, and the bins that the cuts fall into
+      smp_u64 n[3], m[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        n[i] = count[0][lane * 3 + i] + count[1][lane * 3 + i] + (i ? n[i - 1] : 0);
+        m[i] = mass[0][lane * 3 + i] + mass[1][lane * 3 + i] + (i ? m[i - 1] : 0);
+      }
+      const uint32_t in_bin[3] = {uint32_t(n[0]), uint32_t(n[1] - n[0]), uint32_t(n[2] - n[1])};
+      const smp_u64 n0 = smp_wave_upto(n[2]) - n[2], m0 = smp_wave_upto(m[2]) - m[2];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) { n[i] += n0; m[i] += m0; }
+      auto first = [&](auto&& reached) {         // first bin with reached(sums up to it), which holds for all after it; SMP_BINS - 1 if none
+        const int mine = reached(n[0], m[0]) ? 0 : reached(n[1], m[1]) ? 1 : 2;
+        const smp_u64 hit = __ballot(reached(n[2], m[2]));
+        if (hit == 0) return SMP_BINS - 1;
+        const int l = __builtin_ctzll(hit);
+        return l * 3 + __builtin_amdgcn_readlane(mine, l);
+      };
+      auto before_bin = [&](const smp_u64 (&v)[3], int bin) {        // sum over the bins before it
+        if (bin <= 0) return smp_u64(0);
+        const int b = bin - 1, l = b / 3, i = b - l * 3;
+        return i == 0 ? smp_lane(v[0], l) : i == 1 ? smp_lane(v[1], l) : smp_lane(v[2], l);
+      };
+      const smp_u64 all = smp_lane(m[2], 63);
+      smp_u64 least = all, most = all;           // weight that top-k leaves
+      if (ask.k > 0) {
+        r.k_bin = first([&](smp_u64 cn, smp_u64) { return cn >= static_cast<smp_u64>(ask.k); });
+        if (r.k_bin == SMP_BINS - 1) r.k_bin = SMP_BINS;     // what is beyond weighs nothing
+        else {
+          r.k_above = before_bin(n, r.k_bin);
+          r.k_mass = least = before_bin(m, r.k_bin);
+          most = before_bin(m, r.k_bin + 1);
+        }
+      }
+      if (r.k_bin == SMP_BINS) r.k_mass = all;
+      if (ask.p < 1.f) {
+        const double lo = double(ask.p) * double(least), hi = double(ask.p) * double(most);
+        r.p_lo = first([&](smp_u64, smp_u64 cm) { return double(cm) >= lo && cm > 0; });
+        r.p_hi = first([&](smp_u64, smp_u64 cm) { return double(cm) >= hi && cm > 0; });
+        if (r.k_bin < SMP_BINS) { r.p_lo = min(r.p_lo, r.k_bin); r.p_hi = min(r.p_hi, r.k_bin); }
+        r.p_mass = before_bin(m, r.p_lo);
+      }
+      // elements of the cuts' bins: in the row, and in the chunks ahead of this one
+      uint32_t listed = 0;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int b = lane * 3 + i;
+        if (b == r.k_bin || (b >= r.p_lo && b <= r.p_hi)) listed += in_bin[i];
+      }
+      r.listed = int(smp_wave_sum(listed));
+      for (int c = lane; c < chunk; c += 64) {
+        const int db = bins_down[c];
+        for (int b = max(r.p_lo, db); b <= r.p_hi; ++b)
+          if (b != r.k_bin) ahead += of_row[c].count[b - db];
+        if (r.k_bin < SMP_BINS && r.k_bin >= db) ahead += of_row[c].count[r.k_bin - db];
+      }
+      ahead = smp_wave_sum(ahead);
     }
-    listed = uint32_t(smp_wave_sum(listed));
-    ahead = uint32_t(smp_wave_sum(ahead));
-    r.listed = int(listed);
     if (lane == 0) {
       cut = r;
       list_at = ahead;
@@ -365,9 +374,10 @@ __global__ __launch_bounds__(512) void k_sample_cut(SampleArgs a) {
   const int k_bin = cut.k_bin, p_lo = cut.p_lo, p_hi = cut.p_hi, sure = min(k_bin, p_lo);
   const bool listing = cut.listed <= SMP_LIST;
   const double floor_t = ask.least > 0.f ? log2(double(ask.least)) : -INFINITY;
-  uint32_t mine[4];                              // bits of the elements to be listed
+  smp_u64* block = a.block + static_cast<size_t>(s) * a.blocks + chunk * BLOCKS + wave;
+  uint32_t mine[P];                              // bits of the elements to be listed
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < P; ++j) {
     smp_u64 sum = 0;
     mine[j] = 0;
 #pragma unroll
@@ -381,28 +391,28 @@ __global__ __launch_bounds__(512) void k_sample_cut(SampleArgs a) {
       }
     }
     if (__any(sum != 0)) sum = smp_wave_sum(sum);
-    if (lane == 0) a.kept[(static_cast<size_t>(s) * a.chunks + chunk) * SMP_BLOCKS + j * 8 + wave] = sum;
+    if (lane == 0) block[j * 8] = sum;
     const uint32_t n = uint32_t(__popcll(__ballot(mine[j] & 1)) + __popcll(__ballot(mine[j] & 2)) + __popcll(__ballot(mine[j] & 4)) + __popcll(__ballot(mine[j] & 8)));
     if (lane == 0) before[j * 8 + wave] = n;
   }
-  if (!listing) return;
+  if (!bins || !listing) return;
   __syncthreads();
   uint32_t* list = a.list + static_cast<size_t>(s) * SMP_LIST;
+  const uint32_t ahead_of = smp_wave_upto(lane < BLOCKS ? before[lane] : 0u);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < P; ++j) {
     if (!__any(mine[j] != 0)) continue;
-    uint32_t at = list_at;
-    for (int b = 0; b < j * 8 + wave; ++b) at += before[b];
-    at += uint32_t(smp_wave_upto(__popc(mine[j]))) - __popc(mine[j]);
+    const int b = __builtin_amdgcn_readfirstlane(j * 8 + wave);
+    uint32_t at = list_at + (b ? smp_lane(ahead_of, b - 1) : 0u) + smp_wave_upto(uint32_t(__popc(mine[j]))) - __popc(mine[j]);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if ((mine[j] >> e & 1) && at < SMP_LIST) list[at++] = uint32_t(chunk * SMP_CHUNK + j * 2048 + tid * 4 + e);
+      if ((mine[j] >> e & 1) && at < SMP_LIST) list[at++] = uint32_t((chunk * P + j) * (SMP_THREADS * 4) + tid * 4 + e);
   }
 }
 
-// Sum over the work-group of 1024, and inclusive sums.
+// Sum over the work-group, and inclusive sums.
 struct SmpGroup {
-  smp_u64* part;                                 // [16]
+  smp_u64* part;                                 // [8]
   __device__ smp_u64 sum(smp_u64 v) const {
     v = smp_wave_sum(v);
     __syncthreads();
@@ -410,7 +420,7 @@ struct SmpGroup {
     __syncthreads();
     v = 0;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) v += part[w];
+    for (int w = 0; w < 8; ++w) v += part[w];
     return v;
   }
   __device__ smp_u64 upto(smp_u64 v) const {
@@ -418,22 +428,27 @@ struct SmpGroup {
     __syncthreads();
     if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = v;
     __syncthreads();
-    for (int w = 0; w < int(threadIdx.x >> 6); ++w) v += part[w];
+#pragma unroll
+    for (int w = 0; w < 7; ++w) v += w < int(threadIdx.x >> 6) ? part[w] : 0;
     return v;
   }
 };
 
 template <bool BF16>
-__global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
-  constexpr int EACH = SMP_LIST / 1024, KEYS = 1024;
+__global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
+  constexpr int EACH = SMP_LIST / SMP_THREADS, KEYS = 1024, PER = (1 << 20) / SMP_NEIGHBOURS / SMP_THREADS;
   __shared__ double powers[256];
-  __shared__ smp_u64 part[16], hist[KEYS], blocks[(1 << 20) / SMP_NEIGHBOURS];
+  __shared__ smp_u64 part[8], hist[KEYS], blocks[(1 << 20) / SMP_NEIGHBOURS];
   __shared__ smp_u64 found[2];
-  __shared__ int found_at;
+  __shared__ int found_at, units_down[SMP_CHUNKS];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, s = blockIdx.x, V = a.V;
   const SmpGroup group{part};
   const SmpAsk ask(a, s);
   const SampleChunk* of_row = a.chunk + static_cast<size_t>(s) * a.chunks;
+  const int n_blocks = a.blocks, per_chunk = n_blocks / a.chunks;
+  const smp_u64* row_blocks = a.block + static_cast<size_t>(s) * n_blocks;
+  smp_u64 first_blocks = tid < n_blocks ? row_blocks[tid] : 0;        // asked for before it is known how they count
+  if (tid < 256) powers[tid] = SMP_POWERS.v[tid];
   const uint32_t top = smp_row_top(a, s);
   if (top == 0) {
     if (tid == 0) {
@@ -447,27 +462,25 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
     uint32_t first = ~0u;
     for (int c = lane; c < a.chunks; c += 64)
       if (of_row[c].top == top) first = min(first, of_row[c].top_at);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) first = min(first, uint32_t(__shfl_xor(int(first), d)));
+    first = ~smp_wave_max(~first);
     if (lane == 0) {
       a.tokens[s] = int(first);
       if (a.logprobs) a.logprobs[s] = 0.f;
     }
     return;
   }
-  if (tid < 256) powers[tid] = SMP_POWERS.v[tid];
   const double per = SmpScale::per_logit(ask.T);
   const SmpScale sc(per, top);
-  const int n_blocks = a.chunks * SMP_BLOCKS;
   const double floor_t = ask.least > 0.f ? log2(double(ask.least)) : -INFINITY;
-  for (int b = tid; b < n_blocks; b += 1024) {
-    if (ask.filtered) {
-      blocks[b] = a.kept[static_cast<size_t>(s) * n_blocks + b];
-    } else {
-      const SampleChunk& c = of_row[b / SMP_BLOCKS];
-      const int da = c.top ? sc.unit_shift(SmpScale(per, c.top)) : 64;
-      blocks[b] = da < 64 ? c.block[b % SMP_BLOCKS] >> da : 0;
-    }
+  if (tid < a.chunks) {
+    const uint32_t t = of_row[tid].top;
+    units_down[tid] = t ? ask.filtered ? 0 : sc.unit_shift(SmpScale(per, t)) : 64;
+  }
+  __syncthreads();
+  for (int b = tid; b < n_blocks; b += SMP_THREADS) {
+    const int da = units_down[b / per_chunk];
+    const smp_u64 v = b == tid ? first_blocks : row_blocks[b];
+    blocks[b] = da < 64 ? v >> da : 0;
   }
   __syncthreads();
 
@@ -485,7 +498,7 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
       at[i] = listing && n < r.listed ? min(list[n], uint32_t(V - 1)) : 0;
       key[i] = listing && n < r.listed ? smp_one<BF16>(a, s, int(at[i])) : 0;
     }
-    const int run = (V + 1023) / 1024;           // without a list: so many logits a thread, neighbours too
+    const int run = (V + SMP_THREADS - 1) / SMP_THREADS;           // without a list: so many logits a thread, neighbours too
     auto each = [&](auto&& f) {                  // f(key, index) of every element of bins that are in question, by each thread in order
       if (listing) {
 #pragma unroll
@@ -505,16 +518,13 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
       each([&](uint32_t x, int i) {
         if (in(x, i)) { lo = min(lo, x); hi = max(hi, x); }
       });
-#pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) {
-        lo = min(lo, uint32_t(__shfl_xor(int(lo), d)));
-        hi = max(hi, uint32_t(__shfl_xor(int(hi), d)));
-      }
+      lo = ~smp_wave_max(~lo);
+      hi = smp_wave_max(hi);
       __syncthreads();
       if (lane == 0) part[wave] = smp_u64(hi) << 32 | lo;
       __syncthreads();
 #pragma unroll
-      for (int w = 0; w < 16; ++w) {
+      for (int w = 0; w < 8; ++w) {
         lo = min(lo, uint32_t(part[w]));
         hi = max(hi, uint32_t(part[w] >> 32));
       }
@@ -525,7 +535,7 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
         const uint32_t range = hi - lo;
         const int shift = max(0, 32 - __builtin_clz(range | 1) - 10);
         __syncthreads();
-        hist[tid] = 0;
+        hist[2 * tid] = hist[2 * tid + 1] = 0;
         if (tid == 0) found_at = KEYS;
         __syncthreads();
         each([&](uint32_t x, int i) {
@@ -535,10 +545,11 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
           }
         });
         __syncthreads();
-        const smp_u64 mine = hist[tid], upto = over + group.upto(mine);
-        if (upto >= target && upto - mine < target) {            // one bin at most
-          found_at = tid;
-          found[0] = upto - mine;
+        const smp_u64 one = hist[2 * tid], two = hist[2 * tid + 1], upto = over + group.upto(one + two), ahead = upto - one - two;
+        if (upto >= target && ahead < target) {                  // one thread at most
+          const bool second = ahead + one < target;
+          found_at = 2 * tid + second;
+          found[0] = ahead + (second ? one : 0);
         }
         __syncthreads();
         const int bin = found_at;
@@ -588,15 +599,7 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
         whole = r.k_mass + group.sum(m);
       }
     } else if (cut_p) {
-      // no cut by top-k: all of the row's weight
-      smp_u64 m = 0;
-      for (int c = tid; c < a.chunks; c += 1024) {
-        if (of_row[c].top == 0) continue;
-        const int da = sc.unit_shift(SmpScale(per, of_row[c].top));
-        if (da < 64)
-          for (int b = 0; b < SMP_BINS; ++b) m += of_row[c].mass[b] >> da;
-      }
-      whole = group.sum(m);
+      whole = r.k_mass;                          // no cut by top-k: all of the row's weight
     }
     if (cut_p) {
       const uint32_t k_cut = cut;
@@ -629,12 +632,13 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
     __syncthreads();
   }
 
-  // the neighbourhood: thread t has blocks 4 t .. 4 t + 3
+  // the neighbourhood: thread t has some that follow one another
+  const int each_t = (n_blocks + SMP_THREADS - 1) / SMP_THREADS, b0 = tid * each_t, b1 = min(n_blocks, b0 + each_t);
+  static_assert(PER <= 8, "");
   smp_u64 mine = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) mine += tid * 4 + i < n_blocks ? blocks[tid * 4 + i] : 0;
+  for (int b = b0; b < b1; ++b) mine += blocks[b];
   const smp_u64 upto = group.upto(mine);
-  if (tid == 1023) found[1] = upto;
+  if (tid == SMP_THREADS - 1) found[1] = upto;
   __syncthreads();
   const smp_u64 W = found[1];
   float u = a.u[s];
@@ -645,7 +649,7 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
   goal = goal > W ? W : goal;
   if (upto >= goal && upto - mine < goal) {
     smp_u64 run = upto - mine;
-    int b = tid * 4;
+    int b = b0;
     while (run + blocks[b] < goal) run += blocks[b++];
     found_at = b;
     found[0] = goal - run;
@@ -664,7 +668,7 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
     m[e] = in ? sc.mass(x[e], powers) : 0;
     own += m[e];
   }
-  const smp_u64 run_upto = smp_wave_upto(own), in_block = __shfl(run_upto, 63);
+  const smp_u64 run_upto = smp_wave_upto(own), in_block = smp_lane(run_upto, 63);
   if (goal > in_block) goal = in_block;          // sums of a chunk's units and of the row's may differ in the last unit
   if (run_upto >= goal && run_upto - own < goal) {
     smp_u64 run = run_upto - own;
@@ -679,13 +683,14 @@ __global__ __launch_bounds__(1024) void k_sample_draw(SampleArgs a) {
 }
 
 namespace {
-struct SampleSpace { size_t row, kept, list, total; };
+struct SampleSpace { int places, chunks; size_t row, block, list, total; };
 SampleSpace space(int S, int V) {
-  const size_t chunks = (size_t(V) + SMP_CHUNK - 1) / SMP_CHUNK;
   SampleSpace p;
-  p.row = align256(size_t(S) * chunks * sizeof(SampleChunk));
-  p.kept = p.row + align256(size_t(S) * sizeof(SampleRow));
-  p.list = p.kept + align256(size_t(S) * chunks * SMP_BLOCKS * 8);
+  p.places = static_cast<long long>(S) * V < (1 << 21) && V <= SMP_CHUNKS * SMP_THREADS * 4 ? 1 : 4;
+  p.chunks = (V + p.places * SMP_THREADS * 4 - 1) / (p.places * SMP_THREADS * 4);
+  p.row = align256(size_t(S) * p.chunks * sizeof(SampleChunk));
+  p.block = p.row + align256(size_t(S) * sizeof(SampleRow));
+  p.list = p.block + align256(size_t(S) * p.chunks * p.places * 8 * 8);
   p.total = p.list + align256(size_t(S) * SMP_LIST * 4);
   return p;
 }
@@ -697,19 +702,24 @@ int32_t launch_sample(const void* logits, bool bf16, long long stride, int S, in
                       void* ws, hipStream_t st) {
   const SampleSpace p = space(S, V);
   uint8_t* b = static_cast<uint8_t*>(ws);
-  SampleArgs a{logits, stride, how.temperature, how.top_k, how.top_p, how.min_p, u, tokens, logprobs, S, V, (V + SMP_CHUNK - 1) / SMP_CHUNK,
-               reinterpret_cast<SampleChunk*>(b), reinterpret_cast<SampleRow*>(b + p.row), reinterpret_cast<smp_u64*>(b + p.kept), reinterpret_cast<uint32_t*>(b + p.list)};
+  SampleArgs a{logits, stride, how.temperature, how.top_k, how.top_p, how.min_p, u, tokens, logprobs, S, V, p.chunks, p.chunks * p.places * 8,
+               reinterpret_cast<SampleChunk*>(b), reinterpret_cast<SampleRow*>(b + p.row), reinterpret_cast<smp_u64*>(b + p.block), reinterpret_cast<uint32_t*>(b + p.list)};
   ProfileScope ps(MOQE_PK_OTHER, st);
   const bool filters = how.top_k || how.top_p || how.min_p;
-  const dim3 chunks(a.chunks, S);
-  auto go = [&](auto bf) {
+  const dim3 chunks(p.chunks, S), threads(SMP_THREADS);
+  auto go = [&](auto bf, auto places) {
     constexpr bool BF16 = decltype(bf)::value;
-    hipLaunchKernelGGL((k_sample_chunks<BF16>), chunks, dim3(512), 0, st, a);
-    if (filters) hipLaunchKernelGGL((k_sample_cut<BF16>), chunks, dim3(512), 0, st, a);
-    hipLaunchKernelGGL((k_sample_draw<BF16>), dim3(S), dim3(1024), 0, st, a);
+    constexpr int P = decltype(places)::value;
+    hipLaunchKernelGGL((k_sample_chunks<BF16, P>), chunks, threads, 0, st, a);
+    if (filters) hipLaunchKernelGGL((k_sample_cut<BF16, P>), chunks, threads, 0, st, a);
+    hipLaunchKernelGGL((k_sample_draw<BF16>), dim3(S), threads, 0, st, a);
   };
-  if (bf16) go(std::true_type());
-  else go(std::false_type());
+  auto with = [&](auto bf) {
+    if (p.places == 1) go(bf, std::integral_constant<int, 1>());
+    else go(bf, std::integral_constant<int, 4>());
+  };
+  if (bf16) with(std::true_type());
+  else with(std::false_type());
   return check_launch("sample");
 }
 
