@@ -117,6 +117,19 @@ def test_special_values():
     assert check(x, uniform(12, 9), temperature=[0.0] * 12)[3] == 5
 
 
+@pytest.mark.parametrize("t", [F32, BF])
+def test_every_kind_of_nan_is_passed_over(t):
+    x = logits_of(3, 900, t)
+    bits = x.view(torch.int16 if t == BF else torch.int32)
+    kinds = [0x7fc0, 0x7f81, 0xffc0 - 65536, 0xff81 - 65536] if t == BF else [0x7fc00000, 0x7f800001, 0xffc00000 - (1 << 32), 0xff800001 - (1 << 32)]
+    for i, b in enumerate(kinds):
+        bits[:, i::7] = b
+    assert int(x.isnan().sum()) == 3 * sum(len(range(i, 900, 7)) for i in range(4))
+    check(x, uniform(3))
+    check(x, uniform(3), top_k=[5, 0, 100], top_p=[0.9, 0.5, 1.0])
+    check(x, uniform(3), temperature=[0.0] * 3)
+
+
 def test_u_at_its_ends():
     x = logits_of(4, 2000)
     x[:, -300:] = -float("inf")
