@@ -135,7 +135,6 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
     g.y8 = y->rows8.codes; g.y8_scales = y->rows8.scales; g.y8_stride = y->rows8.code_stride; g.y8_scale_stride = y->rows8.scale_stride;
   } else {
     g.y = y->data; g.y_stride = y->stride; g.y_bf16 = y->type == MOQE_TYPE_BF16;
-    g.wide = y->stride % 4 == 0 && aligned(y->data, g.y_bf16 ? 8 : 16);
   }
   if (dry_run()) return MOQE_OK;
   return launch_f8_gemm(g, gated, workspace, static_cast<hipStream_t>(stream));

@@ -58,7 +58,7 @@ struct F8Args {
   uint32_t a_stride, as_stride;                  // bytes
   int32_t S, T, K, n, tiles, blocks, groups;
   uint32_t scale_off;
-  int32_t y_bf16, wide;                          // wide: y and its stride allow stores of four values
+  int32_t y_bf16;
 };
 // Bucket of an expert in rows: first row and number.  Device values are taken into their ranges.
 __device__ __forceinline__ int2 f8_bucket(const F8Args& a, int e) {
@@ -77,16 +77,17 @@ __device__ __forceinline__ uint32_t f8_bf16_pair(float lo, float hi) {
   const __bf16 l = static_cast<__bf16>(lo), h = static_cast<__bf16>(hi);
   return uint32_t(__builtin_bit_cast(uint16_t, l)) | uint32_t(__builtin_bit_cast(uint16_t, h)) << 16;
 }
-// Four values of a row from column n0 on.
+// Four values of a row from column n0 on.  Wide stores need no alignment beyond an element's.
 __device__ __forceinline__ void f8_store(const F8Args& a, int row, int n0, f8_f32x4 v) {
   const long long at = row * a.y_stride + n0;
-  if (a.wide && n0 + 4 <= a.n) {
-    if (a.y_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + at) = make_uint2(f8_bf16_pair(v[0], v[1]), f8_bf16_pair(v[2], v[3]));
-    else *reinterpret_cast<f8_f32x4*>(static_cast<float*>(a.y) + at) = v;
+  if (n0 + 4 <= a.n) {
+    const uint2 h = make_uint2(f8_bf16_pair(v[0], v[1]), f8_bf16_pair(v[2], v[3]));
+    if (a.y_bf16) __builtin_memcpy(static_cast<uint16_t*>(a.y) + at, &h, 8);
+    else __builtin_memcpy(static_cast<float*>(a.y) + at, &v, 16);
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 3; ++i)
     if (n0 + i < a.n) {
       if (a.y_bf16) static_cast<uint16_t*>(a.y)[at + i] = uint16_t(f8_bf16_pair(v[i], 0.f));
       else static_cast<float*>(a.y)[at + i] = v[i];

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256) void k_f8_quantize(F8Args a, const float* h) {
   if (lane == 0) a.y8_scales[row * a.y8_scale_stride + blockIdx.y] = uint8_t(e + 127);
 }
 
-int32_t launch_f8_few(const F8Args& a, bool gated, bool exact, int mb, int wt, hipStream_t st) {
+int32_t launch_f8_few(const F8Args& a, bool gated, bool exact, int blocks, int cols, hipStream_t st) {
   const long long M = static_cast<long long>(a.S) * a.T;
   const uint32_t a_bytes = uint32_t((M - 1) * a.a_stride + a.blocks * 128ll), as_bytes = uint32_t((M - 1) * a.as_stride + a.groups * 4ll);
   const uint32_t w_bytes = uint32_t(size_t(a.scale_off) + size_t(a.tiles) * a.groups * 64);
@@ -144,14 +144,9 @@ int32_t launch_f8_few(const F8Args& a, bool gated, bool exact, int mb, int wt, h
     if (exact) hipLaunchKernelGGL((k_f8_few<MB, WT, false, true>), grid, block, 0, st, a, a_bytes, as_bytes, w_bytes);
     else hipLaunchKernelGGL((k_f8_few<MB, WT, false, false>), grid, block, 0, st, a, a_bytes, as_bytes, w_bytes);
   };
-  auto with = [&](auto mbc) {
-    if (wt == 1 && !gated) go(mbc, std::integral_constant<int, 1>());
-    else if (wt <= 2 || decltype(mbc)::value == 4) go(mbc, std::integral_constant<int, 2>());
-    else go(mbc, std::integral_constant<int, 4>());
-  };
-  if (mb == 1) with(std::integral_constant<int, 1>());
-  else if (mb == 2) with(std::integral_constant<int, 2>());
-  else with(std::integral_constant<int, 4>());
+  if (blocks == 2) go(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
+  else if (cols == 2) go(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+  else go(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
   return check_launch("f8_gemm");
 }
 

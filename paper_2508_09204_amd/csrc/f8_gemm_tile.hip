@@ -274,32 +274,16 @@ static int32_t launch_tile(const F8Args& a, bool gated, hipStream_t st) {
   return check_launch("f8_gemm");
 }
 
-int32_t launch_f8_tile(const F8Args& a, bool gated, bool exact, int shape, hipStream_t st) {
+// The tiles of f8_shape().  fp32 results: no 128 rows, whose operands in bf16 the registers do not hold.
+int32_t launch_f8_tile(const F8Args& a, bool gated, bool exact, int rows, int cols, int parts, hipStream_t st) {
   if (exact) {
-    switch (shape) {
-      case 2: return launch_tile<4, 2, 1, 3, true>(a, gated, st);
-      case 3: return launch_tile<4, 1, 1, 3, true>(a, gated, st);
-      case 4: return launch_tile<4, 1, 2, 3, true>(a, gated, st);
-      case 5: return launch_tile<4, 1, 4, 3, true>(a, gated, st);
-      case 6: return launch_tile<4, 2, 2, 3, true>(a, gated, st);
-      case 7: return launch_tile<2, 2, 2, 3, true>(a, gated, st);
-      case 8: return launch_tile<2, 1, 4, 3, true>(a, gated, st);
-      case 9: return launch_tile<2, 2, 1, 3, true>(a, gated, st);
-      default: return launch_tile<4, 4, 1, 1, true>(a, gated, st);
-    }
+    if (cols == 16) return launch_tile<4, 4, 1, 1, true>(a, gated, st);
+    if (cols == 8) return rows == 64 ? launch_tile<4, 2, 1, 3, true>(a, gated, st) : parts == 1 ? launch_tile<2, 2, 1, 3, true>(a, gated, st) : launch_tile<2, 2, 2, 3, true>(a, gated, st);
+    return rows == 64 ? launch_tile<4, 1, 2, 3, true>(a, gated, st) : launch_tile<2, 1, 4, 3, true>(a, gated, st);
   }
-  switch (shape) {
-    case 0: return launch_tile<8, 4, 1, 1, false>(a, gated, st);
-    case 2: return launch_tile<4, 2, 1, 3, false>(a, gated, st);
-    case 3: return launch_tile<4, 1, 1, 3, false>(a, gated, st);
-    case 4: return launch_tile<4, 1, 2, 3, false>(a, gated, st);
-    case 5: return launch_tile<4, 1, 4, 3, false>(a, gated, st);
-    case 6: return launch_tile<4, 2, 2, 3, false>(a, gated, st);
-    case 7: return launch_tile<2, 2, 2, 3, false>(a, gated, st);
-    case 8: return launch_tile<2, 1, 4, 3, false>(a, gated, st);
-    case 9: return launch_tile<2, 2, 1, 3, false>(a, gated, st);
-    default: return launch_tile<4, 4, 1, 1, false>(a, gated, st);
-  }
+  if (cols == 16) return rows == 128 ? launch_tile<8, 4, 1, 1, false>(a, gated, st) : launch_tile<4, 4, 1, 1, false>(a, gated, st);
+  if (cols == 8) return rows == 64 ? launch_tile<4, 2, 1, 3, false>(a, gated, st) : parts == 1 ? launch_tile<2, 2, 1, 3, false>(a, gated, st) : launch_tile<2, 2, 2, 3, false>(a, gated, st);
+  return rows == 64 ? launch_tile<4, 1, 2, 3, false>(a, gated, st) : launch_tile<2, 1, 4, 3, false>(a, gated, st);
 }
 
 }  // namespace moqe

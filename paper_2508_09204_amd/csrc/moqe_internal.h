@@ -261,8 +261,8 @@ int32_t check_f8_rows(const moqe_f8_rows* r, int32_t d, const char* what, const 
 int32_t launch_f8_pack(const moqe_f8_rows& w, const moqe_f8_rows* up, int n, int k, uint8_t* out, hipStream_t st);
 int32_t launch_f8_unpack(const moqe_f8_mat& m, const moqe_f8_rows& w, const moqe_f8_rows* up, hipStream_t st);
 int32_t launch_f8_gemm(const F8Args& a, bool gated, void* ws, hipStream_t st);
-int32_t launch_f8_tile(const F8Args& a, bool gated, bool exact, int shape, hipStream_t st);
-int32_t launch_f8_few(const F8Args& a, bool gated, bool exact, int mb, int wt, hipStream_t st);
+int32_t launch_f8_tile(const F8Args& a, bool gated, bool exact, int rows, int cols, int parts, hipStream_t st);
+int32_t launch_f8_few(const F8Args& a, bool gated, bool exact, int blocks, int cols, hipStream_t st);
 int32_t launch_f8_quantize(const F8Args& a, const float* h, hipStream_t st);
 size_t  f8_gemm_ws_bytes(long long M, int n, int k, int K, bool gated, bool out8);
 int32_t launch_sample(const void* logits, bool bf16, long long stride, int S, int V, const moqe_sampling& how, const float* u, int32_t* tokens, float* logprobs,
