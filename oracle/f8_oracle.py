@@ -40,7 +40,7 @@ def product(a, w, up=None):
 
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
-    """Token of one row, its log probability, and the gap in units of the whole weight to the nearest choice that would have come out differently."""
+    """Token of one row, its log probability, and the gap in units of the largest weight to the nearest choice that would have come out differently."""
     x = np.asarray(logits, dtype=np.float64)
     live = [i for i in range(len(x)) if x[i] > -np.inf]
     if not live:
@@ -59,7 +59,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     if top_p < 1:
         run, whole = np.concatenate([[0.0], np.cumsum(w[:n])]), w[:n].sum()
         want = max(top_p, 0.0) * whole
-        gap = min(gap, np.abs(run[1:] - want).min() / whole) if top_p > 0 else gap
+        gap = min(gap, np.abs(run[1:] - want).min()) if top_p > 0 else gap
         n = max(1, int((run[:-1] < want).sum()))
     if min_p > 0:
         least = min(min_p, 1.0)
@@ -71,5 +71,5 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     i = int((run <= goal).sum())
     if i >= n:                                                 # u is 1: the last token with weight
         i = max(j for j in range(n) if w[at[j]] > 0)
-    gap = min(gap, np.abs(run - goal).min() / run[-1] if goal > 0 else 1.0)
+    gap = min(gap, np.abs(run - goal).min() if goal > 0 else 1.0)
     return live[at[i]], math.log(w[at[i]] / run[-1]), gap

@@ -21,7 +21,8 @@ constexpr int SMP_THREADS = 512, SMP_NEIGHBOURS = 256;
 constexpr int SMP_CHUNKS = 128;                // of a row at most
 constexpr int SMP_BLOCKS = (1 << 20) / SMP_NEIGHBOURS;      // neighbourhoods of a row at most
 constexpr int SMP_BINS = 192;                  // quarters of an octave below the largest; the last one: everything that weighs nothing (2^-47 and less)
-constexpr int SMP_LIST = 4096;                 // of a row: longer lists are read from the logits instead
+constexpr int SMP_LIST = 16384;                // of a row at most: where the cuts' bins have more, the row is read instead
+constexpr int SMP_HELD = 4096;                 // of them in LDS: longer lists are read again for every pass
 constexpr int SMP_ONE = 43;
 
 typedef unsigned long long smp_u64;
@@ -30,8 +31,8 @@ struct SampleArgs {
   const void* logits; long long stride;
   const float* temperature; const int32_t* top_k; const float *top_p, *min_p; const float* u;
   int32_t* tokens; float* logprobs;
-  int32_t S, V, chunks, blocks;                // blocks: of SMP_NEIGHBOURS logits, as the chunks have them
-  struct SampleChunk* chunk; struct SampleRow* row; smp_u64* block; uint32_t* list;      // [S][chunks], [S], [S][blocks], [S][SMP_LIST]
+  int32_t S, V, chunks, blocks, list_size;     // blocks: of SMP_NEIGHBOURS logits, as the chunks have them
+  struct SampleChunk* chunk; struct SampleRow* row; smp_u64* block; uint2* list;      // [S][chunks], [S], [S][blocks], [S][list_size] (bits, index)
 };
 struct SampleChunk {
   float top;                                   // minus infinity: there is nothing else
@@ -458,9 +459,9 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
     const uint32_t n = uint32_t(__popcll(__ballot(mine[j] & 1)) + __popcll(__ballot(mine[j] & 2)) + __popcll(__ballot(mine[j] & 4)) + __popcll(__ballot(mine[j] & 8)));
     if (lane == 0) before[j * 8 + wave] = n;
   }
-  if (cut.listed == 0 || cut.listed > SMP_LIST) return;
+  if (cut.listed == 0 || cut.listed > a.list_size) return;
   __syncthreads();
-  uint32_t* list = a.list + static_cast<size_t>(s) * SMP_LIST;
+  uint2* list = a.list + static_cast<size_t>(s) * a.list_size;
   const uint32_t ahead_of = smp_wave_upto(lane < BLOCKS ? before[lane] : 0u);
 #pragma unroll
   for (int j = 0; j < P; ++j) {
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
     uint32_t at = list_at + (b ? smp_lane(ahead_of, b - 1) : 0u) + smp_wave_upto(uint32_t(__popc(mine[j]))) - __popc(mine[j]);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if ((mine[j] >> e & 1) && at < SMP_LIST) list[at++] = uint32_t((chunk * P + j) * (SMP_THREADS * 4) + tid * 4 + e);
+      if ((mine[j] >> e & 1) && at < uint32_t(a.list_size)) list[at++] = make_uint2(__float_as_uint(v[j][e]), uint32_t((chunk * P + j) * (SMP_THREADS * 4) + tid * 4 + e));
   }
 }
 
@@ -502,9 +503,9 @@ template <bool BF16>
 __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
   constexpr int KEYS = 1024;
   __shared__ double powers[256];
-  __shared__ smp_u64 part[8], hist[KEYS], blocks[SMP_BLOCKS], found;
-  __shared__ float list_v[SMP_LIST];
-  __shared__ uint32_t list_i[SMP_LIST], lows[8], highs[8];
+  __shared__ smp_u64 part[8], hist[KEYS], blocks[SMP_BLOCKS], found, found_here;
+  __shared__ uint2 held[SMP_HELD];
+  __shared__ uint32_t lows[8], highs[8];
   __shared__ int found_at, units_down[SMP_CHUNKS];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, s = blockIdx.x, V = a.V;
   const SmpGroup group{part};
@@ -548,13 +549,10 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
   int bound = V;
   SampleRow r{SMP_BINS, SMP_BINS, -1, 0, 0, 0, 0};
   if (ask.filtered) r = a.row[s];
-  const bool listing = r.listed <= SMP_LIST;
-  if (r.listed > 0 && listing)
-    for (int i = tid; i < r.listed; i += SMP_THREADS) {
-      const uint32_t at = min(a.list[static_cast<size_t>(s) * SMP_LIST + i], uint32_t(V - 1));
-      list_i[i] = at;
-      list_v[i] = sc.clean(smp_one<BF16>(a, s, int(at)));
-    }
+  const uint2* list = a.list + static_cast<size_t>(s) * a.list_size;
+  const bool in_lds = r.listed <= SMP_HELD, in_list = r.listed <= a.list_size;
+  if (in_lds && in_list)
+    for (int i = tid; i < r.listed; i += SMP_THREADS) held[i] = list[i];
   __syncthreads();
   for (int b = tid; b < n_blocks; b += SMP_THREADS) {
     const int da = units_down[b / per_chunk];
@@ -562,33 +560,51 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
     blocks[b] = da < 64 ? x >> da : 0;
   }
   if (r.listed > 0) {
-    // elements of the bins in question, neighbours to a thread: from the list, or without one all of the row
-    const int n = listing ? r.listed : V, run = ((n + SMP_THREADS - 1) / SMP_THREADS) | 1, i0 = min(n, tid * run), i1 = min(n, i0 + run);
-    auto each = [&](auto&& f) {                  // f(logit, index), by each thread in order
+    const int n = in_list ? r.listed : V;
+    auto each = [&](auto&& f) {                  // f(logit, index) of every element of the bins in question, and others of the row where there is no list
 #pragma unroll 1
-      for (int i = i0; i < i1; ++i) {
-        const float x = listing ? list_v[i] : sc.clean(smp_one<BF16>(a, s, i));
-        if (x > -INFINITY) f(x, listing ? int(list_i[i]) : i);
+      for (int i = tid; i < n; i += SMP_THREADS) {
+        const uint2 y = !in_list ? make_uint2(__float_as_uint(sc.clean(smp_one<BF16>(a, s, i))), i) : in_lds ? held[i] : list[i];
+        const float x = __uint_as_float(y.x);
+        if (x > -INFINITY) f(x, min(int(y.y), V - 1));
       }
     };
     smp_u64 whole = r.k_mass;                    // weight that top-k leaves
+    int b_lo = 0, b_hi = 0, k_bound = bound;
+    float k_cut = cut;
+    smp_u64 target = 0;
+    bool indexes = false;
 #pragma unroll 1
-    for (int stage = 0; stage < 2; ++stage) {    // top-k by counts, top-p by weights
-      const bool by_mass = stage == 1;
-      if (by_mass ? !(ask.p < 1.f) : r.k_bin == SMP_BINS) continue;
-      const int b_lo = by_mass ? r.p_lo : r.k_bin, b_hi = by_mass ? r.p_hi : r.k_bin, k_bound = bound;
-      const float k_cut = cut;
+    for (int stage = 0; stage < 4; ++stage) {    // top-k by counts, the elements equal to its cut by index, top-p by weights, those equal to its cut
+      const bool by_mass = stage == 2, by_index = stage & 1;
+      if (by_index ? !indexes : by_mass ? !(ask.p < 1.f) : r.k_bin == SMP_BINS) continue;
+      if (!by_index) {
+        if (by_mass && r.k_bin < SMP_BINS) {
+          smp_u64 m = 0;
+          each([&](float x, int i) {
+            if (sc.bin(x) == r.k_bin && (x > cut || (x == cut && i < bound))) m += sc.mass(x, powers);
+          });
+          whole = r.k_mass + group.sum(m);
+          __syncthreads();
+        }
+        b_lo = by_mass ? r.p_lo : r.k_bin;
+        b_hi = by_mass ? r.p_hi : r.k_bin;
+        k_cut = cut;
+        k_bound = bound;
+        const double goal = double(ask.p) * double(whole) - double(r.p_mass);
+        target = !by_mass ? static_cast<smp_u64>(ask.k) - r.k_above : goal > 1. ? static_cast<smp_u64>(ceil(goal)) : 1;       // the first one is kept always
+      }
+      indexes = false;
       auto in = [&](float x, int i) {
         const int b = sc.bin(x);
-        return b >= b_lo && b <= b_hi && (x > k_cut || (x == k_cut && i < k_bound));
+        return b >= b_lo && b <= b_hi && (x > k_cut || (x == k_cut && i < k_bound)) && (!by_index || x == cut);
       };
-      const double goal = double(ask.p) * double(whole) - double(r.p_mass);
-      const smp_u64 target = !by_mass ? static_cast<smp_u64>(ask.k) - r.k_above : goal > 1. ? static_cast<smp_u64>(ceil(goal)) : 1;       // the first one is kept always
+      auto key = [&](float x, int i) { return by_index ? ~uint32_t(i) : smp_key<BF16>(x); };
       // the largest key with the sum over it and those above it >= target
       uint32_t lo = ~0u, hi = 0;
       each([&](float x, int i) {
         if (in(x, i)) {
-          const uint32_t k = smp_key<BF16>(x);
+          const uint32_t k = key(x, i);
           lo = min(lo, k);
           hi = max(hi, k);
         }
@@ -599,9 +615,12 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
       __syncthreads();
 #pragma unroll
       for (int w = 0; w < 8; ++w) { lo = min(lo, lows[w]); hi = max(hi, highs[w]); }
-      if (hi < lo) continue;
+      if (hi < lo) {
+        __syncthreads();
+        continue;
+      }
       const uint32_t lowest = lo;
-      smp_u64 over = 0;                          // sum above the bin in question
+      smp_u64 over = 0, here = 0;                // sums above the bin in question and in it
       bool reached = true;
 #pragma unroll 1
       while (true) {
@@ -610,7 +629,7 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
         if (tid == 0) found_at = KEYS;
         __syncthreads();
         each([&](float x, int i) {
-          const uint32_t k = smp_key<BF16>(x);
+          const uint32_t k = key(x, i);
           if (k >= lo && k <= hi && in(x, i)) {
             const smp_u64 w = by_mass ? sc.mass(x, powers) : 1;
             if (w) atomicAdd(&hist[(hi - k) >> shift], w);
@@ -622,46 +641,30 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
           const bool second = ahead + one < target;
           found_at = 2 * tid + second;
           found = ahead + (second ? one : 0);
+          found_here = second ? two : one;
         }
         __syncthreads();
         const int bin = found_at;
         if (bin == KEYS) { reached = false; break; }
         over = found;
+        here = found_here;
         hi -= uint32_t(bin) << shift;
         lo = shift ? max(lo, hi - ((1u << shift) - 1)) : hi;
         __syncthreads();
-        if (lo == hi) break;
+        if (shift == 0) break;
       }
-      if (!reached) {                            // short of it by the last units: all of these bins
-        cut = smp_value<BF16>(lowest);
-        bound = cut == k_cut ? k_bound : V;
-        __syncthreads();
+      __syncthreads();
+      if (by_index) {
+        bound = reached ? int(~hi) + 1 : bound;  // behind the last one that is kept
         continue;
       }
-      cut = smp_value<BF16>(hi);
-      const smp_u64 w = by_mass ? sc.mass(cut, powers) : 1, ties = (target - over + w - 1) / w;
-      // the index behind the `ties`-th element that is equal to the cut
-      smp_u64 mine = 0;
-      each([&](float x, int i) { mine += x == cut && in(x, i); });
-      const smp_u64 upto = group.upto(mine), first = upto - mine;
-      if (tid == 0) found_at = V;
-      __syncthreads();
-      if (first < ties && ties <= upto) {
-        smp_u64 t = first;
-        each([&](float x, int i) {
-          if (x == cut && in(x, i) && ++t == ties) found_at = i + 1;
-        });
+      cut = smp_value<BF16>(reached ? hi : lowest);       // not reached, for want of the last units: all of these bins
+      bound = cut == k_cut ? k_bound : V;
+      if (reached) {                             // of the elements equal to the cut so many
+        const smp_u64 w = by_mass ? sc.mass(cut, powers) : 1;
+        target = (target - over + w - 1) / w;
+        indexes = target * w < here;
       }
-      __syncthreads();
-      bound = cut == k_cut ? min(found_at, k_bound) : found_at;
-      if (!by_mass && ask.p < 1.f) {
-        smp_u64 m = 0;
-        each([&](float x, int i) {
-          if (in(x, i) && (x > cut || (x == cut && i < bound))) m += sc.mass(x, powers);
-        });
-        whole = r.k_mass + group.sum(m);
-      }
-      __syncthreads();
     }
     // what is kept of those bins joins the sums of its neighbourhoods
     const int sure = min(r.k_bin, r.p_lo);
@@ -727,7 +730,7 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
 }
 
 namespace {
-struct SampleSpace { int places, chunks; size_t row, block, list, total; };
+struct SampleSpace { int places, chunks, list_size; size_t row, block, list, total; };
 SampleSpace space(int S, int V) {
   SampleSpace p;
   p.places = static_cast<long long>(S) * V < (1 << 21) && V <= SMP_CHUNKS * SMP_THREADS * 4 ? 1 : 4;
@@ -735,7 +738,8 @@ SampleSpace space(int S, int V) {
   p.row = align256(size_t(S) * p.chunks * sizeof(SampleChunk));
   p.block = p.row + align256(size_t(S) * sizeof(SampleRow));
   p.list = p.block + align256(size_t(S) * p.chunks * p.places * 8 * 8);
-  p.total = p.list + align256(size_t(S) * SMP_LIST * 4);
+  p.list_size = V < SMP_LIST ? V : SMP_LIST;
+  p.total = p.list + align256(size_t(S) * p.list_size * 8);
   return p;
 }
 }  // namespace
@@ -746,8 +750,8 @@ int32_t launch_sample(const void* logits, bool bf16, long long stride, int S, in
                       void* ws, hipStream_t st) {
   const SampleSpace p = space(S, V);
   uint8_t* b = static_cast<uint8_t*>(ws);
-  SampleArgs a{logits, stride, how.temperature, how.top_k, how.top_p, how.min_p, u, tokens, logprobs, S, V, p.chunks, p.chunks * p.places * 8,
-               reinterpret_cast<SampleChunk*>(b), reinterpret_cast<SampleRow*>(b + p.row), reinterpret_cast<smp_u64*>(b + p.block), reinterpret_cast<uint32_t*>(b + p.list)};
+  SampleArgs a{logits, stride, how.temperature, how.top_k, how.top_p, how.min_p, u, tokens, logprobs, S, V, p.chunks, p.chunks * p.places * 8, p.list_size,
+               reinterpret_cast<SampleChunk*>(b), reinterpret_cast<SampleRow*>(b + p.row), reinterpret_cast<smp_u64*>(b + p.block), reinterpret_cast<uint2*>(b + p.list)};
   ProfileScope ps(MOQE_PK_OTHER, st);
   const bool filters = how.top_k || how.top_p || how.min_p;
   const dim3 chunks(p.chunks, S), threads(SMP_THREADS);

@@ -1,8 +1,8 @@
 """moqe_sample on the GPU against the 64-bit oracle.
 
-Tokens have to be equal.  Sums on the GPU are of weights in 64 bits cut to 2^-42 of the largest, V of them, and the oracle's of V rounded ones: a choice that lies nearer to another one than
-V 2^-41 of the whole weight (the oracle's gap) could come out either way and is passed over.  logprobs: fp32, half a step, and 2^-20 absolute for the weights' sums (V 2^-42 for the largest V,
-times four)."""
+Tokens have to be equal.  Sums on the GPU are of weights cut to 2^-42 of the largest, V of them, once for the share that top-p asks for and once for the draw: a choice that lies nearer to another
+one than V 2^-40 of the largest weight (the oracle's gap) could come out either way and is passed over.  logprobs: fp32, half a step, and 2^-20 absolute for the weights' sums (V 2^-42 for the
+largest V, times four)."""
 import math
 
 import numpy as np
@@ -36,7 +36,7 @@ def check(logits, u, **how):
     for s in range(len(x)):
         row = {k: (int(v[s]) if k == "top_k" else float(v[s])) for k, v in args.items()}
         want, want_lp, gap = fo.sample(x[s], u32[s], **row)
-        if gap <= x.shape[1] * 2.0 ** -41:
+        if gap <= x.shape[1] * 2.0 ** -40:
             near += 1
             continue
         assert tokens[s] == want, (s, row, u32[s], tokens[s], want, gap)
@@ -92,6 +92,16 @@ def test_equal_logits_go_by_index():
     check(two, u, top_p=(np.arange(1, S + 1) / S * 0.999 + 1e-4).tolist(), min_p=[0.2, 0.5] * 8)
     steps = torch.round(logits_of(S, V, F32, 1.0, 9) * 2) / 2
     check(steps, u, top_k=[50, 300, 1000, 2500] * 4, top_p=[0.2, 0.6, 0.9, 1.0] * 4)
+
+
+@pytest.mark.parametrize("t", [F32, BF])
+@pytest.mark.parametrize("V,sharp", [(20000, 0.02), (60000, 0.3), (110000, 1.0), (300000, 0.4), (1 << 20, 0.5)])
+def test_cuts_among_many(V, sharp, t):
+    """Cuts fall where thousands to hundreds of thousands of logits lie within a quarter of an octave."""
+    S = 4
+    x, u = logits_of(S, V, t, sharp, 11), uniform(S, V)
+    check(x, u, top_k=[V // 2, V // 7, V - 100, 0], top_p=[1.0, 0.3, 0.9, 0.5])
+    check(x, u, top_p=[0.1, 0.5, 0.9, 0.99], temperature=[0.7, 1.0, 1.5, 1.0], min_p=[0.0, 0.5, 0.0, 0.3])
 
 
 def test_special_values():
