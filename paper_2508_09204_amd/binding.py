@@ -736,7 +736,7 @@ class KvCache:
     @classmethod
     def empty(cls, n_blocks: int, n_heads: int, block_tokens: int, head_dim: int, device) -> "KvCache":
         codes = [torch.empty((n_blocks, n_heads, block_tokens * head_dim), dtype=torch.uint8, device=device) for _ in range(2)]
-        scales = [torch.empty((n_blocks, n_heads), dtype=torch.float32, device=device) for _ in range(2)]
+        scales = [torch.zeros((n_blocks, n_heads), dtype=torch.float32, device=device) for _ in range(2)]      # of blocks that were never written too: numbers
         return cls(*codes, *scales, block_tokens, head_dim)
 
     def tensors(self):

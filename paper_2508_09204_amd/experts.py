@@ -40,3 +40,15 @@ def quantize_and_pack(w: torch.Tensor, bits: int, group: int, symmetric: bool, c
     mq.moqe_quantize_rtn(w, clip, can)
     packed = pack(can)
     return (packed, can) if keep_canonical else packed
+
+
+def quantize_rows_f8(x: torch.Tensor) -> mq.F8Rows:
+    """x: device fp32 or bf16 [M, d].  8-bit floating-point rows, a power-of-two scale for each 128 features."""
+    rows = mq.F8Rows.empty(*x.shape, x.device)
+    mq.moqe_residual_norm_f8(None, x, rows)
+    return rows
+
+
+def quantize_f8(w: torch.Tensor, up: Optional[torch.Tensor] = None) -> mq.F8Mat:
+    """w: device fp32 or bf16 [n, k]; with `up`, the gated pair of both."""
+    return mq.F8Mat.pack(quantize_rows_f8(w), quantize_rows_f8(up) if up is not None else None)

@@ -1,0 +1,54 @@
+"""The decoder in 8-bit floating point and its draws without a GPU: all calls with their arguments checked (dry-run mode), and what it refuses."""
+import pytest
+import torch
+
+from paper_2508_09204_amd import decoder as dec
+
+
+@pytest.fixture(scope="module")
+def mq():
+    from paper_2508_09204_amd import binding
+    binding.moqe_set_dry_run(True)
+    yield binding
+    binding.moqe_set_dry_run(False)
+
+
+def _aligned(nbytes):
+    t = torch.zeros(nbytes + 256, dtype=torch.uint8)
+    at = -t.data_ptr() % 256
+    return t[at:at + nbytes]
+
+
+def _model(mq, layers=2, d=256, f=384, heads=4, kv=2, dh=64, K=3, V=500, out_int=False, mlp_int=False):
+    f8 = lambda n, k, gated=False: mq.F8Mat(_aligned(mq.moqe_f8_packed_bytes(n, k, gated)), n, k, gated)
+    ints = lambda n, k: [mq.QMat(_aligned(mq.moqe_packed_bytes(n, k, 4, 128, False)), None, None, n, k, 4, 128, False, 0, mq.LAYOUT_PACKED) for _ in range(K)]
+    router = mq.Router(None, None, torch.zeros(K, d), None, d, 0, K)
+    norm = lambda: mq.Norm("rms", 1e-6, torch.ones(d))
+    mlp = lambda: (mq.Block(kind=mq.KIND_SILU_MLP, router=router, w0=ints(f, d), w1=ints(f, d), w2=ints(d, f)) if mlp_int else
+                   dec.F8Mlp([f8(f, d, True) for _ in range(K)], [f8(d, f) for _ in range(K)]))
+    made = [dec.Layer(norm(), [f8((heads + 2 * kv) * dh, d)], ints(d, heads * dh) if out_int else [f8(d, heads * dh) for _ in range(K)], norm(), mlp()) for _ in range(layers)]
+    return dec.Decoder(made, norm(), router, mq.Rope(dec.rope_frequencies(dh, device="cpu"), dh), heads, kv, dh, head=f8(V, d) if V else None,
+                       embedding=torch.zeros(V, d) if V else None)
+
+
+@pytest.mark.parametrize("out_int,mlp_int", [(False, False), (True, False), (False, True)])
+def test_a_step_and_a_draw_pass_every_check(mq, out_int, mlp_int):
+    model = _model(mq, out_int=out_int, mlp_int=mlp_int)
+    seqs = dec.Sequences(model, 3, 100, 32, device="cpu")
+    for T in (97, 1):
+        step = dec.Step(model, seqs, T, _aligned(1 << 24))
+        assert step().shape == (3 * T, 256)
+        assert step.out8.M == 3 * T and step.out8.d == 256
+    assert int(seqs.kv_len[1]) == 98
+    with pytest.raises(ValueError):
+        dec.Step(model, seqs, 1, _aligned(256))
+
+
+def test_what_has_no_head_gives_no_tokens(mq):
+    model = _model(mq, layers=1, V=0)
+    step = dec.Step(model, dec.Sequences(model, 2, 50, 32, device="cpu"), 1, _aligned(1 << 24))
+    assert step.out8 is None
+    with pytest.raises(ValueError):
+        dec.Draw(model, step)
+    with pytest.raises(ValueError):
+        dec.Generator(model, 2, 10, 10)
