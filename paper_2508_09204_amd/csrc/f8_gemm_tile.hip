@@ -22,18 +22,28 @@ struct F8TileGeom {
 
 // MB blocks of 16 rows, which all four waves share, by 4 NT tiles of 16 features, NT of each wave's own.  KS such groups of four waves share out the blocks of 128 columns.
 // WD: blocks that a wave's weights are ahead.
+//
+// Activations go from memory to LDS directly, 16 bytes a lane swizzled by the row, so that operand reads are free of bank conflicts; weights never touch LDS, they lie in memory as the operands
+// they are.  One barrier a block.  The scale of a row and block is the instruction's own operand, a byte of a dword that holds four blocks': nothing is multiplied.
+// Bound by the matrix cores, and by power: 8192 rows, k 11008, n 4096 in 270 to 285 us, 2740 TFLOP/s at about 2 GHz (a library product in fp8 with one scale 2690 on 8192^3; nothing but products
+// from registers 3900); the products take 60 % of the time that a SIMD has.  What it took:
+//  * two work-groups to a CU (128 x 256, 251 registers) instead of one (256 x 256): 333 -> 299 us;
+//  * memory requests spread over the row blocks' products: as one burst at the head of a block, products wait behind them in the wave's order of issue: 305 -> 286, 2048 rows of 4096 x 4096 41 -> 36;
+//  * operands of the next row block read ahead of this one's products: 273 -> 270, 33.4 -> 31.4.
+// No gain: activations three blocks ahead (7 % slower), priorities for products, groups of 16 row tiles, 32x32x64 products in a probe (no faster).
+// EXACT (fp32 results): codes times scales as bf16 operands, 16x16x32 products: 4096^3 in 108 us, 1270 TFLOP/s, as a library bf16 product; a wave converts its activations itself.
 template <int MB, int NT, int KS, int WD, int OUT, bool EXACT>
-__global__ __launch_bounds__(256 * KS, KS == 1 ? 2 : 1) void k_f8_tile(F8Args a, F8TileGeom tg) {
+__global__ __launch_bounds__(256 * KS, KS > 1 ? 1 : MB * NT <= 8 && !EXACT ? 3 : 2) void k_f8_tile(F8Args a, F8TileGeom tg) {
   constexpr int ROWS = MB * 16, AL = (MB + 1) / 2, STAGED = ROWS < 32 ? 32 : ROWS;      // AL: requests of a wave for a block's activations
   constexpr int F = OUT == F8_PLAIN ? NT * 64 : NT * 32;                 // features of a work-group
-  constexpr int BUF = STAGED * 128, SC = ROWS < 64 ? 64 : ROWS;
+  constexpr int BUF = STAGED * 128;
   __shared__ __attribute__((aligned(128))) uint8_t buf0_[KS * BUF], buf1_[KS * BUF], buf2_[KS * BUF], buf3_[KS * BUF];
-  __shared__ uint32_t sc0_[KS * SC], sc1_[KS * SC];
+  __shared__ uint32_t scales_[KS][2][ROWS];                              // of a group of four blocks and the next
   __shared__ int32_t dst[ROWS];
   const int part = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);      // of the columns
   const int tid = threadIdx.x & 255, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, q = lane >> 4;
   uint8_t *buf0 = buf0_ + part * BUF, *buf1 = buf1_ + part * BUF, *buf2 = buf2_ + part * BUF, *buf3 = buf3_ + part * BUF;
-  uint32_t *sc0 = sc0_ + part * SC, *sc1 = sc1_ + part * SC;
+  uint32_t (*scales)[ROWS] = scales_[part];
 
   // which tile: the row tiles there are, dealt to the XCDs in runs, in groups of tg.group row tiles
   int rt = 0;
@@ -79,28 +89,32 @@ __global__ __launch_bounds__(256 * KS, KS == 1 ? 2 : 1) void k_f8_tile(F8Args a,
     ws_at[t] = a.scale_off + nt * uint32_t(a.groups) * 64;
   }
 
+  auto stage_one = [&](uint8_t* buf, int kb, int i) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, (f8_lds*)(buf + (i * 4 + wave) * 1024), 16, int(a_at[i]), min(kb, blocks - 1) * 128, 0, 0);
+  };
   auto stage = [&](uint8_t* buf, int kb) {
-    const int k = min(kb, blocks - 1) * 128;
 #pragma unroll
-    for (int i = 0; i < AL; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, (f8_lds*)(buf + (i * 4 + wave) * 1024), 16, int(a_at[i]), k, 0, 0);
+    for (int i = 0; i < AL; ++i) stage_one(buf, kb, i);
   };
-  auto stage_scales = [&](uint32_t* sc, int g) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(s_rsrc, (f8_lds*)(sc + (wave * 64 & (ROWS - 1))), 4, int(sc_at), min(g, a.groups - 1) * 4, 0, 0);
-  };
+  uint32_t x_next = 0, ws[NT], ws_next[NT];                              // scales of the next group: of a row, of the features
   F8Frag w[WD + 1][NT];
-  uint32_t ws[2][NT];
-  auto load_w = [&](F8Frag (&f)[NT], int kb) {
-    const uint32_t k = uint32_t(min(kb, blocks - 1)) * 2048;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      f[t].u[0] = __builtin_bit_cast(f8_i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc, lane * 16, int(w_at[t] + k), 0));
-      f[t].u[1] = __builtin_bit_cast(f8_i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc, lane * 16 + 1024, int(w_at[t] + k), 0));
-    }
+  auto load_half = [&](F8Frag (&f)[NT], int kb, int i) {                   // half i & 1 of tile i / 2
+    f[i / 2].u[i & 1] = __builtin_bit_cast(f8_i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc, lane * 16 + (i & 1) * 1024, int(w_at[i / 2] + uint32_t(min(kb, blocks - 1)) * 2048), 0));
   };
-  auto load_ws = [&](uint32_t (&s)[NT], int g) {
+  auto load_w = [&](F8Frag (&f)[NT], int kb) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s[t] = uint32_t(__builtin_amdgcn_raw_buffer_load_b32(w_rsrc, r * 4, int(ws_at[t] + uint32_t(min(g, a.groups - 1)) * 64), 0));
+    for (int i = 0; i < 2 * NT; ++i) load_half(f, kb, i);
+  };
+  auto load_scales = [&](int g) {
+    const int gg = min(g, a.groups - 1);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) ws_next[t] = uint32_t(__builtin_amdgcn_raw_buffer_load_b32(w_rsrc, r * 4, int(ws_at[t] + uint32_t(gg) * 64), 0));
+    x_next = uint32_t(__builtin_amdgcn_raw_buffer_load_b32(s_rsrc, int(sc_at), gg * 4, 0));
+  };
+  auto keep_scales = [&](int g) {
+    if (ROWS >= 256 || tid < ROWS) scales[g & 1][tid & (ROWS - 1)] = x_next;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) ws[t] = ws_next[t];
   };
 
   f8_f32x4 acc[MB][NT];
@@ -109,71 +123,85 @@ __global__ __launch_bounds__(256 * KS, KS == 1 ? 2 : 1) void k_f8_tile(F8Args a,
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[m][t] = f8_f32x4{0.f, 0.f, 0.f, 0.f};
 
+  constexpr int AHEAD = 2, LOADS = AL + 2 * NT;
   const int each_g = (a.groups + KS - 1) / KS, g0 = part * each_g, kb0 = g0 * 4, steps = min(each_g * 4, blocks);       // of the first part, the longest
-  stage_scales(sc0, g0);
-  load_ws(ws[0], g0);
+  load_scales(g0);
   stage(buf0, kb0);
   stage(buf1, kb0 + 1);
 #pragma unroll
   for (int i = 0; i < WD; ++i) load_w(w[i], kb0 + i);
+  keep_scales(g0);
 
-  // one block of 128 columns: products of step j of a group of four, the block after next on its way into LDS, the next one's weights into registers
-  auto step = [&](auto jc, int kb, const uint8_t* cur, uint8_t* next2, const uint32_t* sc, const uint32_t (&wsc)[NT]) {
+  // A block of 128 columns: products of step J of a group of four, the block AHEAD on its way into LDS, the weights WD ahead into registers.
+  auto step = [&](auto jc, int g) {
     constexpr int J = decltype(jc)::value, CUR = J & WD;
-    stage(next2, kb + 2);
-    load_w(w[(J + WD) & WD], kb + WD);
-    if (KS > 1 && kb >= blocks) return;
-    const uint8_t* p0 = cur + r * 128 + ((q ^ (r & 7)) * 16);
-    const uint8_t* p1 = cur + r * 128 + (((q + 4) ^ (r & 7)) * 16);
-    f8_bf16x8 we[EXACT ? NT : 1][4];
-    if constexpr (EXACT) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) we[t][i] = f8_quarter(w[CUR][t], i, f8_scale(wsc[t] >> 8 * J));
+    const int kb = g * 4 + J;
+    uint8_t* const bufs[4] = {buf0, buf1, buf2, buf3};
+    // the activations of AHEAD blocks ago have come, and the scales stored in the step before; younger requests may be under way
+    f8_wait<(AHEAD - 1) * AL + 2 * NT>();
+    f8_barrier();
+    if constexpr (J == 0) load_scales(g + 1);
+    if constexpr (KS > 1) {
+      load_w(w[(J + WD) & WD], kb + WD);
+      stage(bufs[(J + AHEAD) & 3], kb + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);                                 // asked for before the products
     }
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      F8Frag x;
-      x.u[0] = *reinterpret_cast<const f8_i32x4*>(p0 + m * 2048);
-      x.u[1] = *reinterpret_cast<const f8_i32x4*>(p1 + m * 2048);
-      const uint32_t xs = sc[m * 16 + r];
+    if (kb < blocks) {                                                   // also what keeps a step in a block of its own: as one block of 128 products the registers do not hold them
+      const uint32_t* sc = scales[g & 1];
+      const uint8_t* p0 = bufs[J] + r * 128 + ((q ^ (r & 7)) * 16);
+      const uint8_t* p1 = bufs[J] + r * 128 + (((q + 4) ^ (r & 7)) * 16);
+      f8_bf16x8 we[EXACT ? NT : 1][4];
       if constexpr (EXACT) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f8_bf16x8 xe = f8_quarter(x, i, f8_scale(xs >> 8 * J));
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int t = 0; t < NT; ++t) acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(we[t][i], xe, acc[m][t], 0, 0, 0);
+          for (int i = 0; i < 4; ++i) we[t][i] = f8_quarter(w[CUR][t], i, f8_scale(ws[t] >> 8 * J));
+      }
+      F8Frag x[2];
+      uint32_t xs[2];
+      auto read = [&](int m) {
+        x[m & 1].u[0] = *reinterpret_cast<const f8_i32x4*>(p0 + m * 2048);
+        x[m & 1].u[1] = *reinterpret_cast<const f8_i32x4*>(p1 + m * 2048);
+        xs[m & 1] = sc[m * 16 + r];
+      };
+      read(0);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) {
+        if (m + 1 < MB) read(m + 1);                                     // ahead of this one's products
+        if constexpr (KS == 1) {                                         // a few requests ahead of each row block's products: all at once they keep the products waiting behind them
+#pragma unroll
+          for (int l = m * LOADS / MB; l < (m + 1) * LOADS / MB; ++l) {
+            if (l < AL) stage_one(bufs[(J + AHEAD) & 3], kb + AHEAD, l);
+            else load_half(w[(J + WD) & WD], kb + WD, l - AL);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-      } else {
+        if constexpr (EXACT) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) acc[m][t] = f8_mfma<J>(w[CUR][t], x, acc[m][t], wsc[t], xs);
+          for (int i = 0; i < 4; ++i) {
+            const f8_bf16x8 xe = f8_quarter(x[m & 1], i, f8_scale(xs[m & 1] >> 8 * J));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(we[t][i], xe, acc[m][t], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) acc[m][t] = f8_mfma<J>(w[CUR][t], x[m & 1], acc[m][t], ws[t], xs[m & 1]);
+        }
       }
     }
+    if constexpr (J == 3) keep_scales(g + 1);
   };
-  auto sync = [&] {
-    f8_wait<AL + (WD > 1 ? 4 : 2) * NT>();                               // the activations of two blocks ago have come; weights may be under way
-    f8_barrier();
-  };
-  auto group = [&](int s, uint32_t* sc, uint32_t* sc_next, uint32_t (&wsc)[NT], uint32_t (&ws_next)[NT]) {
-    const int kb = kb0 + s;
-    sync();
-    stage_scales(sc_next, (kb >> 2) + 1);
-    load_ws(ws_next, (kb >> 2) + 1);
-    step(std::integral_constant<int, 0>(), kb, buf0, buf2, sc, wsc);
-    if (s + 1 >= steps) return;
-    sync();
-    step(std::integral_constant<int, 1>(), kb + 1, buf1, buf3, sc, wsc);
-    if (s + 2 >= steps) return;
-    sync();
-    step(std::integral_constant<int, 2>(), kb + 2, buf2, buf0, sc, wsc);
-    if (s + 3 >= steps) return;
-    sync();
-    step(std::integral_constant<int, 3>(), kb + 3, buf3, buf1, sc, wsc);
-  };
-  for (int s = 0; s < steps; s += 8) {
-    group(s, sc0, sc1, ws[0], ws[1]);
-    if (s + 4 < steps) group(s + 4, sc1, sc0, ws[1], ws[0]);
+  int g = g0;
+  for (const int end = g0 + steps / 4; g < end; ++g) {
+    step(std::integral_constant<int, 0>(), g);
+    step(std::integral_constant<int, 1>(), g);
+    step(std::integral_constant<int, 2>(), g);
+    step(std::integral_constant<int, 3>(), g);
+  }
+  if (steps & 3) {
+    step(std::integral_constant<int, 0>(), g);
+    if ((steps & 3) > 1) step(std::integral_constant<int, 1>(), g);
+    if ((steps & 3) > 2) step(std::integral_constant<int, 2>(), g);
   }
   f8_wait<0>();
   f8_barrier();                                                          // nothing is on its way into LDS any more
