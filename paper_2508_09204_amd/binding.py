@@ -867,6 +867,7 @@ def moqe_kv_attention(q: torch.Tensor, attn: Attention, batch: KvBatch, cache: K
 # 8-bit floating point, tokens
 # --------------------------------------------------------------------------------------
 TYPE_F8 = 2
+FAST_SUMS = 8
 F8_BLOCK = 128
 
 
@@ -1003,10 +1004,11 @@ def moqe_f8_gemm_workspace_bytes(experts: Sequence[F8Mat], S: int, T: int, y_typ
 
 class F8GemmCall(_DeviceCall):
     """moqe_f8_gemm with its arguments marshalled once and a workspace of its own.  a: S * T rows in 8 bits; y: fp32 or bf16 [S * T, n], or F8Rows (gated pairs).
-    Without offsets there is one matrix, for all rows (S: as many as a has, T 1, if not given)."""
+    Without offsets there is one matrix, for all rows (S: as many as a has, T 1, if not given).  fast: sums of the matrix cores' 8-bit products whatever the result's type (MOQE_FAST_SUMS)."""
 
     def __init__(self, a: F8Rows, experts: Sequence[F8Mat], y, offsets: Optional[torch.Tensor] = None, perm: Optional[torch.Tensor] = None,
-                 S: Optional[int] = None, T: int = 1, scatter: bool = False, in_bucket_order: bool = False, workspace: Optional[torch.Tensor] = None):
+                 S: Optional[int] = None, T: int = 1, scatter: bool = False, in_bucket_order: bool = False, workspace: Optional[torch.Tensor] = None,
+                 fast: bool = False):
         S = a.M // T if S is None else S
         if S * T != a.M or a.d != experts[0].k:
             raise ValueError(f"a is {a.M} rows of {a.d} features, the call is of {S} * {T} of {experts[0].k}")
@@ -1031,7 +1033,8 @@ class F8GemmCall(_DeviceCall):
         self._keep = (a, experts, y, offsets, perm)
         self._hold(*a.tensors(), *out, offsets, perm, workspace, *(m.packed for m in experts))
         self._args = (C.byref(self._a), _vector(offsets, K + 1, "offsets", torch.int32), _vector(perm, S, "perm", torch.int32), _int32(S, "S"), _int32(T, "T"), self._mats, K,
-                      C.byref(r), (SCATTER_OUTPUT if scatter else 0) | (INPUT_IN_BUCKET_ORDER if in_bucket_order else 0), _ptr(workspace), workspace.numel())
+                      C.byref(r), (SCATTER_OUTPUT if scatter else 0) | (INPUT_IN_BUCKET_ORDER if in_bucket_order else 0) | (FAST_SUMS if fast else 0), _ptr(workspace),
+                      workspace.numel())
 
     def __call__(self, stream: Optional[int] = None) -> None:
         self._on_device()
@@ -1041,8 +1044,8 @@ class F8GemmCall(_DeviceCall):
 
 
 def moqe_f8_gemm(a: F8Rows, experts: Sequence[F8Mat], y, offsets: Optional[torch.Tensor] = None, perm: Optional[torch.Tensor] = None,
-                 S: Optional[int] = None, T: int = 1, scatter: bool = False, in_bucket_order: bool = False, workspace: Optional[torch.Tensor] = None) -> None:
-    F8GemmCall(a, experts, y, offsets, perm, S, T, scatter, in_bucket_order, workspace)()
+                 S: Optional[int] = None, T: int = 1, scatter: bool = False, in_bucket_order: bool = False, workspace: Optional[torch.Tensor] = None, fast: bool = False) -> None:
+    F8GemmCall(a, experts, y, offsets, perm, S, T, scatter, in_bucket_order, workspace, fast)()
 
 
 def moqe_sample_workspace_bytes(S: int, V: int) -> int:

@@ -95,7 +95,7 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
   if (!y) return set_error(MOQE_E_NULL, "%s: y is NULL", who);
   int32_t rc = check_f8_call(experts, K, S, T, y->type, who);
   if (rc) return rc;
-  if (flags & ~(MOQE_SCATTER_OUTPUT | MOQE_INPUT_IN_BUCKET_ORDER)) return set_error(MOQE_E_FORMAT, "%s: flags %d", who, flags);
+  if (flags & ~(MOQE_SCATTER_OUTPUT | MOQE_INPUT_IN_BUCKET_ORDER | MOQE_FAST_SUMS)) return set_error(MOQE_E_FORMAT, "%s: flags %d", who, flags);
   if (!offsets && K != 1) return set_error(MOQE_E_NULL, "%s: offsets is NULL with %d experts", who, K);
   if ((flags & MOQE_SCATTER_OUTPUT) && !perm) return set_error(MOQE_E_NULL, "%s: perm is NULL, results cannot be scattered", who);
   if (!aligned(offsets, 4) || !aligned(perm, 4)) return set_error(MOQE_E_SHAPE, "%s: misaligned offsets or perm", who);
@@ -130,6 +130,7 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
   g.offsets = offsets;
   g.a_perm = (flags & MOQE_INPUT_IN_BUCKET_ORDER) ? nullptr : perm;
   g.y_perm = (flags & MOQE_SCATTER_OUTPUT) ? perm : nullptr;
+  g.exact = y->type != MOQE_TYPE_BF16 && !(flags & MOQE_FAST_SUMS);
   g.S = S; g.T = T; g.K = K; g.n = n; g.tiles = p.tiles; g.blocks = p.blocks; g.groups = p.groups; g.scale_off = uint32_t(p.scale_off);
   if (y->type == MOQE_TYPE_F8) {
     g.y8 = y->rows8.codes; g.y8_scales = y->rows8.scales; g.y8_stride = y->rows8.code_stride; g.y8_scale_stride = y->rows8.scale_stride;

@@ -31,7 +31,7 @@ struct F8TileGeom {
 //  * memory requests spread over the row blocks' products: as one burst at the head of a block, products wait behind them in the wave's order of issue: 305 -> 286, 2048 rows of 4096 x 4096 41 -> 36;
 //  * operands of the next row block read ahead of this one's products: 273 -> 270, 33.4 -> 31.4.
 // No gain: activations three blocks ahead (7 % slower), priorities for products, groups of 16 row tiles, 32x32x64 products in a probe (no faster).
-// EXACT (fp32 results): codes times scales as bf16 operands, 16x16x32 products: 4096^3 in 108 us, 1270 TFLOP/s, as a library bf16 product; a wave converts its activations itself.
+// EXACT: codes times scales as bf16 operands, 16x16x32 products: 4096^3 in 108 us, 1270 TFLOP/s, as a library bf16 product; a wave converts its activations itself.
 template <int MB, int NT, int KS, int WD, int OUT, bool EXACT>
 __global__ __launch_bounds__(256 * KS, KS > 1 ? 1 : MB * NT <= 8 && !EXACT ? 3 : 2) void k_f8_tile(F8Args a, F8TileGeom tg) {
   constexpr int ROWS = MB * 16, AL = (MB + 1) / 2, STAGED = ROWS < 32 ? 32 : ROWS;      // AL: requests of a wave for a block's activations
@@ -298,11 +298,11 @@ static int32_t launch_tile(const F8Args& a, bool gated, hipStream_t st) {
   if (!gated) hipLaunchKernelGGL((k_f8_tile<MB, NT, KS, WD, F8_PLAIN, EXACT>), grid, block, 0, st, a, tg);
   else if (!a.y8) {
     if constexpr (NT > 1) hipLaunchKernelGGL((k_f8_tile<MB, NT, KS, WD, F8_GATED, EXACT>), grid, block, 0, st, a, tg);
-  } else if constexpr (!EXACT && NT == 4) hipLaunchKernelGGL((k_f8_tile<MB, NT, KS, WD, F8_GATED8, false>), grid, block, 0, st, a, tg);
+  } else if constexpr (NT == 4) hipLaunchKernelGGL((k_f8_tile<MB, NT, KS, WD, F8_GATED8, EXACT>), grid, block, 0, st, a, tg);
   return check_launch("f8_gemm");
 }
 
-// The tiles of f8_shape().  fp32 results: no 128 rows, whose operands in bf16 the registers do not hold.
+// The tiles of f8_shape().  Exact products: no 128 rows, whose operands in bf16 the registers do not hold.
 int32_t launch_f8_tile(const F8Args& a, bool gated, bool exact, int rows, int cols, int parts, hipStream_t st) {
   if (exact) {
     if (cols == 16) return launch_tile<4, 4, 1, 1, true>(a, gated, st);

@@ -46,9 +46,10 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, stretch: float = 1.0,
 
 @dataclass
 class F8Mlp:
-    """A SILU_MLP block in 8-bit floating point: a gated pair [f, d] and a matrix [d, f] per expert, or one of each for all."""
+    """A SILU_MLP block in 8-bit floating point: a gated pair [f, d] and a matrix [d, f] per expert, or one of each for all.  fast: sums of the first product as binding.F8GemmCall has them."""
     gate_up: List[mq.F8Mat]
     down: List[mq.F8Mat]
+    fast: bool = True
 
 
 @dataclass
@@ -156,7 +157,7 @@ class Step:
             self._calls += self._norm(y, layer.mlp_norm, layer.mlp)
             if _f8(layer.mlp):
                 y = self.y16
-                self._calls += self._product(None, self.normed8, layer.mlp.gate_up, self.h8) + self._product(None, self.h8, layer.mlp.down, y)
+                self._calls += self._product(None, self.normed8, layer.mlp.gate_up, self.h8, layer.mlp.fast) + self._product(None, self.h8, layer.mlp.down, y)
             else:
                 y = self.y
                 self._calls.append(self._mlp(layer.mlp, ws))
@@ -176,14 +177,14 @@ class Step:
         kind, out = (mq.ResidualNormF8Call, self.normed8) if _f8(mats) else (mq.ResidualNormCall, self.normed)
         return [kind(y, self.x, out, residual_out=self.x if y is not None else None, scale=self.model.residual_scale if y is not None else 1.0, pre=norm)]
 
-    def _product(self, a, a8, mats, y):
+    def _product(self, a, a8, mats, y, fast=False):
         s, ws = self.seqs, self.workspace
         if not _f8(mats):
             flags = mq.SCATTER_OUTPUT | (mq.OUTPUT_BF16 if y.dtype == torch.bfloat16 else 0)
             return [lambda: mq.moqe_grouped_qgemm(a, s.offsets, s.perm, s.S, self.T, mats, y, flags, ws)]
         if len(mats) == 1:
-            return [mq.F8GemmCall(a8, mats, y, S=s.S, T=self.T, workspace=ws)]
-        return [mq.F8GemmCall(a8, mats, y, s.offsets, s.perm, s.S, self.T, scatter=True, workspace=ws)]
+            return [mq.F8GemmCall(a8, mats, y, S=s.S, T=self.T, workspace=ws, fast=fast)]
+        return [mq.F8GemmCall(a8, mats, y, s.offsets, s.perm, s.S, self.T, scatter=True, workspace=ws, fast=fast)]
 
     def _mlp(self, block, ws):
         return lambda: mq.moqe_forward_routed(block, self.seqs.expert_idx, self.normed, self.seqs.S, self.T, self.y, None, ws)

@@ -91,7 +91,7 @@ def _gemm(mq, a=None, offsets=FAKE, perm=FAKE, S=6, T=5, mats=None, K=2, y=None,
 
 @pytest.mark.parametrize("change,code", [
     ({}, 0), ({"S": 0}, 0), ({"flags": 3}, 0), ({"flags": 0, "perm": None}, 0), ({"offsets": None, "perm": None, "K": 1, "flags": 0}, 0), ({"K": 16}, 0),
-    ({"S": -1}, -2), ({"T": 0}, -2), ({"S": 1 << 20, "T": 1 << 11}, -2), ({"K": 17}, -2), ({"K": 0, "mats": [(FAKE, 40, 300, 0)]}, -2), ({"flags": 4}, -3), ({"flags": 9}, -3),
+    ({"S": -1}, -2), ({"T": 0}, -2), ({"S": 1 << 20, "T": 1 << 11}, -2), ({"K": 17}, -2), ({"K": 0, "mats": [(FAKE, 40, 300, 0)]}, -2), ({"flags": 9}, 0), ({"flags": 4}, -3), ({"flags": 17}, -3),
     ({"offsets": None}, -1), ({"perm": None}, -1), ({"offsets": FAKE + 2}, -2), ({"perm": FAKE + 1}, -2),
     ({"mats": [(FAKE, 40, 300, 0), (None, 40, 300, 0)]}, -1), ({"mats": [(FAKE, 40, 300, 0), (FAKE + 16, 40, 300, 0)]}, -2), ({"mats": [(FAKE, 40, 300, 0), (FAKE, 41, 300, 0)]}, -2),
     ({"mats": [(FAKE, 40, 300, 0), (FAKE, 40, 300, 1)]}, -2), ({"mats": [(FAKE, 40, 300, 0), (FAKE, 40, 301, 0)]}, -2), ({"n": 0}, -2), ({"k": 0}, -2),

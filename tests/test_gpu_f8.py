@@ -4,7 +4,7 @@ Tolerances, from the roundings of each path (half a step: bf16 2^-8 of a value, 
   codes     bit-equal where the value is exact in fp32; behind norms (fp32 sums of d terms: 2^-18 of the row's largest value, as for bf16 results) half a step of the
             value plus that; a scale may be the neighbour's only where the block's largest value lies within 2^-18 of 448 * 2^e
   products  codes and scales are exact, sums in fp32 in any order: k steps of 2^-24 of sum |a w| are the bound for sums one by one, of which 128 are added inside an
-            instruction; 2^-24 (blocks + 128) of sum |a w| covers both.  bf16 and 8-bit results come from products of codes, which the matrix cores add 8 neighbouring columns at a time, each cut
+            instruction; 2^-24 (blocks + 128) of sum |a w| covers both.  bf16 results, and others with fast sums, come from products of codes, which the matrix cores add 8 neighbouring columns at a time, each cut
             towards zero to a multiple of 2^(E - 13), 2^E the power of two of the largest of the 8 products: the other seven lose less than 2^-13 of the largest each, and that is at most the
             largest |a| of the 8 columns times the largest |w|.  bf16 results half a step more; silu 2^-20 of the result, and its inputs' error (|silu'| <= 1.1)
 """
@@ -188,11 +188,11 @@ def cut_products(a, w):
     return 7 * 2.0 ** -13 * pad(a) @ pad(w).T
 
 
-def check_product(y, a, w, up, t):
+def check_product(y, a, w, up, t, fast=False):
     """y from the GPU (F8Rows or tensor), operands' values."""
     rel = 2.0 ** -24 * (-(-a.shape[1] // 128) + 128)
     want = fo.product(a, w, up)
-    off = lambda m: rel * (np.abs(a) @ np.abs(m).T) + (0 if t == F32 else cut_products(a, m))
+    off = lambda m: rel * (np.abs(a) @ np.abs(m).T) + (cut_products(a, m) if t == BF or fast else 0)
     if up is None:
         tol = off(w)
     else:
@@ -224,6 +224,34 @@ def test_dense_products(M, n, k, gated, t):
     mq.moqe_f8_gemm(a, [mq.F8Mat.pack(*(r for r, _ in w))], y)
     sync()
     check_product(y, av, w[0][1], w[1][1] if gated else None, t)
+
+
+@pytest.mark.parametrize("M,n,k", SIZES)
+@pytest.mark.parametrize("gated,t", [(False, F32), (True, F32), (True, "f8")])
+def test_fast_sums(M, n, k, gated, t):
+    rng = np.random.default_rng(M + n + k + 1)
+    a, av = rows_of(rng.normal(size=(M, k)))
+    w = [rows_of(rng.normal(size=(n, k)) * k ** -0.5) for _ in range(2 if gated else 1)]
+    y = result(M, n, t)
+    mq.moqe_f8_gemm(a, [mq.F8Mat.pack(*(r for r, _ in w))], y, fast=True)
+    sync()
+    check_product(y, av, w[0][1], w[1][1] if gated else None, t, fast=True)
+
+
+@pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("M,n,k", [(200, 11008, 512), (1100, 2048, 1024)])
+def test_mean_error_of_sums(M, n, k, fast):
+    """fp32 sums of exact products: 2^-24 sqrt(blocks + 128) of sum |a w| would be one rounding after the other; fast ones 2^-15 of the results (1.4e-5 measured for normal values)."""
+    rng = np.random.default_rng(M)
+    a, av = rows_of(rng.normal(size=(M, k)))
+    w, wv = rows_of(rng.normal(size=(n, k)))
+    y = result(M, n, F32)
+    mq.moqe_f8_gemm(a, [mq.F8Mat.pack(w)], y, fast=fast)
+    sync()
+    want = torch.from_numpy(av).to(DEV) @ torch.from_numpy(wv).to(DEV).T
+    rms = float((y.double() - want).pow(2).mean().sqrt() / want.pow(2).mean().sqrt())
+    size = float((torch.from_numpy(np.abs(av)).to(DEV) @ torch.from_numpy(np.abs(wv)).to(DEV).T).pow(2).mean().sqrt() / want.pow(2).mean().sqrt())
+    assert rms < (2.0 ** -15 if fast else 2.0 ** -24 * (k // 128 + 128) ** 0.5 * size)
 
 
 @pytest.mark.parametrize("S,T,K", [(1, 1, 2), (5, 1, 3), (40, 1, 4), (7, 9, 3), (12, 33, 2), (3, 130, 4), (300, 1, 16), (64, 5, 1)])

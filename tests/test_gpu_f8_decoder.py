@@ -60,7 +60,7 @@ def test_stages_of_a_layer(T):
     for s in range(S):
         at = slice(s * T, (s + 1) * T)
         gate, up = _values(layer.mlp.gate_up[e[s]])
-        check_product(mq.F8Rows(step.h8.codes[at], step.h8.scales[at], T, step.h8.d), h_in[at], gate, up, "f8")
+        check_product(mq.F8Rows(step.h8.codes[at], step.h8.scales[at], T, step.h8.d), h_in[at], gate, up, "f8", fast=layer.mlp.fast)
         check_product(step.y16[at], h[at], _values(layer.mlp.down[e[s]])[0], None, BF)
     want = do.norm(f64(step.x), "rms", 1e-6, f64(model.final_norm.gain))
     near = 2.0 ** -18 * np.abs(want).max(1, keepdims=True)
