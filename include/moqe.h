@@ -523,7 +523,7 @@ int32_t moqe_kv_attention(const void* q, int64_t q_stride, const moqe_attention*
 /* Rows in 8 bits: e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; largest 448, no infinities) in blocks of 128 features, each block with a power-of-two scale 2^e,
  * -120 <= e <= 120, stored as the byte 127 + e.  An element is 2^e * code.  A row of d features has B = ceil(d / 128) blocks; codes past d in its last block are zeros.
  *   codes  : device, 16-byte aligned, row i at byte i * code_stride (a multiple of 16, at least 128 B)
- *   scales : device, 4-byte aligned, row i at byte i * scale_stride (a multiple of 4, at least B); bytes past B are neither written nor used
+ *   scales : device, 4-byte aligned, row i at byte i * scale_stride (a multiple of 4, at least B); bytes past B, up to a multiple of 4, have to be there but are neither written nor used
  * Quantizing a block of fp32 values: e is the smallest with max |x| <= 448 * 2^e over its finite values (-120 if they are all zero), codes are x / 2^e to nearest
  * (ties to even); infinities become the largest code of their sign, NaN stays. */
 typedef struct moqe_f8_rows { uint8_t *codes, *scales; int64_t code_stride, scale_stride; } moqe_f8_rows;
@@ -569,7 +569,7 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
  *   min_p       : float; of those, the ones with w_i >= min_p (taken as 1 if larger); all if not above 0
  * Equal logits are ordered by index, the lowest first.  With W the weight of what is kept, tokens[s] is the first kept index, in ascending order, whose running weight
  * exceeds u[s] * W, and logprobs[s] = log(w_token / W).
- *   logits   : MOQE_TYPE_F32 or MOQE_TYPE_BF16, aligned to the type, row s at element s * stride (at least V);  V <= 2^20
+ *   logits   : MOQE_TYPE_F32 or MOQE_TYPE_BF16, aligned to the type, row s at element s * stride (at least V);  V <= 2^20, S <= 65535
  *   u        : device float [S] (taken into [0, 1]; NaN is 0);  tokens: device int32 [S];  logprobs: device float [S] or NULL
  * Minus infinity and NaN are never taken; a row without anything else gives token -1 and log probability minus infinity.  Infinite logits share all of the weight.
  * Weights are in 64 bits, summed as integers of 2^-42 of the largest (results do not depend on any order); smaller ones count as nothing.

@@ -662,10 +662,13 @@ class _DeviceCall:
         if len(devices) > 1:
             raise ValueError(f"tensors on different devices: {', '.join(sorted(map(str, devices)))}")
         self._host = any(d.type != "cuda" for d in devices)
+        self._device = next(iter(devices)).index if devices and not self._host else None
 
     def _on_device(self) -> None:
         if self._host and not _dry_run:
             raise ValueError("the library reads and writes device memory, these tensors are not on the GPU")
+        if self._device is not None and self._device != torch._C._cuda_getDevice():      # the stream is the current device's
+            raise ValueError(f"the tensors are on GPU {self._device}, the current one is {torch._C._cuda_getDevice()}")
 
 
 @dataclass
@@ -873,7 +876,8 @@ F8_BLOCK = 128
 
 @dataclass
 class F8Rows:
-    """M rows of d features in 8 bits: codes uint8 [M, >= 128 * blocks], scales uint8 [M, >= blocks] (127 + the power of two), each with dense rows.
+    """M rows of d features in 8 bits: codes uint8 [M, >= 128 * blocks], scales uint8 [M, >= blocks, up to a multiple of 4] (127 + the power
+    of two), each with dense rows.
     Codes past d in the last block are zeros, as moqe_residual_norm_f8 and moqe_f8_gemm leave them."""
     codes: torch.Tensor
     scales: torch.Tensor
@@ -901,7 +905,7 @@ class F8Rows:
 
     def c(self, what: str = "rows") -> _F8Rows:
         got = []
-        for name, t, least in (("codes", self.codes, self.blocks * F8_BLOCK), ("scales", self.scales, self.blocks)):
+        for name, t, least in (("codes", self.codes, self.blocks * F8_BLOCK), ("scales", self.scales, (self.blocks + 3) // 4 * 4)):
             if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != self.M or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1):
                 raise ValueError(f"{name} of {what} must be {self.M} dense rows of at least {least} bytes, got {tuple(t.shape)} of {t.dtype}")
             unit = 16 if name == "codes" else 4

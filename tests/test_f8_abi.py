@@ -238,6 +238,22 @@ def test_binding_refuses(mq, call):
         call(mq, _host_rows(mq, 12, 300))
 
 
+def test_tensors_of_another_gpu_are_refused(mq, monkeypatch):
+    call = mq.SampleCall(torch.zeros(3, 50), torch.zeros(3), torch.zeros(3, dtype=torch.int32), workspace=_aligned(1 << 20))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    call._device = 0
+    call()
+    call._device = 1
+    with pytest.raises(ValueError):
+        call()
+
+
+def test_scales_end_at_a_multiple_of_four(mq):
+    a = _host_rows(mq, 12, 300)
+    with pytest.raises(ValueError):
+        mq.F8GemmCall(mq.F8Rows(a.codes, a.scales[:, :3], 12, 300), [_mat(mq, 40, 300)], torch.zeros(12, 40))
+
+
 def test_host_memory_is_for_dry_runs_only(mq):
     call = mq.F8GemmCall(_host_rows(mq, 12, 300), [_mat(mq, 40, 300)], torch.zeros(12, 40))
     draw = mq.SampleCall(torch.zeros(3, 50), torch.zeros(3), torch.zeros(3, dtype=torch.int32), workspace=_aligned(1 << 20))
