@@ -21,6 +21,7 @@ constexpr int SMP_THREADS = 512, SMP_NEIGHBOURS = 256;
 constexpr int SMP_CHUNKS = 128;                // of a row at most
 constexpr int SMP_BLOCKS = (1 << 20) / SMP_NEIGHBOURS;      // neighbourhoods of a row at most
 constexpr int SMP_BINS = 192;                  // quarters of an octave below the largest; the last one: everything that weighs nothing (2^-47 and less)
+constexpr int SMP_COPIES = 4;                  // of the bins while they are counted, for neighbouring lanes: most logits of a wave fall into a few
 constexpr int SMP_LIST = 16384;                // of a row at most: where the cuts' bins have more, the row is read instead
 constexpr int SMP_HELD = 4096;                 // of them in LDS: longer lists are read again for every pass
 constexpr int SMP_ONE = 43;
@@ -213,15 +214,15 @@ template <bool BF16, int P>
 __global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
   __shared__ double powers[256];
   __shared__ float tops[8];
-  __shared__ uint32_t firsts[8], count[SMP_BINS];
-  __shared__ smp_u64 mass[SMP_BINS], totals[8];
+  __shared__ uint32_t firsts[8], count[SMP_BINS][SMP_COPIES];
+  __shared__ smp_u64 mass[SMP_BINS][SMP_COPIES], totals[8];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, s = blockIdx.y, chunk = blockIdx.x;
   SampleChunk& out = a.chunk[static_cast<size_t>(s) * a.chunks + chunk];
   float v[P][4];
   smp_load<BF16, P>(a, s, chunk, v);
   if (tid < 256) powers[tid] = SMP_POWERS.v[tid];
   const SmpAsk ask(a, s);
-  if (tid < SMP_BINS) { count[tid] = 0; mass[tid] = 0; }
+  for (int i = tid; i < SMP_BINS * SMP_COPIES; i += SMP_THREADS) { (&count[0][0])[i] = 0; (&mass[0][0])[i] = 0; }
   float top = -INFINITY;
 #pragma unroll
   for (int j = 0; j < P; ++j)
@@ -277,17 +278,24 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
     for (int e = 0; e < 4; ++e)
       if (v[j][e] > -INFINITY) {
         const int b = sc.bin(v[j][e]);
-        atomicAdd(&count[b], 1u);
+        atomicAdd(&count[b][lane % SMP_COPIES], 1u);
         if (ask.p < 1.f) {
           const smp_u64 m = sc.mass(v[j][e], powers);
           total += m;
-          if (m) atomicAdd(&mass[b], m);
+          if (m) atomicAdd(&mass[b][lane % SMP_COPIES], m);
         }
       }
   total = smp_wave_sum(total);
   if (lane == 0) totals[wave] = total;
   __syncthreads();
-  if (tid < SMP_BINS) { out.count[tid] = count[tid]; out.mass[tid] = mass[tid]; }
+  if (tid < SMP_BINS) {
+    uint32_t n = 0;
+    smp_u64 m = 0;
+#pragma unroll
+    for (int c = 0; c < SMP_COPIES; ++c) { n += count[tid][c]; m += mass[tid][c]; }
+    out.count[tid] = n;
+    out.mass[tid] = m;
+  }
   if (tid == 0) {
     total = 0;
 #pragma unroll
@@ -434,7 +442,11 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
     if (chunk == 0) a.row[s] = cut;
   }
   __syncthreads();
+  // bins as ranges of 4 t: bin b is [floor4 - b, floor4 - b + 1), the last one all below it
   const int k_bin = cut.k_bin, p_lo = cut.p_lo, p_hi = cut.p_hi, sure = min(k_bin, p_lo);
+  auto from = [&](int b) { return b >= SMP_BINS - 1 ? -INFINITY : sc.floor4 - b; };
+  auto behind = [&](int b) { return b >= SMP_BINS ? -INFINITY : b <= 0 ? INFINITY : sc.floor4 - b + 1; };      // the first one has no end: where t is far from 0 a 1 more may be lost
+  const double sure_from = sure >= SMP_BINS ? -INFINITY : behind(sure), p_from = from(p_hi), p_end = p_hi < 0 ? -INFINITY : behind(p_lo), k_from = from(k_bin), k_end = behind(k_bin);
   const double floor_t = ask.least > 0.f ? log2(double(ask.least)) : -INFINITY;
   smp_u64* block = a.block + static_cast<size_t>(s) * a.blocks + chunk * BLOCKS + wave;
   uint32_t mine[P];                              // bits of the elements to be listed
@@ -442,17 +454,18 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
   for (int j = 0; j < P; ++j) {
     double sum = 0;
     mine[j] = 0;
-    int b[4];
-    bool any = false;
+    bool in[4], any = false;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      b[e] = v[j][e] > -INFINITY ? sc.bin(v[j][e]) : SMP_BINS + 1;
-      any |= b[e] < sure;
-      if (b[e] >= sure && (b[e] == k_bin || (b[e] >= p_lo && b[e] <= p_hi))) mine[j] |= 1u << e;
+      const double t4 = double(v[j][e]) * sc.c * 4;
+      const bool there = v[j][e] > -INFINITY;
+      in[e] = there && t4 >= sure_from;
+      any |= in[e];
+      if (there && ((t4 >= k_from && t4 < k_end) || (t4 >= p_from && t4 < p_end))) mine[j] |= 1u << e;
     }
     if (__any(any)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += b[e] < sure && sc.below(v[j][e]) >= floor_t ? sc.mass_bits(v[j][e], powers) - 4503599627370496.0 : 0.0;
+      for (int e = 0; e < 4; ++e) sum += in[e] && sc.below(v[j][e]) >= floor_t ? sc.mass_bits(v[j][e], powers) - 4503599627370496.0 : 0.0;
       sum = smp_wave_upto(sum);
     }
     if (lane == 63) block[j * 8] = static_cast<smp_u64>(sum);
