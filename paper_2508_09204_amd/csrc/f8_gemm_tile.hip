@@ -25,7 +25,7 @@ struct F8TileGeom {
 //
 // Activations go from memory to LDS directly, 16 bytes a lane swizzled by the row, so that operand reads are free of bank conflicts; weights never touch LDS, they lie in memory as the operands
 // they are.  One barrier a block.  The scale of a row and block is the instruction's own operand, a byte of a dword that holds four blocks': nothing is multiplied.
-// Bound by the matrix cores, and by power: 8192 rows, k 11008, n 4096 in 270 to 285 us, 2740 TFLOP/s at about 2 GHz (a library product in fp8 with one scale 2690 on 8192^3; nothing but products
+// Bound by the matrix cores, and by power: 8192 rows, k 11008, n 4096 in 270 to 290 us, 2560 to 2740 TFLOP/s at about 2 GHz (a library product in fp8 with one scale 2690 on 8192^3; nothing but products
 // from registers 3900); the products take 60 % of the time that a SIMD has.  What it took:
 //  * two work-groups to a CU (128 x 256, 251 registers) instead of one (256 x 256): 333 -> 299 us;
 //  * memory requests spread over the row blocks' products: as one burst at the head of a block, products wait behind them in the wave's order of issue: 305 -> 286, 2048 rows of 4096 x 4096 41 -> 36;

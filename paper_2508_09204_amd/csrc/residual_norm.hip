@@ -141,7 +141,8 @@ __device__ __forceinline__ void normed(float (&t)[NV][8], int d, int th, int lan
 }
 
 // A row in the registers of a.row_threads threads, every input read once.  Rows of one wave need no barrier, and four share a work-group.
-// F8: the result as 8-bit rows, besides bf16 ones if those are wanted too.  A block of 128 features is a piece of 16 neighbouring lanes.
+// F8: the result as 8-bit rows, besides bf16 ones if those are wanted too.  A block of 128 features is a piece of 16 neighbouring lanes.  64 rows of 4096 4.5 us (a launch); 32768 of 3584 with
+// norms before and after 276, 4.7 TB/s: memory.  The arithmetic stays in fp32, as the sums are: all of it in 64 bits took 451 us there, for some codes of a million at the border of a rounding.
 template <int NV, bool ODD, bool YBF, bool RBF, bool F8>
 __global__ __launch_bounds__(1024) void k_residual_norm(NormArgs a) {
   __shared__ float part[4 * 16];
