@@ -234,25 +234,41 @@ class Draw:
         return self.tokens
 
 
+def check_tokens(tokens: torch.Tensor, S: int, T: int, V: int) -> None:
+    """Refuses what is not S sequences of T tokens below V (reads them: waits for the device)."""
+    if tuple(tokens.shape) != (S, T) or tokens.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"tokens must be int32 or int64 {(S, T)}, got {tuple(tokens.shape)} of {tokens.dtype}")
+    least, most = (int(v) for v in torch.aminmax(tokens))
+    if least < 0 or most >= V:
+        raise ValueError(f"tokens from {least} to {most}, the vocabulary has {V}")
+
+
+def embed(table: torch.Tensor, tokens: torch.Tensor, x: torch.Tensor) -> None:
+    """Rows of the table for tokens (below its length) into x, in place.  Where none was drawn (-1), that of token 0."""
+    torch.index_select(table, 0, tokens.clamp(min=0), out=x)
+
+
 class Generator:
     """Sequences continued token by token.  `start` takes the prompts' tokens (int [S, prompt]), chooses the experts and draws the first tokens; `next` draws the ones after, from the first
-    call on as a replayed graph: embedding, layers, head and sampling without the host."""
+    call on as a replayed graph: embedding, layers, head and sampling without the host.  A sequence for which no token was left (-1: its logits are all NaN or minus
+    infinity) goes on as from token 0."""
 
     def __init__(self, model: Decoder, S: int, prompt: int, tokens: int, block_tokens: int = 64, **how):
         if model.head is None or model.embedding is None:
             raise ValueError("the model has no head or no embedding")
+        V, d = model.head.n, model.layers[0].qkv[0].k
+        if tuple(model.embedding.shape) != (V, d) or model.embedding.dtype != torch.float32:
+            raise ValueError(f"the embedding must be fp32 {(V, d)}, got {tuple(model.embedding.shape)} of {model.embedding.dtype}")
         dev = model.embedding.device
         self.model, self.seqs = model, Sequences(model, S, prompt + tokens, block_tokens, dev)
         self.prompt, self.token = Step(model, self.seqs, prompt), Step(model, self.seqs, 1)
         self.first, self.draw = Draw(model, self.prompt, **how), Draw(model, self.token, **how)
         self._graph: Optional[torch.cuda.CUDAGraph] = None
 
-    def _embed(self, tokens: torch.Tensor, x: torch.Tensor) -> None:
-        torch.index_select(self.model.embedding, 0, tokens, out=x)
-
     def start(self, prompt: torch.Tensor, u: torch.Tensor) -> torch.Tensor:
+        check_tokens(prompt, self.seqs.S, self.prompt.T, self.model.head.n)
         self.seqs.clear()
-        self._embed(prompt.reshape(-1), self.prompt.x)
+        embed(self.model.embedding, prompt.reshape(-1), self.prompt.x)
         self.seqs.route(self.model, self.prompt.x.bfloat16(), self.prompt.T)
         self.prompt()
         self.first.u.copy_(u)
@@ -260,7 +276,7 @@ class Generator:
         return self.draw.tokens
 
     def _enqueue(self) -> None:
-        self._embed(self.draw.tokens, self.token.x)
+        embed(self.model.embedding, self.draw.tokens, self.token.x)
         self.token._enqueue()
         self.draw()
 

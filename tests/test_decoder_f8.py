@@ -52,3 +52,26 @@ def test_what_has_no_head_gives_no_tokens(mq):
         dec.Draw(model, step)
     with pytest.raises(ValueError):
         dec.Generator(model, 2, 10, 10)
+
+
+def test_a_generator_refuses_tables_and_prompts_that_do_not_fit(mq):
+    """Before anything reaches the device: a lookup outside a table ends the process there, and a lookup of another size would move the buffer that the calls point to."""
+    model = _model(mq, layers=1, V=50)
+    good = model.embedding
+    for table in (good[:-1], torch.zeros(50, 255), good.bfloat16()):
+        model.embedding = table
+        with pytest.raises(ValueError, match="embedding"):
+            dec.Generator(model, 2, 10, 10)
+    dec.check_tokens(torch.tensor([[0, 49], [3, 4], [5, 6]]), 3, 2, 50)
+    dec.check_tokens(torch.tensor([[0], [49]], dtype=torch.int32), 2, 1, 50)
+    for tokens in (torch.tensor([[0, 50]]), torch.tensor([[-1, 0]]), torch.zeros(2, 1, dtype=torch.long), torch.zeros(2, dtype=torch.long), torch.zeros(1, 3, dtype=torch.long),
+                   torch.zeros(1, 2)):
+        with pytest.raises(ValueError, match="tokens"):
+            dec.check_tokens(tokens, 1, 2, 50)
+
+
+def test_a_sequence_without_a_token_goes_on_as_from_token_0():
+    table, x = torch.randn(7, 5), torch.empty(3, 5)
+    at = x.data_ptr()
+    dec.embed(table, torch.tensor([-1, 6, 2], dtype=torch.int32), x)
+    assert torch.equal(x, table[[0, 6, 2]]) and x.data_ptr() == at

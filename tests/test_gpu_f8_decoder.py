@@ -161,3 +161,26 @@ def test_integer_and_8_bit_matrices_in_one_layer():
         err = (o - outs[0]).pow(2).mean().sqrt() / outs[0].pow(2).mean().sqrt()
         # e4m3 rounds by 2^-4 / sqrt(3) = 0.036 of a value at most in the mean square, for both operands of three products in a row and two layers: 0.036 * sqrt(12)
         assert o.isfinite().all() and float(err) < 0.036 * 12 ** 0.5
+
+
+def test_a_sequence_without_a_token_goes_on():
+    """Token -1 (a row of logits that are all NaN or minus infinity) is looked up as token 0, in the first launch and in the replayed graph; the other sequences see nothing of it."""
+    S, T, V, n = 3, 5, 500, 4
+    model = _model(layers=1, V=V, seed=9)
+    prompt = torch.randint(0, V, (S, T), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+    u = _uniform(n + 1, S)
+    seen = []
+    for none in (-1, 0):
+        g = dec.Generator(model, S, T, n, 32, **_how(S))
+        g.start(prompt, u[0])
+        got = []
+        for i in range(n):
+            g.draw.tokens[1] = none
+            got.append(torch.cat([g.next(u[1 + i]).float(), g.draw.logprobs]))
+        torch.cuda.synchronize()
+        seen.append(torch.stack(got))
+    assert torch.equal(*seen)
+    with pytest.raises(ValueError, match="tokens"):
+        g.start(prompt[:, 1:], u[0])
+    with pytest.raises(ValueError, match="tokens"):
+        g.start(prompt + V, u[0])
