@@ -1013,6 +1013,8 @@ class F8GemmCall(_DeviceCall):
     def __init__(self, a: F8Rows, experts: Sequence[F8Mat], y, offsets: Optional[torch.Tensor] = None, perm: Optional[torch.Tensor] = None,
                  S: Optional[int] = None, T: int = 1, scatter: bool = False, in_bucket_order: bool = False, workspace: Optional[torch.Tensor] = None,
                  fast: bool = False):
+        if not experts or T < 1:
+            raise ValueError(f"{len(experts)} matrices, {T} rows a sample: there must be at least one")
         S = a.M // T if S is None else S
         if S * T != a.M or a.d != experts[0].k:
             raise ValueError(f"a is {a.M} rows of {a.d} features, the call is of {S} * {T} of {experts[0].k}")

@@ -75,3 +75,11 @@ def test_a_sequence_without_a_token_goes_on_as_from_token_0():
     at = x.data_ptr()
     dec.embed(table, torch.tensor([-1, 6, 2], dtype=torch.int32), x)
     assert torch.equal(x, table[[0, 6, 2]]) and x.data_ptr() == at
+
+
+def test_products_refuse_no_matrix_and_no_rows_a_sample(mq):
+    rows = mq.F8Rows(_aligned(2 * 256).view(2, 256), _aligned(8).view(2, 4), 2, 256)
+    mat = mq.F8Mat(_aligned(mq.moqe_f8_packed_bytes(32, 256)), 32, 256)
+    for mats, T in (([], 1), ([mat], 0), ([mat], -1)):
+        with pytest.raises(ValueError):
+            mq.F8GemmCall(rows, mats, torch.zeros(2, 32), T=T)
