@@ -579,9 +579,9 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
     auto each = [&](auto&& f) {                  // f(logit, index) of every element of the bins in question, and others of the row where there is no list
 #pragma unroll 1
       for (int i = tid; i < n; i += SMP_THREADS) {
-        const uint2 y = !in_list ? make_uint2(__float_as_uint(sc.clean(smp_one<BF16>(a, s, i))), i) : in_lds ? held[i] : list[i];
+        const uint2 y = !in_list ? make_uint2(__float_as_uint(sc.clean(smp_one<BF16>(a, s, i))), uint32_t(i)) : in_lds ? held[i] : list[i];
         const float x = __uint_as_float(y.x);
-        if (x > -INFINITY) f(x, min(int(y.y), V - 1));
+        if (x > -INFINITY) f(x, int(min(y.y, uint32_t(V - 1))));
       }
     };
     smp_u64 whole = r.k_mass;                    // weight that top-k leaves
