@@ -573,7 +573,9 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
  *   logits   : MOQE_TYPE_F32 or MOQE_TYPE_BF16, aligned to the type, row s at element s * stride (at least V);  V <= 2^20, S <= 65535
  *   u        : device float [S] (taken into [0, 1]; NaN is 0);  tokens: device int32 [S];  logprobs: device float [S] or NULL
  * Minus infinity and NaN are never taken; a row without anything else gives token -1 and log probability minus infinity.  Infinite logits share all of the weight.
- * Weights are in 64 bits, summed as integers of 2^-42 of the largest (results do not depend on any order); smaller ones count as nothing.
+ * Weights are in 64 bits, summed as integers, first over 256 neighbours (rows without filters) or the logits of a quarter of an octave (the cuts), in 2^-43 of the power of two above
+ * the largest of these, then in whole 2^-43 of that above the row's largest, in which single weights count where filters leave them.  What a row draws depends on its logits, its settings and u alone,
+ * not on the other rows or how the work is divided.  Running weights are within V * 2^-40 of the largest weight.
  * Workspace as the query says, 256-byte aligned.  S == 0 is a no-op. */
 typedef struct moqe_sampling { const float* temperature; const int32_t* top_k; const float *top_p, *min_p; } moqe_sampling;
 size_t  moqe_sample_workspace_bytes(int32_t S, int32_t V);

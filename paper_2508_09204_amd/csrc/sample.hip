@@ -1,8 +1,8 @@
 // Tokens from logits by temperature, top-k, top-p and min-p.
 //
-// Weights are 2^t for t = l log2(e) / T.  Everything that decides is an integer sum, so that neither the division of a row over work-groups nor the order of atomics can change a result:
-// weights are counted in units of 2^(a - 43), a the first integer above the largest t, from a table of 2^(j / 256) and a cubic (2^-42 of a weight).  A chunk of a row does not know the row's
-// largest logit; but it can take an integer `a` of its own, and sums of different chunks differ by a shift.
+// Weights are 2^t for t = l log2(e) / T, and everything that decides is an integer sum, from a table of 2^(j / 256) and a cubic (2^-42 of a weight).  A weight is counted in 2^-43 of the power of
+// two above the largest weight of what it is summed with first, which no division of a row over work-groups changes: a bin (a quarter of an octave) for the cuts, 256 neighbours for the draw
+// of rows without filters, the whole row where its largest is known.  Sums of different units differ by a shift, on the sum.  So neither a row's division nor the order of atomics changes a result.
 //
 //   k_sample_chunks  2048 or 8192 logits a work-group: their largest, sums of 256 neighbours, and (rows with cuts) counts and weights of bins a quarter of an octave wide, counted down from
 //                    the largest
@@ -35,13 +35,12 @@ struct SampleArgs {
   const float* temperature; const int32_t* top_k; const float *top_p, *min_p; const float* u;
   int32_t* tokens; float* logprobs;
   int32_t S, V, chunks, blocks, list_size;     // blocks: of SMP_NEIGHBOURS logits, as the chunks have them
-  struct SampleChunk* chunk; struct SampleRow* row; smp_u64* block; uint2* list;      // [S][chunks], [S], [S][blocks], [S][list_size] (bits, index)
+  struct SampleChunk* chunk; struct SampleRow* row; smp_u64* block; float* block_top; uint2* list;      // [S][chunks], [S], [S][blocks] twice, [S][list_size] (bits, index)
 };
 struct SampleChunk {
   float top;                                   // minus infinity: there is nothing else
   uint32_t top_at;                             // first index of the largest (rows of temperature 0)
-  smp_u64 total;                               // (rows cut by top-p)
-  smp_u64 mass[SMP_BINS];
+  smp_u64 mass[SMP_BINS];                      // in units of the bin (rows cut by top-p)
   uint32_t count[SMP_BINS];
 };
 struct SampleRow {                             // where the cuts lie
@@ -75,24 +74,27 @@ constexpr SmpTable smp_table() {
 }
 __device__ constexpr SmpTable SMP_POWERS = smp_table();
 
-// How a row's logits weigh, given the largest (of a chunk or of the row).  Differences of logits come first: they are exact or nearly so, also where t itself is far from 0.  Of a largest of
-// plus infinity the others count as minus infinity and the infinite ones as 0 (clean()).
+// How logits weigh, given the largest (of 256 neighbours, of a chunk, of the row).  Differences of logits come first: they are exact or nearly so, also where t itself is far from 0.  Of a largest
+// of plus infinity the others count as minus infinity and the infinite ones as 0 (clean()).
 struct SmpScale {
-  double c, c256, top_v, top_t, shift, floor4;
+  double c, c256, top_v, top_t, octave, shift, floor4;
   bool infinite;
   static __device__ double per_logit(float T) { return T > 0.f ? 1.4426950408889634074 / double(T) : 0.0; }
   __device__ SmpScale(double c_, float top) : c(c_), c256(c_ * 256), infinite(top == INFINITY) {
     top_v = infinite ? 0.0 : double(top);
-    top_t = top_v * c;                           // rounded here: as part of the difference below it would be a fused multiply-add's exact product, far from the anchor's where T is tiny
-    shift = (top_t - anchor() + SMP_ONE) * 256;
+    top_t = top_v * c;
+    octave = floor(top_t);
+    const double part = top_t - octave;
+    shift = (part + lost(top_v, top_t) + (SMP_ONE - 1)) * 256;
     floor4 = floor(top_t * 4);
   }
-  __device__ double anchor() const { return floor(top_t) + 1; }
+  // What the rounded product t = v c lacks.  Where t has no digits behind the point (T is tiny), logits that differ are octaves apart and it does not matter.
+  __device__ double lost(double v, double t) const { return fabs(t) < 4503599627370496.0 ? fma(v, c, -t) : 0.0; }
   __device__ float clean(float v) const { return infinite ? (v == INFINITY ? 0.f : -INFINITY) : v; }
-  // how many units of the other (a chunk's) are one of this (the row's), as a shift; bins between their largest
-  __device__ int unit_shift(const SmpScale& chunk) const {
-    if (infinite != chunk.infinite) return 64;
-    const double d = anchor() - chunk.anchor();
+  // how many units of the other (of some of the row's logits) are one of this (the row's), as a shift; bins between their largest
+  __device__ int unit_shift(const SmpScale& other) const {
+    if (infinite != other.infinite) return 64;
+    const double d = octave - other.octave;
     return d < 64 ? int(d) : 64;
   }
   __device__ int bin_shift(const SmpScale& chunk) const {
@@ -100,18 +102,25 @@ struct SmpScale {
     const double d = floor4 - chunk.floor4;
     return d < SMP_BINS ? int(d) : SMP_BINS;
   }
+  __device__ int bin_unit_shift(int bin) const { return int(octave - floor((floor4 - bin) * 0.25)); }       // as unit_shift(), for a bin's units
   __device__ int bin(float v) const { return int(fmin(floor4 - floor(double(v) * c * 4), double(SMP_BINS - 1))); }
   __device__ double below(float v) const { return (double(v) - top_v) * c; }           // log2 of its weight over the largest
-  // Its weight in units, in the last bits of a double of 2^52 and more.  0 from 2^-2 units on.
-  __device__ double mass_bits(float v, const double* powers) const {
-    const double u = fmax(fma(double(v) - top_v, c256, shift), -512.0);                // 256 log2 of the units; minus infinity too
+  // 2^(u / 256), u at least -512, to an integer in the last bits of a double of 2^52 and more.  0 from 2^-2 on.
+  static __device__ double power_bits(double u, const double* powers) {
     const double magic = 6755399441055744.0, n = u + magic, r = u - (n - magic);       // 1.5 * 2^52: the integer next to u stands in the last bits
     const int i = int(uint32_t(__builtin_bit_cast(smp_u64, n)));
     constexpr double L = 0.69314718055994530942 / 256;
     const double p = fma(r, fma(r, fma(r, L * L * L / 6, L * L / 2), L), 1.0) * powers[i & 255];
     return __builtin_bit_cast(double, __builtin_bit_cast(smp_u64, p) + (smp_u64(uint32_t(i & ~255) << 12) << 32)) + 4503599627370496.0;      // times 2^(i / 256), plus 2^52
   }
+  // Its weight in units.  Minus infinity weighs nothing.
+  __device__ double mass_bits(float v, const double* powers) const { return power_bits(fmax(fma(double(v) - top_v, c256, shift), -512.0), powers); }
   __device__ smp_u64 mass(float v, const double* powers) const { return __builtin_bit_cast(smp_u64, mass_bits(v, powers)) & 0xfffffffffffffull; }
+  // Its weight in units of its bin, 2^-43 of the power of two above the bin: a matter of the logit alone.
+  __device__ smp_u64 bin_mass(float v, const double* powers) const {
+    const double t = double(v) * c, whole = floor(t), part = t - whole;
+    return __builtin_bit_cast(smp_u64, power_bits((part + lost(double(v), t) + (SMP_ONE - 1)) * 256, powers)) & 0xfffffffffffffull;
+  }
   __device__ double units(float v) const { return below(v) + shift * (1.0 / 256); }    // log2 of its mass
 };
 
@@ -217,7 +226,7 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
   __shared__ double powers[256];
   __shared__ float tops[8];
   __shared__ uint32_t firsts[8], count[SMP_BINS][SMP_COPIES];
-  __shared__ smp_u64 mass[SMP_BINS][SMP_COPIES], totals[8];
+  __shared__ smp_u64 mass[SMP_BINS][SMP_COPIES];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, s = blockIdx.y, chunk = blockIdx.x;
   SampleChunk& out = a.chunk[static_cast<size_t>(s) * a.chunks + chunk];
   float v[P][4];
@@ -225,12 +234,12 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
   if (tid < 256) powers[tid] = SMP_POWERS.v[tid];
   const SmpAsk ask(a, s);
   for (int i = tid; i < SMP_BINS * SMP_COPIES; i += SMP_THREADS) { (&count[0][0])[i] = 0; (&mass[0][0])[i] = 0; }
-  float top = -INFINITY;
+  float top = -INFINITY, most[P];              // of the chunk, of 256 neighbours
 #pragma unroll
-  for (int j = 0; j < P; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) top = fmaxf(top, v[j][e]);
-  top = smp_wave_max(top);
+  for (int j = 0; j < P; ++j) {
+    most[j] = smp_wave_max(fmaxf(fmaxf(v[j][0], v[j][1]), fmaxf(v[j][2], v[j][3])));
+    top = fmaxf(top, most[j]);
+  }
   if (lane == 0) tops[wave] = top;
   __syncthreads();
 #pragma unroll
@@ -255,40 +264,35 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
   }
   if (top == -INFINITY || (ask.filtered && !ask.cuts)) return;
   const SmpScale sc(SmpScale::per_logit(ask.T), top);
-  if (sc.infinite) {
-#pragma unroll
-    for (int j = 0; j < P; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[j][e] = sc.clean(v[j][e]);
-  }
   if (!ask.filtered) {
-    smp_u64* block = a.block + static_cast<size_t>(s) * a.blocks + chunk * (P * 8) + wave;
+    const size_t block = static_cast<size_t>(s) * a.blocks + chunk * (P * 8) + wave;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       double sum = 0;                          // integers below 2^53: exact in any order
+      if (most[j] > -INFINITY) {
+        const SmpScale bs(sc.c, most[j]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += sc.mass_bits(v[j][e], powers) - 4503599627370496.0;
-      sum = smp_wave_upto(sum);
-      if (lane == 63) block[j * 8] = static_cast<smp_u64>(sum);
+        for (int e = 0; e < 4; ++e) sum += bs.mass_bits(bs.clean(v[j][e]), powers) - 4503599627370496.0;
+        sum = smp_wave_upto(sum);
+      }
+      if (lane == 63) {
+        a.block[block + j * 8] = static_cast<smp_u64>(sum);
+        a.block_top[block + j * 8] = most[j];
+      }
     }
     return;
   }
-  smp_u64 total = 0;
 #pragma unroll
   for (int j = 0; j < P; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (v[j][e] > -INFINITY) {
-        const int b = sc.bin(v[j][e]);
+    for (int e = 0; e < 4; ++e) {
+      const float x = sc.clean(v[j][e]);
+      if (x > -INFINITY) {
+        const int b = sc.bin(x);
         atomicAdd(&count[b][lane % SMP_COPIES], 1u);
-        if (ask.p < 1.f) {
-          const smp_u64 m = sc.mass(v[j][e], powers);
-          total += m;
-          if (m) atomicAdd(&mass[b][lane % SMP_COPIES], m);
-        }
+        if (ask.p < 1.f && b < SMP_BINS - 1) atomicAdd(&mass[b][lane % SMP_COPIES], sc.bin_mass(x, powers));
       }
-  total = smp_wave_sum(total);
-  if (lane == 0) totals[wave] = total;
+    }
   __syncthreads();
   if (tid < SMP_BINS) {
     uint32_t n = 0;
@@ -298,12 +302,6 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
     out.count[tid] = n;
     out.mass[tid] = m;
   }
-  if (tid == 0) {
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) total += totals[w];
-    out.total = total;
-  }
 }
 
 template <bool BF16, int P>
@@ -312,7 +310,7 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
   __shared__ double powers[256];
   __shared__ smp_u64 mass[8][64];
   __shared__ uint32_t count[8][64], before[BLOCKS];
-  __shared__ int bins_down[SMP_CHUNKS], units_down[SMP_CHUNKS];
+  __shared__ int bins_down[SMP_CHUNKS];
   __shared__ SampleRow cut;
   __shared__ uint32_t list_at;
   __shared__ int done;
@@ -336,34 +334,25 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
   if (ask.cuts) {
     if (tid < a.chunks) {
       const float t = tid < 64 ? chunk_top : of_row[tid].top;
-      const SmpScale cs(per, t);
-      bins_down[tid] = t > -INFINITY ? sc.bin_shift(cs) : SMP_BINS;
-      units_down[tid] = t > -INFINITY ? sc.unit_shift(cs) : 64;
+      bins_down[tid] = t > -INFINITY ? sc.bin_shift(SmpScale(per, t)) : SMP_BINS;
     }
     __syncthreads();
-    // The row's bins, 64 at a time (16 octaves, mostly enough): wave w adds up those of every eighth chunk, wave 0 looks for the cuts.  What a shift puts past the last bin weighs nothing and is
-    // not counted.
+    // The row's bins, 64 at a time (16 octaves, mostly enough for top-k; top-p alone asks for the weight of all): wave w adds up those of every eighth chunk, wave 0 looks for the cuts.  What a
+    // shift puts past the last bin weighs nothing and is not counted, and neither does the last bin's weight, which some chunks have and others not.
     SampleRow r{};
     r.k_bin = r.p_lo = SMP_BINS;
     r.p_hi = -1;
-    smp_u64 n[SEGMENTS], m[SEGMENTS], all = 0;      // of wave 0: sums up to bin 64 g + lane
-    if (wave == 0) {
-      if (ask.p < 1.f && ask.k == 0) {
-        for (int c = lane; c < a.chunks; c += 64)
-          if (units_down[c] < 64) all += of_row[c].total >> units_down[c];
-        all = smp_wave_sum(all);
-      }
-    }
+    smp_u64 n[SEGMENTS], m[SEGMENTS];          // of wave 0: sums up to bin 64 g + lane, weights in units of the row
 #pragma unroll
     for (int g = 0; g < SEGMENTS; ++g) {
       smp_u64 mm = 0;
       uint32_t nn = 0;
 #pragma unroll 4
       for (int c = wave; c < a.chunks; c += 8) {
-        const int from = g * 64 + lane - bins_down[c], da = units_down[c];
+        const int from = g * 64 + lane - bins_down[c];
         if (from >= 0) {
           nn += of_row[c].count[from];
-          if (da < 64 && ask.p < 1.f) mm += of_row[c].mass[from] >> da;
+          if (ask.p < 1.f) mm += of_row[c].mass[from];
         }
       }
       count[wave][lane] = nn;
@@ -373,11 +362,11 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
         n[g] = m[g] = 0;
 #pragma unroll
         for (int w = 0; w < 8; ++w) { n[g] += count[w][lane]; m[g] += mass[w][lane]; }
+        m[g] = g * 64 + lane < SMP_BINS - 1 ? m[g] >> sc.bin_unit_shift(g * 64 + lane) : 0;
         n[g] = smp_wave_upto(n[g]) + (g ? smp_lane(n[g > 0 ? g - 1 : 0], 63) : 0);
         m[g] = smp_wave_upto(m[g]) + (g ? smp_lane(m[g > 0 ? g - 1 : 0], 63) : 0);
-        const smp_u64 so_far = smp_lane(n[g], 63), weight = smp_lane(m[g], 63);
-        const bool k_there = ask.k == 0 || so_far >= static_cast<smp_u64>(ask.k), p_there = !(ask.p < 1.f) || ask.k > 0 || double(weight) >= double(ask.p) * double(all);
-        if (lane == 0) done = (k_there && p_there) || g + 1 == SEGMENTS ? g + 1 : 0;
+        const smp_u64 so_far = smp_lane(n[g], 63);
+        if (lane == 0) done = (ask.k > 0 && so_far >= static_cast<smp_u64>(ask.k)) || g + 1 == SEGMENTS ? g + 1 : 0;
       }
       __syncthreads();
       if (done) break;
@@ -401,12 +390,11 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_cut(SampleArgs a) {
           if (bin > 0 && (bin - 1) / 64 == g) sum = smp_lane(x[g], (bin - 1) & 63);
         return sum;
       };
-      smp_u64 least = all, most = all;           // weight that top-k leaves
+      smp_u64 least = have == SEGMENTS ? smp_lane(m[SEGMENTS - 1], 63) : 0, most = least;       // weight that top-k leaves
       if (ask.k > 0) {
         r.k_bin = first([&](smp_u64 cn, smp_u64) { return cn >= static_cast<smp_u64>(ask.k); });
         if (r.k_bin == SMP_BINS - 1) {           // what is beyond weighs nothing
           r.k_bin = SMP_BINS;
-          least = most = smp_lane(m[SEGMENTS - 1], 63);
         } else {
           r.k_above = before_bin(n, r.k_bin);
           least = before_bin(m, r.k_bin);
@@ -521,12 +509,13 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
   __shared__ smp_u64 part[8], hist[KEYS], blocks[SMP_BLOCKS], found, found_here;
   __shared__ uint2 held[SMP_HELD];
   __shared__ uint32_t lows[8], highs[8];
-  __shared__ int found_at, units_down[SMP_CHUNKS];
+  __shared__ int found_at;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, s = blockIdx.x, V = a.V;
   const SmpGroup group{part};
   const SampleChunk* of_row = a.chunk + static_cast<size_t>(s) * a.chunks;
-  const int n_blocks = a.blocks, per_chunk = n_blocks / a.chunks;
+  const int n_blocks = a.blocks;
   const smp_u64* row_blocks = a.block + static_cast<size_t>(s) * n_blocks;
+  const float* block_tops = a.block_top + static_cast<size_t>(s) * n_blocks;
   const smp_u64 first_blocks = tid < n_blocks ? row_blocks[tid] : 0;        // asked for before it is known how they count
   float chunk_top;
   const float top = smp_row_top(of_row, a.chunks, &chunk_top);
@@ -554,10 +543,6 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
   const double per = SmpScale::per_logit(ask.T);
   const SmpScale sc(per, top);
   const double floor_t = ask.least > 0.f ? log2(double(ask.least)) : -INFINITY;
-  if (tid < a.chunks) {
-    const float t = tid < 64 ? chunk_top : of_row[tid].top;
-    units_down[tid] = t > -INFINITY ? ask.filtered ? 0 : sc.unit_shift(SmpScale(per, t)) : 64;
-  }
 
   // kept: logits above `cut`, and those equal to it before index `bound`
   float cut = -INFINITY;
@@ -570,9 +555,13 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
     for (int i = tid; i < r.listed; i += SMP_THREADS) held[i] = list[i];
   __syncthreads();
   for (int b = tid; b < n_blocks; b += SMP_THREADS) {
-    const int da = units_down[b / per_chunk];
     const smp_u64 x = b == tid ? first_blocks : row_blocks[b];
-    blocks[b] = da < 64 ? x >> da : 0;
+    int down = 0;
+    if (!ask.filtered) {
+      const float t = block_tops[b];
+      down = t > -INFINITY ? sc.unit_shift(SmpScale(per, t)) : 64;
+    }
+    blocks[b] = down < 64 ? x >> down : 0;
   }
   if (r.listed > 0) {
     const int n = in_list ? r.listed : V;
@@ -717,6 +706,9 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
   if (wave != 0) return;
   const int block = found_at;
   goal = found;
+  // The same weights in the same units again, shifted as their sum was: the running weight of the last one is the neighbourhood's.
+  const SmpScale bs(per, ask.filtered ? top : block_tops[block]);
+  const int down = sc.unit_shift(bs);
   float x[4];
   smp_u64 m[4], own = 0;
 #pragma unroll
@@ -729,15 +721,14 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
     const int i = block * SMP_NEIGHBOURS + lane * 4 + e;
     x[e] = sc.clean(x[e]);
     const bool in = (x[e] > cut || (x[e] == cut && i < bound)) && sc.below(x[e]) >= floor_t;
-    m[e] = in && x[e] > -INFINITY ? sc.mass(x[e], powers) : 0;
+    m[e] = in && x[e] > -INFINITY ? bs.mass(x[e], powers) : 0;
     own += m[e];
   }
-  const smp_u64 run_upto = smp_wave_upto(own), in_block = smp_lane(run_upto, 63);
-  if (goal > in_block) goal = in_block;          // sums of a chunk's units and of the row's may differ in the last unit
-  if (run_upto >= goal && run_upto - own < goal) {
+  const smp_u64 run_upto = smp_wave_upto(own);
+  if ((run_upto >> down) >= goal && ((run_upto - own) >> down) < goal) {
     smp_u64 run = run_upto - own;
     int e = 0;
-    while (e < 3 && run + m[e] < goal) run += m[e++];
+    while (e < 3 && ((run + m[e]) >> down) < goal) run += m[e++];
     const float v = e == 0 ? x[0] : e == 1 ? x[1] : e == 2 ? x[2] : x[3];
     a.tokens[s] = block * SMP_NEIGHBOURS + lane * 4 + e;
     if (a.logprobs) a.logprobs[s] = float((sc.units(v) - log2(double(W))) * 0.69314718055994530942);
@@ -745,14 +736,15 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
 }
 
 namespace {
-struct SampleSpace { int places, chunks, list_size; size_t row, block, list, total; };
+struct SampleSpace { int places, chunks, list_size; size_t row, block, block_top, list, total; };
 SampleSpace space(int S, int V) {
   SampleSpace p;
   p.places = static_cast<long long>(S) * V < (1 << 21) && V <= SMP_CHUNKS * SMP_THREADS * 4 ? 1 : 4;
   p.chunks = (V + p.places * SMP_THREADS * 4 - 1) / (p.places * SMP_THREADS * 4);
   p.row = align256(size_t(S) * p.chunks * sizeof(SampleChunk));
   p.block = p.row + align256(size_t(S) * sizeof(SampleRow));
-  p.list = p.block + align256(size_t(S) * p.chunks * p.places * 8 * 8);
+  p.block_top = p.block + align256(size_t(S) * p.chunks * p.places * 8 * 8);
+  p.list = p.block_top + align256(size_t(S) * p.chunks * p.places * 8 * 4);
   p.list_size = V < SMP_LIST ? V : SMP_LIST;
   p.total = p.list + align256(size_t(S) * p.list_size * 8);
   return p;
@@ -766,7 +758,8 @@ int32_t launch_sample(const void* logits, bool bf16, long long stride, int S, in
   const SampleSpace p = space(S, V);
   uint8_t* b = static_cast<uint8_t*>(ws);
   SampleArgs a{logits, stride, how.temperature, how.top_k, how.top_p, how.min_p, u, tokens, logprobs, S, V, p.chunks, p.chunks * p.places * 8, p.list_size,
-               reinterpret_cast<SampleChunk*>(b), reinterpret_cast<SampleRow*>(b + p.row), reinterpret_cast<smp_u64*>(b + p.block), reinterpret_cast<uint2*>(b + p.list)};
+               reinterpret_cast<SampleChunk*>(b), reinterpret_cast<SampleRow*>(b + p.row), reinterpret_cast<smp_u64*>(b + p.block), reinterpret_cast<float*>(b + p.block_top),
+               reinterpret_cast<uint2*>(b + p.list)};
   ProfileScope ps(MOQE_PK_OTHER, st);
   const bool filters = how.top_k || how.top_p || how.min_p;
   const dim3 chunks(p.chunks, S), threads(SMP_THREADS);
