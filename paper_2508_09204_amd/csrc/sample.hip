@@ -262,15 +262,14 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
     }
     return;
   }
-  if (top == -INFINITY || (ask.filtered && !ask.cuts)) return;
-  const SmpScale sc(SmpScale::per_logit(ask.T), top);
-  if (!ask.filtered) {
+  const double per = SmpScale::per_logit(ask.T);
+  if (!ask.filtered) {                         // a chunk of nothing says so too
     const size_t block = static_cast<size_t>(s) * a.blocks + chunk * (P * 8) + wave;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       double sum = 0;                          // integers below 2^53: exact in any order
       if (most[j] > -INFINITY) {
-        const SmpScale bs(sc.c, most[j]);
+        const SmpScale bs(per, most[j]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum += bs.mass_bits(bs.clean(v[j][e]), powers) - 4503599627370496.0;
         sum = smp_wave_upto(sum);
@@ -282,6 +281,8 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_chunks(SampleArgs a) {
     }
     return;
   }
+  if (top == -INFINITY || !ask.cuts) return;
+  const SmpScale sc(per, top);
 #pragma unroll
   for (int j = 0; j < P; ++j)
 #pragma unroll

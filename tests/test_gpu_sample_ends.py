@@ -48,6 +48,25 @@ def test_one_logit_above_faint_ones(V, faint):
     check_all(x, [u for u in ENDS for _ in range(3)])
 
 
+@pytest.mark.parametrize("none", [-float("inf"), NAN])
+@pytest.mark.parametrize("V,S", [(5003, 16), (40000, 16), (40000, 64), (300000, 16)])
+def test_places_without_anything(none, V, S):
+    """Rows of which whole stretches, of thousands of logits and of 256, hold nothing that can be taken; a workspace that held other numbers."""
+    x = torch.full((S, V), none, device=DEV)
+    for i in range(S):
+        x[i, (i * 2711) % V :: 997 if i % 2 else V] = float(i % 5)
+        x[i, (i * 1301) % V] = 3.0
+    u = [ENDS[i % len(ENDS)] if i < 8 else i / S for i in range(S)]
+    tokens, lp = torch.full((S,), -9, dtype=torch.int32, device=DEV), torch.full((S,), 7.0, device=DEV)
+    for fill in (0, 0x3f, 0xff):
+        ws = torch.full((mq.moqe_sample_workspace_bytes(S, V),), fill, dtype=torch.uint8, device=DEV)
+        mq.moqe_sample(x, torch.tensor(u, dtype=F32, device=DEV), tokens.fill_(-9), logprobs=lp, workspace=ws)
+        torch.cuda.synchronize()
+        rows, u32 = torch.where(x.isnan(), -float("inf"), x).double().cpu().numpy(), torch.tensor(u, dtype=F32).double().numpy()
+        for s in range(S):
+            check_token(rows[s], u32[s], int(tokens[s]), float(lp[s]))
+
+
 @pytest.mark.parametrize("t", [F32, BF])
 def test_a_confident_models_rows(t):
     """Normal logits and one winner far above them, by temperatures below 1, at both ends of u."""
