@@ -576,6 +576,7 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
  * Weights are in 64 bits, summed as integers, first over 256 neighbours (rows without filters) or the logits of a quarter of an octave (the cuts), in 2^-43 of the power of two above
  * the largest of these, then in whole 2^-43 of that above the row's largest, in which single weights count where filters leave them.  What a row draws depends on its logits, its settings and u alone,
  * not on the other rows or how the work is divided.  Running weights are within V * 2^-40 of the largest weight.
+ * Log probabilities are never above 0, and 0 of a token that is the only one kept; they are within 2^-24 of themselves and V * 2^-40.
  * Workspace as the query says, 256-byte aligned.  S == 0 is a no-op. */
 typedef struct moqe_sampling { const float* temperature; const int32_t* top_k; const float *top_p, *min_p; } moqe_sampling;
 size_t  moqe_sample_workspace_bytes(int32_t S, int32_t V);

@@ -732,7 +732,12 @@ __global__ __launch_bounds__(SMP_THREADS) void k_sample_draw(SampleArgs a) {
     while (e < 3 && ((run + m[e]) >> down) < goal) run += m[e++];
     const float v = e == 0 ? x[0] : e == 1 ? x[1] : e == 2 ? x[2] : x[3];
     a.tokens[s] = block * SMP_NEIGHBOURS + lane * 4 + e;
-    if (a.logprobs) a.logprobs[s] = float((sc.units(v) - log2(double(W))) * 0.69314718055994530942);
+    if (a.logprobs) {
+      // Of a token with half of the weight or more, by what is not its: integers, 0 where it is the only one.  Of others, by their weight before it was rounded: that may be far below a unit.
+      const smp_u64 one = e == 0 ? m[0] : e == 1 ? m[1] : e == 2 ? m[2] : m[3];
+      const double rest = fmax(ldexp(double(W), down) - double(one), 0.0);
+      a.logprobs[s] = float(rest <= double(one) ? 0.0 - log1p(rest / double(one)) : (sc.units(v) - log2(double(W))) * 0.69314718055994530942);
+    }
   }
 }
 

@@ -1,4 +1,5 @@
-"""moqe_sample where single weights are far below what a row's sums are counted in: tokens at the ends of u on rows with faint neighbourhoods, the same token whatever else a call has.
+"""moqe_sample where single weights are far below what a row's sums are counted in: tokens at the ends of u on rows with faint neighbourhoods, the same token whatever else a call has, and log
+probabilities next to 0.
 
 Without filters, weights are rounded to 2^-43 of the power of two above the largest of their 256 neighbours, whose sums are cut to whole units of the row: of a largest weight of 1, V 2^-42 for
 roundings and for the table and cubic (2^-42 of a weight) each, and V / 256 units of 2^-42, together less than V 2^-40.  So a token is right if u W lies within V 2^-40 of its part of the running weight.
@@ -28,7 +29,7 @@ def check_token(x, u, token, lp, T=1.0):
     assert 0 <= token < len(x), (u, token)
     assert w[token] > 0 and upto[token] - w[token] <= goal + tol and upto[token] >= goal - tol, (u, token, goal, upto[token])
     want = math.log(w[token] / upto[-1])
-    assert abs(lp - want) <= 2.0 ** -24 * abs(want) + 2.0 ** -20, (lp, want)
+    assert lp <= 0 and abs(lp - want) <= 2.0 ** -24 * abs(want) + 2.0 ** -20, (lp, want)
 
 
 def check_all(x, u, T=None, **how):
@@ -82,7 +83,7 @@ def test_a_generators_first_numbers():
     x = torch.full((4, 3000), -32.0, device=DEV)
     x[:, 2900] = 0.0
     tokens, lp, _ = run(x, [0.0] * 4)
-    assert (tokens >= 0).all() and (tokens < 3000).all()
+    assert (tokens >= 0).all() and (tokens < 3000).all() and (lp <= 0).all()
 
 
 @pytest.mark.parametrize("how", [{}, {"temperature": 0.7}, {"top_p": 0.9}, {"top_p": 0.999999, "temperature": 0.8}, {"top_k": 40, "top_p": 0.9}, {"top_k": 20000, "top_p": 0.97}, {"min_p": 1e-12},
@@ -140,4 +141,40 @@ def test_filters_at_the_ends_of_u(t, above, V):
         assert 0 <= at < V and may[at], (settings, u[s], at)
         assert few[:at].sum() <= end * many.sum() + tol and many[: at + 1].sum() >= end * few.sum() - tol, (settings, u[s], at)
         most, least = math.log(many[at] / few.sum()), math.log(many[at] / many.sum())
-        assert least - 2.0 ** -24 * abs(least) - 2.0 ** -20 <= lp[s] <= most + 2.0 ** -24 * abs(most) + 2.0 ** -20, (settings, u[s], lp[s])
+        assert lp[s] <= 0 and least - 2.0 ** -24 * abs(least) - 2.0 ** -20 <= lp[s] <= most + 2.0 ** -24 * abs(most) + 2.0 ** -20, (settings, u[s], lp[s])
+
+
+@pytest.mark.parametrize("t", [F32, BF])
+def test_the_only_token_kept_has_log_probability_0(t):
+    S, V = 64, 5003
+    x, u = logits_of(S, V, t, 2.0, 2), uniform(S, 4)
+    top = x.double().cpu().numpy().argmax(1)
+    T = (0.3 + 0.05 * np.arange(S)).tolist()
+    peaked = x.clone()
+    peaked[torch.arange(S, device=DEV), torch.from_numpy(top).to(DEV)] = 40.0
+    alone = torch.full_like(x, -float("inf"))
+    alone[torch.arange(S, device=DEV), torch.from_numpy(top).to(DEV)] = x.amax(1)
+    for logits, how in ((x, dict(top_k=[1] * S)), (x, dict(top_k=[1] * S, top_p=[0.9] * S, min_p=[0.1] * S)), (x.float() + torch.arange(V, device=DEV) * 1e-6, dict(min_p=[1.0] * S)),
+                        (peaked, dict(top_p=[0.9] * S)), (peaked, dict(min_p=[0.5] * S)), (x, dict(top_p=[0.0] * S)), (alone, {}), (alone, dict(top_p=[0.9] * S))):
+        best = logits.double().cpu().numpy().argmax(1)
+        for temperature in ({}, {"temperature": T}):
+            tokens, lp, _ = run(logits, u, **how, **temperature)
+            assert np.array_equal(tokens, best) and (lp == 0).all(), (how.keys(), lp[lp != 0][:4])
+
+
+@pytest.mark.parametrize("gap", [1e-3, 0.1, 1.0, 5.0, 10.0, 20.0, 30.0, 60.0])
+def test_log_probabilities_are_at_most_0(gap):
+    """Two tokens, and two above faint ones: next to 0 the log probability is as near as the sums' units let it be, 2^-40, and never above."""
+    S, V = 40, 4000
+    for rest in (-float("inf"), -60.0):
+        x = torch.full((S, V), rest, device=DEV)
+        x[:, 5] = torch.linspace(-3.0, 17.0, S, device=DEV)
+        x[:, 3005] = x[:, 5] - gap
+        u = uniform(S, 8)
+        for how in ({}, {"top_k": [2] * S}):
+            tokens, lp, _ = run(x, u, **how)
+            v = x.double().cpu().numpy()
+            for s in range(S):
+                w = np.exp(v[s] - v[s].max())
+                want = math.log(w[tokens[s]] / w.sum())
+                assert tokens[s] in (5, 3005) and lp[s] <= 0 and abs(lp[s] - want) <= 2.0 ** -24 * abs(want) + 2.0 ** -40, (rest, how, lp[s], want)
