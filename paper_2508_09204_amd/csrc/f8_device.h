@@ -14,12 +14,14 @@ typedef float f8_f32x4 __attribute__((ext_vector_type(4)));
 // Scale exponent for values whose largest finite size is `top`.
 __device__ __forceinline__ int f8_exponent(float top) { return kv_scale_exponent(__float_as_uint(top)); }
 
-// Eight codes of x * 2^-e, to nearest even.  |x| <= 448 * 2^e but for infinities, which the conversion would make NaN of: they become the largest code.
+// Eight codes of x * 2^-e, to nearest even.  |x| <= 448 * 2^e but for infinities, which the conversion would make NaN of: they become the largest code.  448 * 2^120 is an infinity itself: values
+// of that scale are halved first, by which only those that are zeros in it lose digits.
 __device__ __forceinline__ uint2 f8_codes(const float* x, int e) {
-  const float scale = __uint_as_float(uint32_t(e + 127) << 23), most = 448.f * scale;
+  const bool far = e > 119;
+  const float scale = __uint_as_float(uint32_t(e - far + 127) << 23), most = 448.f * scale;
   float v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = fabsf(x[i]) == INFINITY ? copysignf(most, x[i]) : x[i];
+  for (int i = 0; i < 8; ++i) v[i] = fabsf(x[i]) == INFINITY ? copysignf(most, x[i]) : x[i] * (far ? 0.5f : 1.f);
   typedef short s16x2 __attribute__((ext_vector_type(2)));
   s16x2 lo = {0, 0}, hi = {0, 0};
   lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, v[0], v[1], scale, false);
