@@ -208,12 +208,15 @@ __device__ __forceinline__ void largest(const float (&x)[N], float* top, bool* i
   }
   *top = fmaxf(*top, m);
 }
+// Infinities as what becomes the largest code by the scale returned: that given, or half of it, of values halved too, where 448 of it would be an infinity again.  All of a thread's values of a block
+// have the same one.
 template <int N>
-__device__ __forceinline__ void no_infinities(float (&x)[N], bool infinite, float scale) {
-  if (!infinite) return;
+__device__ __forceinline__ float no_infinities(float (&x)[N], bool infinite, float scale) {
+  if (!infinite) return scale;
+  const float by = 448.f * scale < INFINITY ? 1.f : 0.5f;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (fabsf(x[i]) == INFINITY) x[i] = copysignf(448.f * scale, x[i]);
+  for (int i = 0; i < N; ++i) x[i] = fabsf(x[i]) == INFINITY ? copysignf(448.f * (scale * by), x[i]) : x[i] * by;
+  return scale * by;
 }
 
 // A block of a sequence that a call writes to: its new tokens lo .. hi, its first token, its place in the cache.
@@ -294,16 +297,16 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const BlockToke
     for (int n = 0; n < NS; ++n) {
       const int u = n * th + tid;
       if (u >= slots) continue;
-      no_infinities(x[n], infinite, s.scale);
+      const float scale = no_infinities(x[n], infinite, s.scale);
       const uint32_t t = uint32_t(b.lo - b.first + u / SL);
       uint8_t* ka = codes + kv_key_at(t, uint32_t(da), DH);
       uint8_t* kb = codes + kv_key_at(t, uint32_t(db), DH);
       if constexpr (BF16) {
-        *reinterpret_cast<uint2*>(ka) = make_uint2(codes4(x[n], s.scale), codes4(x[n] + 4, s.scale));
-        *reinterpret_cast<uint2*>(kb) = make_uint2(codes4(x[n] + 8, s.scale), codes4(x[n] + 12, s.scale));
+        *reinterpret_cast<uint2*>(ka) = make_uint2(codes4(x[n], scale), codes4(x[n] + 4, scale));
+        *reinterpret_cast<uint2*>(kb) = make_uint2(codes4(x[n] + 8, scale), codes4(x[n] + 12, scale));
       } else {
-        *reinterpret_cast<uint32_t*>(ka) = codes4(x[n], s.scale);
-        *reinterpret_cast<uint32_t*>(kb) = codes4(x[n] + 4, s.scale);
+        *reinterpret_cast<uint32_t*>(ka) = codes4(x[n], scale);
+        *reinterpret_cast<uint32_t*>(kb) = codes4(x[n] + 4, scale);
       }
     }
   }
@@ -366,27 +369,27 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, const BlockTo
     const int u = n * th + tid;
     if (u < quads) {
       uint32_t* to = lds + kv_value_at(uint32_t(32 * g_lo + u / PCS * 4), uint32_t(u % PCS * P), DH) / 4;
-      float x[4][P];
+      float x[4][P], scale;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         piece_values<BF16>(vq[n][t], x[t]);
-        no_infinities(x[t], infinite, s.scale);
+        scale = no_infinities(x[t], infinite, s.scale);
       }
 #pragma unroll
       for (int i = 0; i < P; ++i) {              // neighbouring dims of 16 lie 16 bytes apart
         const float y[4] = {x[0][i], x[1][i], x[2][i], x[3][i]};
-        to[4 * i] = codes4(y, s.scale);
+        to[4 * i] = codes4(y, scale);
       }
     }
   }
   for (int u = tid; u < rest; u += th) {
     float x[P];
     piece_values<BF16>(u == tid ? vr : rest_piece(u), x);
-    no_infinities(x, infinite, s.scale);
+    const float scale = no_infinities(x, infinite, s.scale);
     uint8_t* to = codes + kv_value_at(uint32_t(rest_token(u) - b.first), uint32_t(u % PCS * P), DH);
 #pragma unroll
     for (int i = 0; i < P; i += 4) {
-      const uint32_t w = codes4(x + i, s.scale);
+      const uint32_t w = codes4(x + i, scale);
 #pragma unroll
       for (int t = 0; t < 4; ++t) to[16 * (i + t)] = uint8_t(w >> (8 * t));
     }

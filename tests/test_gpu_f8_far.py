@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import decoder_oracle as do
 from oracle import f8_oracle as fo
 from paper_2508_09204_amd import binding as mq
 from tests.test_gpu_f8 import dev, empty_rows, f64, rows_of, sync
@@ -58,3 +59,27 @@ def test_gated_results_beside_infinities(M, n, fast):
     assert scales[0, 0] == 127 + 120 and codes[0, 3] == 0x7e and codes[0, 4] == 0xfe
     b = y.blocks
     assert (y.scales[:, :b].cpu().numpy() == scales).all() and (y.codes[:, : b * 128].cpu().numpy() == codes).all()
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_infinities_beside_the_largest_keys_and_values(t, dh):
+    """The same of the cache's blocks, whose tokens come 32 at a time and one by one."""
+    rng = np.random.default_rng(dh)
+    rows, bt = 40, 32
+    x = np.where(rng.random((rows, 3 * dh)) < 0.5, 1.0, -1.0) * 2.0 ** 127 * rng.uniform(0.01, 1.99, size=(rows, 3 * dh))
+    x[:, :dh] = 1.0
+    x[3, dh + 7], x[35, dh + 1], x[20, 2 * dh + 9], x[9, 2 * dh + 8], x[39, 3 * dh - 1] = INF, -INF, INF, -INF, INF
+    x = dev(x, torch.float32).to(t)
+    cache = mq.KvCache.empty(2, 1, bt, dh, DEV)
+    q = torch.empty((rows, dh), dtype=torch.bfloat16, device=DEV)
+    mq.moqe_kv_append(x, 1, mq.Rope(None, 0), mq.KvBatch(dev(np.array([[1, 0]], np.int32)), dev(np.array([rows], np.int32)), 1, rows, rows), cache, q)
+    sync()
+    want = f64(x)
+    tok, d = np.meshgrid(np.arange(bt), np.arange(dh), indexing="ij")
+    for codes, scales, at, first in ((cache.k, cache.k_scale, do.key_at(tok, d, dh), dh), (cache.v, cache.v_scale, do.value_at(tok, d, dh), 2 * dh)):
+        for n, block in enumerate((1, 0)):
+            part = want[n * bt : (n + 1) * bt, first : first + dh]
+            s = do.scale_for(np.abs(part[np.isfinite(part)]).max())
+            assert s == 2.0 ** 120 == float(scales[block, 0]) and np.isinf(part).any()
+            assert np.array_equal(codes[block, 0].cpu().numpy()[at][: len(part)], do.e4m3_code(part / s))
