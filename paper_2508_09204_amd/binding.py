@@ -664,10 +664,10 @@ class _DeviceCall:
         self._host = any(d.type != "cuda" for d in devices)
         self._device = next(iter(devices)).index if devices and not self._host else None
 
-    def _on_device(self) -> None:
+    def _on_device(self, stream: Optional[int] = None) -> None:
         if self._host and not _dry_run:
             raise ValueError("the library reads and writes device memory, these tensors are not on the GPU")
-        if self._device is not None and self._device != torch._C._cuda_getDevice():      # the stream is the current device's
+        if not stream and self._device is not None and self._device != torch._C._cuda_getDevice():      # the stream is the current device's then; one that is given is where the caller has it
             raise ValueError(f"the tensors are on GPU {self._device}, the current one is {torch._C._cuda_getDevice()}")
 
 
@@ -714,7 +714,7 @@ class ResidualNormCall(_DeviceCall):
         self._arg = C.byref(s)
 
     def __call__(self, stream: Optional[int] = None) -> None:
-        self._on_device()
+        self._on_device(stream)
         rc = lib.moqe_residual_norm(self._arg, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
@@ -823,7 +823,7 @@ class KvAppendCall(_DeviceCall):
         self._args = (qp, _type_of(qkv, "qkv"), qs, _int32(n_heads, "n_heads"), *(C.byref(x) for x in self._c), op, os_)
 
     def __call__(self, stream: Optional[int] = None) -> None:
-        self._on_device()
+        self._on_device(stream)
         rc = lib.moqe_kv_append(*self._args, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
@@ -855,7 +855,7 @@ class KvAttentionCall(_DeviceCall):
         self._args = (qp, qs, *refs, op, os_, _ptr(workspace), workspace.numel())
 
     def __call__(self, stream: Optional[int] = None) -> None:
-        self._on_device()
+        self._on_device(stream)
         rc = lib.moqe_kv_attention(*self._args, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
@@ -926,7 +926,7 @@ class ResidualNormF8Call(ResidualNormCall):
         self._marshal(y, residual, out, residual_out, gate, gate_rows, scale, post, pre, *rows.tensors())
 
     def __call__(self, stream: Optional[int] = None) -> None:
-        self._on_device()
+        self._on_device(stream)
         rc = lib.moqe_residual_norm_f8(self._arg, C.byref(self._rows_c), _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
@@ -1043,7 +1043,7 @@ class F8GemmCall(_DeviceCall):
                       workspace.numel())
 
     def __call__(self, stream: Optional[int] = None) -> None:
-        self._on_device()
+        self._on_device(stream)
         rc = lib.moqe_f8_gemm(*self._args, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
@@ -1079,7 +1079,7 @@ class SampleCall(_DeviceCall):
                       _vector(logprobs, S, "logprobs"), _ptr(workspace), workspace.numel())
 
     def __call__(self, stream: Optional[int] = None) -> None:
-        self._on_device()
+        self._on_device(stream)
         rc = lib.moqe_sample(*self._args, _stream() if stream is None else stream)
         if rc != 0:
             _check(rc)
