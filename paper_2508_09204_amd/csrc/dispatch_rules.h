@@ -89,6 +89,11 @@ inline F8Shape f8_shape(long long M, int K, int tiles, bool gated, bool exact) {
   if (m > 8 && wgs(32, 8) >= enough) return {32, 8, 1, 0};
   return {0, gated || (m > 1 && (tiles > 512 || m > 16)) ? 2 : 1, 1, 1};
 }
+// Work-groups of a tile kernel's launch: as many row tiles as any buckets can make, a multiple of 8.  At most F8_MAX_WGS are launched.
+constexpr long long F8_MAX_WGS = (1ll << 23) - 1;
+inline long long f8_work_groups(const F8Shape& s, long long M, int K, int tiles) {
+  return s.rows == 0 ? 0 : (((M + s.rows - 1) / s.rows + K - 1) * ((tiles + s.cols - 1) / s.cols) + 7) / 8 * 8;
+}
 // Rows in 8 bits need a block of 128 features of a row in one work-group: 16 tiles of gated pairs.  Where there is none, results go through the workspace.
 inline bool f8_through_workspace(const F8Shape& s) { return s.rows == 0 || s.cols != 16; }
 

@@ -1,4 +1,5 @@
 // C-ABI entry points of rows, matrices and products in 8-bit floating point, and of sampling: argument checks on the host, then the launches.
+#include "dispatch_rules.h"
 #include "f8_device.h"
 
 namespace moqe {
@@ -137,6 +138,8 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
   } else {
     g.y = y->data; g.y_stride = y->stride; g.y_bf16 = y->type == MOQE_TYPE_BF16;
   }
+  const long long wgs = f8_work_groups(f8_shape(M, K, g.tiles, gated, g.exact), M, K, g.tiles);
+  if (wgs > F8_MAX_WGS) return set_error(MOQE_E_SHAPE, "%s: %lld work-groups", who, wgs);
   if (dry_run()) return MOQE_OK;
   return launch_f8_gemm(g, gated, workspace, static_cast<hipStream_t>(stream));
 }

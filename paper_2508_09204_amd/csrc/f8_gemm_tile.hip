@@ -1,4 +1,5 @@
 // Products of 8-bit rows and matrices, tile kernel for many rows.
+#include "dispatch_rules.h"
 #include "f8_device.h"
 
 namespace moqe {
@@ -292,9 +293,7 @@ static int32_t launch_tile(const F8Args& a, bool gated, hipStream_t st) {
   tg.w_bytes = uint32_t(size_t(a.scale_off) + size_t(a.tiles) * a.groups * 64);
   tg.col_tiles = (a.tiles + NT * 4 - 1) / (NT * 4);
   tg.group = 8;
-  const long long rt = (M + ROWS - 1) / ROWS + a.K - 1, wgs = (rt * tg.col_tiles + 7) / 8 * 8;
-  if (wgs >= (1ll << 23)) return set_error(MOQE_E_SHAPE, "moqe_f8_gemm: %lld work-groups", wgs);
-  const dim3 grid(static_cast<unsigned>(wgs)), block(256 * KS);
+  const dim3 grid(static_cast<unsigned>(f8_work_groups(F8Shape{ROWS, NT * 4, KS, 0}, M, a.K, a.tiles))), block(256 * KS);
   if (!gated) hipLaunchKernelGGL((k_f8_tile<MB, NT, KS, WD, F8_PLAIN, EXACT>), grid, block, 0, st, a, tg);
   else if (!a.y8) {
     if constexpr (NT > 1) hipLaunchKernelGGL((k_f8_tile<MB, NT, KS, WD, F8_GATED, EXACT>), grid, block, 0, st, a, tg);
