@@ -550,9 +550,10 @@ int32_t moqe_f8_unpack(const moqe_f8_mat* mat, const moqe_f8_rows* w, const moqe
  *             quantized from fp32; n <= 32768).  y and a must not overlap.
  *   flags   : MOQE_SCATTER_OUTPUT, MOQE_INPUT_IN_BUCKET_ORDER as in moqe_grouped_qgemm; MOQE_FAST_SUMS
  * Arithmetic: fp32 sums of exact products (codes times scales are exact in bf16, which the matrix cores multiply, but for
- * elements below 2^-126, which may count as zeros, and of 2^128 and more, which are infinite in fp32 too).  BF16 results, whose rounding hides the difference, and with MOQE_FAST_SUMS all,
+ * elements below 2^-126, which may count as zeros, and of 2^128 and more, which are infinite in fp32 too), whatever the results' type.  With MOQE_FAST_SUMS they
  * come from the matrix cores' products of codes, at twice the rate in large calls: those add eight neighbouring columns at a time, each product cut to 2^-13 of the largest one's power of two,
- * 1.4e-5 of the results in the mean square for normal values (8-bit results: one code in 1000 is a neighbour of what fp32 sums give).  The same call gives the same bits.
+ * 1.8e-5 of the results in the mean square for normal values.  BF16 results' own rounding is a hundred times that for most, but not for those far below the others, whose sums cancel; of
+ * 8-bit results one code in 1000 is a neighbour of what fp32 sums give.  The same call gives the same bits.
  * a stays below 4 GiB (S * T * code_stride).  NaN in a row of a makes NaN of that row, NaN in a row of a matrix of that feature. */
 #define MOQE_TYPE_F8     2
 #define MOQE_FAST_SUMS   8

@@ -1008,7 +1008,7 @@ def moqe_f8_gemm_workspace_bytes(experts: Sequence[F8Mat], S: int, T: int, y_typ
 
 class F8GemmCall(_DeviceCall):
     """moqe_f8_gemm with its arguments marshalled once and a workspace of its own.  a: S * T rows in 8 bits; y: fp32 or bf16 [S * T, n], or F8Rows (gated pairs).
-    Without offsets there is one matrix, for all rows (S: as many as a has, T 1, if not given).  fast: sums of the matrix cores' 8-bit products whatever the result's type (MOQE_FAST_SUMS)."""
+    Without offsets there is one matrix, for all rows (S: as many as a has, T 1, if not given).  fast: sums of the matrix cores' 8-bit products (MOQE_FAST_SUMS) instead of fp32 ones."""
 
     def __init__(self, a: F8Rows, experts: Sequence[F8Mat], y, offsets: Optional[torch.Tensor] = None, perm: Optional[torch.Tensor] = None,
                  S: Optional[int] = None, T: int = 1, scatter: bool = False, in_bucket_order: bool = False, workspace: Optional[torch.Tensor] = None,

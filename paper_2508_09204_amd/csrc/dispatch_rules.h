@@ -67,9 +67,9 @@ inline bool kv_few_rows(long long T, int group, int head_dim) { return T * group
 // waves; rows 0: the kernel for few rows, `blocks` blocks of 16 rows and `cols` tiles of 16 features to a work-group.
 //
 // The largest tile that still makes 160 work-groups (0.6 of the CUs), but not one with more rows than half of it is needed for: a larger one reads weights and activations less often, a smaller
-// one has more of them under way.  us, dense, bf16 results: 64 rows on 32000 x 4096: 64 x 128 (250 work-groups) 27.7, 64 x 256 (125) 39.2, 32 x 128 (500) 33.7; 128 rows: 64 x 256 (250) 38.8,
+// one has more of them under way.  us, dense, fast sums: 64 rows on 32000 x 4096: 64 x 128 (250 work-groups) 27.7, 64 x 256 (125) 39.2, 32 x 128 (500) 33.7; 128 rows: 64 x 256 (250) 38.8,
 // 128 x 256 (125) 48.7; 512 rows: 128 x 256 (500) 68.5, 64 x 256 (1000) 90.4; 512 rows on 4096 x 4096: 64 x 128 (256) 18.1, 64 x 256 (128) 30.4; 256 rows: 64 x 64 in two parts (256) 12.7,
-// 32 x 128 (256) 15.2, 64 x 128 (128) 17.7; 128 rows: 32 x 64 in four parts (256) 11.1, 64 x 64 in two parts (128) 12.6.  Products in bf16 (fp32 results) convert a wave's activations for all of
+// 32 x 128 (256) 15.2, 64 x 128 (128) 17.7; 128 rows: 32 x 64 in four parts (256) 11.1, 64 x 64 in two parts (128) 12.6.  Products in bf16 (fp32 sums) convert a wave's activations for all of
 // its features: 64 x 128 up to 400 work-groups of the next (128 rows on 32000 x 4096 43 / 54, 256 rows 77 / 74).
 // Few rows: one row on 32000 x 4096: few 23.5, 32 x 128 24.8; 16 rows 28.4 / 25.5; 16 rows on 4096 x 4096 7.2 / 14.7, 32 rows 7.8 / 15.5; 64 rows 10.4, 32 x 64 in four parts 11.0; four experts of
 // 11008 gated pairs x 4096, a mean of 4 rows 63 / 65, of 16 74.5 / 68, of 32 76 / 72; eight experts, a mean of 8 124 / 131.

@@ -131,7 +131,7 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
   g.offsets = offsets;
   g.a_perm = (flags & MOQE_INPUT_IN_BUCKET_ORDER) ? nullptr : perm;
   g.y_perm = (flags & MOQE_SCATTER_OUTPUT) ? perm : nullptr;
-  g.exact = y->type != MOQE_TYPE_BF16 && !(flags & MOQE_FAST_SUMS);
+  g.exact = !(flags & MOQE_FAST_SUMS);
   g.S = S; g.T = T; g.K = K; g.n = n; g.tiles = p.tiles; g.blocks = p.blocks; g.groups = p.groups; g.scale_off = uint32_t(p.scale_off);
   if (y->type == MOQE_TYPE_F8) {
     g.y8 = y->rows8.codes; g.y8_scales = y->rows8.scales; g.y8_stride = y->rows8.code_stride; g.y8_scale_stride = y->rows8.scale_stride;

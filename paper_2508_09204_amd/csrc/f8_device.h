@@ -113,9 +113,9 @@ __device__ __forceinline__ f8_f32x4 f8_mfma(const F8Frag& w, const F8Frag& x, co
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, c, 0, 0, J, int(ws), J, int(xs));
 }
 
-// That instruction adds 8 neighbouring columns at a time, each product cut to 2^-13 of the largest one's power of two: 1.4e-5 of the result in the mean square for normal operands, which is
-// a hundredth of what rounding to bf16 does, but 200 times what fp32 sums do.  Results in fp32, and in 8 bits, where it moves one code in a thousand to its neighbour, take products of bf16 instead
-// (unless the caller asks for the fast ones), at half the rate: codes times their scale are exact there.
+// That instruction adds 8 neighbouring columns at a time, each product cut to 2^-13 of the largest one's power of two: 1.8e-5 of the result in the mean square for normal operands, which is
+// 200 times what fp32 sums do, and more than a rounding to bf16 for results far below the others.  So products of bf16, at half the rate, unless the caller asks for the fast ones: codes times
+// their scale are exact there.
 __device__ __forceinline__ float f8_scale(uint32_t byte) { return __uint_as_float((byte & 255) << 23); }
 __device__ __forceinline__ f8_bf16x8 f8_exact(uint32_t lo, uint32_t hi, float scale) {
   union { f8_bf16x2 p[4]; f8_bf16x8 v; } u;

@@ -12,7 +12,7 @@ equally long; ragged rows, prefixes, biases by distance, gates and norms behind 
 A model with a `head` goes on to tokens: `Draw` is the vocabulary's product on the last row of every sequence and moqe_sample, `Generator` a prompt and single tokens, the latter captured with
 embedding, layers, head and sampling in one graph.
 
-    python -m paper_2508_09204_amd.decoder --prompt 512 --tokens 64 [--f8] [--vocabulary 32000]
+    python -m paper_2508_09204_amd.decoder --prompt 512 --tokens 64 [--f8] [--fast-sums] [--vocabulary 32000]
 
 times prompts and single tokens of a few layers on seeded synthetic weights and prints one JSON line.
 """
@@ -46,20 +46,22 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, stretch: float = 1.0,
 
 @dataclass
 class F8Mlp:
-    """A SILU_MLP block in 8-bit floating point: a gated pair [f, d] and a matrix [d, f] per expert, or one of each for all.  fast: sums of the first product as binding.F8GemmCall has them."""
+    """A SILU_MLP block in 8-bit floating point: a gated pair [f, d] and a matrix [d, f] per expert, or one of each for all.  fast: both products with fast sums (binding.F8GemmCall)."""
     gate_up: List[mq.F8Mat]
     down: List[mq.F8Mat]
-    fast: bool = True
+    fast: bool = False
 
 
 @dataclass
 class Layer:
-    """qkv and out: a packed matrix per expert, [(n_heads + 2 kv heads) * head_dim, d] and [d, n_heads * head_dim], or one F8Mat for all; mlp: a block on d features."""
+    """qkv and out: a packed matrix per expert, [(n_heads + 2 kv heads) * head_dim, d] and [d, n_heads * head_dim], or one F8Mat for all; mlp: a block on d features.  fast: those projections that
+    are in 8 bits with fast sums (binding.F8GemmCall)."""
     attn_norm: mq.Norm
     qkv: Union[List[mq.QMat], List[mq.F8Mat]]
     out: Union[List[mq.QMat], List[mq.F8Mat]]
     mlp_norm: mq.Norm
     mlp: Union[mq.Block, F8Mlp]
+    fast: bool = False
 
 
 @dataclass
@@ -147,17 +149,18 @@ class Step:
         self.workspace = ws
         self._calls = self._norm(None, first.attn_norm, first.qkv)
         for i, layer in enumerate(model.layers):
-            self._calls += self._product(self.normed, self.normed8, layer.qkv, self.qkv)
+            self._calls += self._product(self.normed, self.normed8, layer.qkv, self.qkv, layer.fast)
             self._calls += [mq.KvAppendCall(self.qkv, model.n_heads, model.rope, batch, seqs.caches[i], self.q),
                             mq.KvAttentionCall(self.q, attn, batch, seqs.caches[i], self.att, ws)]
             if _f8(layer.out):
                 self._calls.append(mq.ResidualNormF8Call(None, self.att, self.att8))
             y = self.y16 if _f8(layer.out) else self.y
-            self._calls += self._product(self.att, self.att8, layer.out, y)
+            self._calls += self._product(self.att, self.att8, layer.out, y, layer.fast)
             self._calls += self._norm(y, layer.mlp_norm, layer.mlp)
             if _f8(layer.mlp):
                 y = self.y16
-                self._calls += self._product(None, self.normed8, layer.mlp.gate_up, self.h8, layer.mlp.fast) + self._product(None, self.h8, layer.mlp.down, y)
+                self._calls += self._product(None, self.normed8, layer.mlp.gate_up, self.h8, layer.mlp.fast)
+                self._calls += self._product(None, self.h8, layer.mlp.down, y, layer.mlp.fast)
             else:
                 y = self.y
                 self._calls.append(self._mlp(layer.mlp, ws))
@@ -296,9 +299,9 @@ class Generator:
 
 
 def synthetic(layers: int, d: int, f: int, n_heads: int, kv_heads: int, head_dim: int, experts, router_hidden: int = 0, seed: int = 0, theta: float = 1e4,
-              head_norms: bool = False, cap: float = 0.0, window: int = 0, device="cuda", vocabulary: int = 0) -> Decoder:
+              head_norms: bool = False, cap: float = 0.0, window: int = 0, device="cuda", vocabulary: int = 0, fast: bool = False) -> Decoder:
     """A decoder of seeded normal weights; experts: (bits, group, symmetric) each, all quantized from the same weights, or a number: so many MLP blocks of their own in 8-bit floating point
-    between projections in 8 bits that all share.  vocabulary: tokens of an embedding and a head, 0: none."""
+    between projections in 8 bits that all share.  vocabulary: tokens of an embedding and a head, 0: none.  fast: fast sums of 8-bit products, but the head's."""
     from . import experts as ex
     gen = torch.Generator(device=device).manual_seed(seed)
     rand = lambda *shape, by=1.0: torch.randn(shape, generator=gen, device=device) * by  # noqa: E731
@@ -312,13 +315,13 @@ def synthetic(layers: int, d: int, f: int, n_heads: int, kv_heads: int, head_dim
     def mlp():
         if not eight:
             return mq.Block(kind=mq.KIND_SILU_MLP, router=router, w0=matrix(f, d), w1=matrix(f, d), w2=matrix(d, f))
-        return F8Mlp([ex.quantize_f8(rand(f, d, by=d ** -0.5), rand(f, d, by=d ** -0.5)) for _ in range(K)], [ex.quantize_f8(rand(d, f, by=f ** -0.5)) for _ in range(K)])
+        return F8Mlp([ex.quantize_f8(rand(f, d, by=d ** -0.5), rand(f, d, by=d ** -0.5)) for _ in range(K)], [ex.quantize_f8(rand(d, f, by=f ** -0.5)) for _ in range(K)], fast)
 
     K = experts if eight else len(experts)
     hidden = router_hidden
     router = mq.Router(rand(hidden, d, by=d ** -0.5) if hidden else None, torch.zeros(hidden, device=device) if hidden else None,
                        rand(K, hidden or d, by=(hidden or d) ** -0.5), None, d, hidden, K)
-    made = [Layer(norm(d), matrix((n_heads + 2 * kv_heads) * head_dim, d), matrix(d, n_heads * head_dim), norm(d), mlp()) for _ in range(layers)]
+    made = [Layer(norm(d), matrix((n_heads + 2 * kv_heads) * head_dim, d), matrix(d, n_heads * head_dim), norm(d), mlp(), fast) for _ in range(layers)]
     gains = [1.0 + 0.1 * rand(head_dim) if head_norms else None for _ in range(2)]
     rope = mq.Rope(rope_frequencies(head_dim, theta, device=device), head_dim, q_gain=gains[0], k_gain=gains[1])
     model = Decoder(made, norm(d), router, rope, n_heads, kv_heads, head_dim, cap, window, residual_scale=(2 * layers) ** -0.5)
@@ -334,11 +337,12 @@ def main() -> None:
     ap.add_argument("--tokens", type=int, default=64)
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--f8", action="store_true", help="projections and experts in 8-bit floating point")
+    ap.add_argument("--fast-sums", action="store_true", help="fast sums of products in 8-bit floating point")
     ap.add_argument("--vocabulary", type=int, default=0, help="draw tokens of so many (0: rows go in and out)")
     a = ap.parse_args()
     S, d, heads = a.sequences, 4096, 32
     experts = 4 if a.f8 else [(4, 128, False), (4, 128, False), (3, 128, False), (8, 0, True)]
-    model = synthetic(a.layers, d, 11008, heads, heads, 128, experts, router_hidden=256, vocabulary=a.vocabulary)
+    model = synthetic(a.layers, d, 11008, heads, heads, 128, experts, router_hidden=256, vocabulary=a.vocabulary, fast=a.fast_sums)
     gen = torch.Generator(device="cuda").manual_seed(1)
     marks = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
     if a.vocabulary:
