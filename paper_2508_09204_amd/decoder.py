@@ -270,11 +270,11 @@ class Generator:
 
     def start(self, prompt: torch.Tensor, u: torch.Tensor) -> torch.Tensor:
         check_tokens(prompt, self.seqs.S, self.prompt.T, self.model.head.n)
+        self.first.u.copy_(u)                            # refused, if it does not fit, while nothing has changed
         self.seqs.clear()
         embed(self.model.embedding, prompt.reshape(-1), self.prompt.x)
         self.seqs.route(self.model, self.prompt.x.bfloat16(), self.prompt.T)
         self.prompt()
-        self.first.u.copy_(u)
         self.draw.tokens.copy_(self.first())
         return self.draw.tokens
 
@@ -286,8 +286,8 @@ class Generator:
     def next(self, u: torch.Tensor) -> torch.Tensor:
         if self.seqs.tokens + 1 > self.seqs.max_tokens:
             raise ValueError(f"{self.seqs.tokens} tokens, sequences hold {self.seqs.max_tokens}")
-        self.seqs.tokens += 1
         self.draw.u.copy_(u)
+        self.seqs.tokens += 1
         if self._graph is None:
             self._enqueue()                              # what a process does once is done before the capture
             self._graph = torch.cuda.CUDAGraph()
