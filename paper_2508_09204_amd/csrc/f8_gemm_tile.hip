@@ -26,13 +26,14 @@ struct F8TileGeom {
 //
 // Activations go from memory to LDS directly, 16 bytes a lane swizzled by the row, so that operand reads are free of bank conflicts; weights never touch LDS, they lie in memory as the operands
 // they are.  One barrier a block.  The scale of a row and block is the instruction's own operand, a byte of a dword that holds four blocks': nothing is multiplied.
-// Bound by the matrix cores, and by power: 8192 rows, k 11008, n 4096 in 270 to 290 us, 2560 to 2740 TFLOP/s at about 2 GHz (a library product in fp8 with one scale 2690 on 8192^3; nothing but products
+// Fast sums are bound by the matrix cores, and by power: 8192 rows, k 11008, n 4096 in 270 to 290 us, 2560 to 2740 TFLOP/s at about 2 GHz (a library product in fp8 with one scale 2690 on 8192^3; nothing but products
 // from registers 3900); the products take 60 % of the time that a SIMD has.  What it took:
 //  * two work-groups to a CU (128 x 256, 251 registers) instead of one (256 x 256): 333 -> 299 us;
 //  * memory requests spread over the row blocks' products: as one burst at the head of a block, products wait behind them in the wave's order of issue: 305 -> 286, 2048 rows of 4096 x 4096 41 -> 36;
 //  * operands of the next row block read ahead of this one's products: 273 -> 270, 33.4 -> 31.4.
 // No gain: activations three blocks ahead (7 % slower), priorities for products, groups of 16 row tiles, 32x32x64 products in a probe (no faster).
-// EXACT: codes times scales as bf16 operands, 16x16x32 products: 4096^3 in 108 us, 1270 TFLOP/s, as a library bf16 product; a wave converts its activations itself.
+// EXACT: codes times scales as bf16 operands, 16x16x32 products: 4096^3 in 108 us, 1270 TFLOP/s, as a library bf16 product, 8192 rows, k 11008, n 4096 in 556, 1330; a wave converts its activations
+// itself.
 template <int MB, int NT, int KS, int WD, int OUT, bool EXACT>
 __global__ __launch_bounds__(256 * KS, KS > 1 ? 1 : MB * NT <= 8 && !EXACT ? 3 : 2) void k_f8_tile(F8Args a, F8TileGeom tg) {
   constexpr int ROWS = MB * 16, AL = (MB + 1) / 2, STAGED = ROWS < 32 ? 32 : ROWS;      // AL: requests of a wave for a block's activations
