@@ -574,9 +574,9 @@ int32_t moqe_f8_gemm(const moqe_f8_rows* a, const int32_t* offsets, const int32_
  *   logits   : MOQE_TYPE_F32 or MOQE_TYPE_BF16, aligned to the type, row s at element s * stride (at least V);  V <= 2^20, S <= 65535
  *   u        : device float [S] (taken into [0, 1]; NaN is 0);  tokens: device int32 [S];  logprobs: device float [S] or NULL
  * Minus infinity and NaN are never taken; a row without anything else gives token -1 and log probability minus infinity.  Infinite logits share all of the weight.
- * Weights are in 64 bits, summed as integers, first over 256 neighbours (rows without filters) or the logits of a quarter of an octave (the cuts), in 2^-43 of the power of two above
- * the largest of these, then in whole 2^-43 of that above the row's largest, in which single weights count where filters leave them.  What a row draws depends on its logits, its settings and u alone,
- * not on the other rows or how the work is divided.  Running weights are within V * 2^-40 of the largest weight.
+ * What a row draws depends on its logits, its settings and u alone, not on the other rows or on how the work is divided.  Weights are in 64 bits and are summed as integers: rows without
+ * filters over 256 neighbours in 2^-43 of the power of two above the largest of these, cuts over bins of a quarter of an octave likewise, everything else in units of 2^-43 of the power of two
+ * above the row's largest, to which those sums are cut.  Running weights are within V * 2^-40 of the largest weight.
  * Log probabilities are never above 0, and 0 of a token that is the only one kept; they are within 2^-24 of themselves and V * 2^-40.
  * Workspace as the query says, 256-byte aligned.  S == 0 is a no-op. */
 typedef struct moqe_sampling { const float* temperature; const int32_t* top_k; const float *top_p, *min_p; } moqe_sampling;
